@@ -322,6 +322,98 @@ ADASUM_API int adasum_group_combine(const void* const* x, int R,
                          int dtype, const double* weights,
                          void* out, int out_dtype, double* sqnorm, void* stream);
 
+/* ---- the gradients that fill a worker's buffer ----
+ *
+ * What a training program computes a layer's gradient from, written where the reduction above reads it: at
+ * `offset` (elements) of the worker's flat buffer, layer_offsets[l] for layer l, in the buffer's storage type,
+ * whatever alignment that place has.  Nothing outside the layer is touched.  The entry points below follow the
+ * conventions at the top.  None of them allocates, keeps anything between calls or synchronises, so all may be
+ * captured; what they need beside their operands is a DEVICE workspace of the caller (256-byte aligned; its
+ * contents do not matter), which calls that may overlap in time must not share.
+ *
+ * A matrix of n rows is given by its first element, which is 16-byte aligned, and the distance of two rows in
+ * elements (`..._stride`).  Rows that are written lie at least their width apart; rows that are only read may
+ * lie closer, or all be the same one (stride 0).  n = 0 and width 0 are allowed.
+ * Storage types: any of ADASUM_F32, ADASUM_BF16 and ADASUM_F16 goes with any other of the three, ADASUM_F64
+ * only with itself and not with checkpoints (else ADASUM_ERR_UNSUPPORTED).  Sums are formed in fp32 or more
+ * (fp64 for fp64) and rounded once to the result's type, with `accumulate` after what the layer held is added.
+ * `accumulate` = 0 overwrites the layer, 1 adds to what it holds (micro-batches, or a table that is also an
+ * output layer).
+ */
+#define ADASUM_ID_I32 0
+#define ADASUM_ID_I64 1
+
+/*
+ * Rows of an embedding table that lies at `offset` of a flat parameter buffer:
+ *   out[t][:] = scale * table[ids[t]][:],   table = params[offset .. offset + rows * width)
+ * An id outside [0, rows) (padding) gives a row of zeros.  `out` must not overlap params' table or ids
+ * (ADASUM_ERR_ALIAS).  rows and n_ids at most 2^31 - 65536, width at most 2^24.
+ */
+ADASUM_API int adasum_embedding(const void* params, int dtype, int64_t offset, int64_t rows, int64_t width,
+                                const void* ids, int id_type, int64_t n_ids, double scale,
+                                void* out, int out_dtype, int64_t out_stride, void* stream);
+
+/*
+ * The table's gradient:  grad[offset + v * width + j] (+)= scale * sum over t with ids[t] = v of dy[t][j].
+ * Ids outside [0, rows) are left out, whatever their row of dy holds.  The tokens are sorted by id and every
+ * row's sum runs over its tokens in ascending t: up to 32 of them in fp32, such runs in fp64.  No atomic additions
+ * to results: bit-identical from run to run.  With `accumulate` rows that no token names are not touched.
+ * `dtype`: of dy, on which (and on nothing in the data) the workspace's size depends.
+ */
+ADASUM_API int adasum_embedding_grad_workspace_bytes(int64_t rows, int64_t width, int64_t n_ids, int dtype,
+                                                     size_t* bytes);
+ADASUM_API int adasum_embedding_grad(const void* dy, int dtype, int64_t dy_stride,
+                                     const void* ids, int id_type, int64_t n_ids, double scale,
+                                     void* grad, int grad_dtype, int64_t offset, int64_t rows, int64_t width,
+                                     int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Activations kept for the backward pass in 8 bits.  Blocks of ADASUM_CHECKPOINT_BLOCK consecutive channels of a
+ * row (the last may be shorter) share an exponent e:
+ *   e = floor(log2(max |x|)) - 6, but at least -120 (also for a block of zeros);
+ *   q = x / 2^e rounded to nearest even, and to at most 127 in magnitude;   x is kept as q * 2^e.
+ * That is off by at most half of 2^e (all of it where |x| / 2^e > 127), which is at most 2^-7 (2^-6) of the block's
+ * largest value, and by at most 2^-121 in blocks below 2^-114.  q * 2^e has seven significant bits: it is a value of the type that x had, so that what follows computes
+ * with exactly what is kept.  A block with an infinity or NaN in it is kept as NaN (e = -128).
+ * Layout: rows x pitch bytes of q (int8; pitch = width rounded up to a whole block, zeros behind the last
+ * channel), then rows x (pitch / 32) bytes of e (int8): adasum_checkpoint_bytes in all, 16-byte aligned.
+ * rows at most 2^31 - 65536, width at most 2^24.
+ */
+#define ADASUM_CHECKPOINT_BLOCK 32
+ADASUM_API int adasum_checkpoint_bytes(int64_t rows, int64_t width, size_t* bytes);
+ADASUM_API int adasum_checkpoint_store(const void* x, int dtype, int64_t x_stride, int64_t rows, int64_t width,
+                                       void* checkpoint, void* stream);
+/* out = q * 2^e, in `dtype`. */
+ADASUM_API int adasum_checkpoint_load(const void* checkpoint, int64_t rows, int64_t width,
+                                      void* out, int dtype, int64_t out_stride, void* stream);
+
+/*
+ * Gradient through an activation function whose input x was kept:  dx = dy * act'(x), both of `dtype`.
+ * `dx` may be `dy` itself (same stride); any other overlap is ADASUM_ERR_ALIAS.  relu'(0) = 0.
+ */
+#define ADASUM_ACT_RELU      0
+#define ADASUM_ACT_GELU      1   /* x Phi(x) */
+#define ADASUM_ACT_GELU_TANH 2   /* x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) */
+#define ADASUM_ACT_SILU      3   /* x / (1 + exp(-x)) */
+ADASUM_API int adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows, int64_t width, int act,
+                                          const void* dy, int dtype, int64_t dy_stride,
+                                          void* dx, int64_t dx_stride, void* stream);
+
+/*
+ * Gradients of a linear layer y = W x + b (W: outputs x width, row-major) whose input x was kept:
+ *   grad[offset + o * width + i]  (+)= sum_t dy[t][o] * x[t][i]
+ *   grad[bias_offset + o]         (+)= sum_t dy[t][o]           (bias_offset < 0: no bias)
+ * The products are exact (matrix cores; fp32 dy as three bf16 parts) and summed in fp32.  With `dtype`
+ * ADASUM_F16 the kept values must be fp16's own: a checkpoint of fp16 activations (others are rounded to
+ * fp16).  rows, width and outputs as above; outputs at most 2^24.
+ */
+ADASUM_API int adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t width, int64_t outputs,
+                                                             int dtype, size_t* bytes);
+ADASUM_API int adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t width,
+                                             const void* dy, int dtype, int64_t dy_stride, int64_t outputs,
+                                             void* grad, int grad_dtype, int64_t offset, int64_t bias_offset,
+                                             int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- host-side planning, exposed for inspection and tests (no GPU needed) ---- */
 
 typedef struct adasum_tile {

@@ -24,11 +24,17 @@ OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_MISALIGNED = -1, -2, -3
 ERR_OUT_OF_MEMORY, ERR_HIP, ERR_WORKSPACE, ERR_ALIAS, ERR_TOO_LARGE = -4, -5, -6, -7, -8
 NOALLOC_SCRATCH_BYTES = 64 << 20
+ID_I32, ID_I64 = 0, 1
+ACTS = {"relu": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
+CHECKPOINT_BLOCK = 32
 
 EXPORTS = [
     "adasum_reduce", "adasum_reduce_ex", "adasum_reduce_noalloc", "adasum_workspace_bytes",
     "adasum_plan_create", "adasum_plan_execute", "adasum_plan_workspace_bytes", "adasum_plan_destroy",
     "adasum_group_gram", "adasum_group_weights", "adasum_group_combine",
+    "adasum_embedding", "adasum_embedding_grad_workspace_bytes", "adasum_embedding_grad",
+    "adasum_checkpoint_bytes", "adasum_checkpoint_store", "adasum_checkpoint_load", "adasum_checkpoint_act_grad",
+    "adasum_checkpoint_weight_grad_workspace_bytes", "adasum_checkpoint_weight_grad",
     "adasum_tile_capacity", "adasum_plan_tiles", "adasum_plan_levels", "adasum_plan_groups",
     "adasum_profile_enable", "adasum_profile_collect",
     "adasum_strerror", "adasum_last_hip_error", "adasum_version", "adasum_shutdown",
@@ -94,6 +100,16 @@ def load() -> C.CDLL:
     lib.adasum_group_weights.argtypes = [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
     lib.adasum_group_combine.argtypes = [pp, C.c_int, i64p, C.c_int, C.c_int, C.c_void_p, C.c_void_p,
                                          C.c_int, C.c_void_p, C.c_void_p]
+    vp, i32, i64, szp = C.c_void_p, C.c_int, C.c_int64, C.POINTER(C.c_size_t)
+    lib.adasum_embedding.argtypes = [vp, i32, i64, i64, i64, vp, i32, i64, C.c_double, vp, i32, i64, vp]
+    lib.adasum_embedding_grad_workspace_bytes.argtypes = [i64, i64, i64, i32, szp]
+    lib.adasum_embedding_grad.argtypes = [vp, i32, i64, vp, i32, i64, C.c_double, vp, i32, i64, i64, i64, i32, vp, C.c_size_t, vp]
+    lib.adasum_checkpoint_bytes.argtypes = [i64, i64, szp]
+    lib.adasum_checkpoint_store.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+    lib.adasum_checkpoint_load.argtypes = [vp, i64, i64, vp, i32, i64, vp]
+    lib.adasum_checkpoint_act_grad.argtypes = [vp, i64, i64, i32, vp, i32, i64, vp, i64, vp]
+    lib.adasum_checkpoint_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32, szp]
+    lib.adasum_checkpoint_weight_grad.argtypes = [vp, i64, i64, vp, i32, i64, i64, vp, i32, i64, i64, i32, vp, C.c_size_t, vp]
     lib.adasum_tile_capacity.argtypes = []
     lib.adasum_plan_tiles.argtypes = [i64p, C.c_int, C.c_int64, C.POINTER(Tile), C.c_int64, i64p]
     lib.adasum_plan_levels.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_int), C.c_int, C.POINTER(C.c_int)]
@@ -384,6 +400,231 @@ def adasum_group_combine(xs: Sequence, layer_offsets: Sequence[int], weights, *,
                                    C.c_void_p(out.data_ptr()), out_code,
                                    C.c_void_p(sq.data_ptr()) if sq is not None else None, _stream(stream)))
     return out, sq
+
+
+# ---- the gradients that fill a worker's buffer ----------------------------------------
+
+def _rows_of(t, width=None, what="tensor"):
+    """(rows, width, distance of two rows) of a device tensor whose last dimension is contiguous: a matrix, or any
+    contiguous tensor with its leading dimensions taken together."""
+    if not t.is_cuda:
+        raise ValueError("libadasum works on device memory only (no CPU path)")
+    if t.dim() < 2:
+        raise ValueError(f"{what} must have rows: at least two dimensions")
+    w = t.shape[-1]
+    if width is not None and w != width:
+        raise ValueError(f"{what} must have rows of {width} elements")
+    if t.dim() == 2:
+        if w > 1 and t.stride(1) != 1:
+            raise ValueError(f"the rows of {what} must be contiguous")
+        return t.shape[0], w, t.stride(0)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be a matrix or contiguous")
+    return (t.numel() // w if w else 0), w, w
+
+
+def _flat(t, offset, elems, what):
+    """A flat buffer that holds `elems` elements at `offset`."""
+    if not t.is_cuda:
+        raise ValueError("libadasum works on device memory only (no CPU path)")
+    if t.dim() != 1 or not t.is_contiguous() or offset < 0 or offset + elems > t.numel():
+        raise ValueError(f"{what} must be a contiguous 1-D buffer that holds the layer at its offset")
+
+
+def _id_type(ids) -> int:
+    import torch
+    if not ids.is_cuda or not ids.is_contiguous() or ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError("ids must be a contiguous int32 or int64 device tensor")
+    return ID_I64 if ids.dtype == torch.int64 else ID_I32
+
+
+def _same_device(first, *others):
+    dev = first.get_device()
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("all tensors must be on one device")
+    return dev
+
+
+def _call(fn, dev, stream, *args):
+    """The library launches on the current device: make that the tensors'."""
+    import torch
+    if dev == torch.cuda.current_device():
+        check(fn(*args, _stream(stream)))
+    else:
+        with torch.cuda.device(dev):
+            check(fn(*args, _stream(stream)))
+
+
+def _empty(shape, dtype, dev, stream):
+    """A new tensor for work on `stream` (None: the device's current one): memory of that stream, so that nothing that still
+    runs on another has it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _scratch(workspace, need, dev, stream):
+    import torch
+    if workspace is None:
+        return _empty(need, torch.uint8, dev, stream) if need else None
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the device of the operands")
+    return workspace
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def adasum_embedding(params, offset: int, rows: int, width: int, ids, *, scale: float = 1.0, out=None, out_dtype=None, stream=None):
+    """``scale * table[ids]`` for the table of ``rows`` x ``width`` that lies at ``offset`` of the flat buffer ``params``; rows of
+    zeros where an id names no row.  Returns ``out``, [*ids.shape, width] (made here when None)."""
+    lib = load()
+    _flat(params, offset, rows * width, "params")
+    id_type = _id_type(ids)
+    n = ids.numel()
+    if out is None:
+        out = _empty((*ids.shape, width), out_dtype or params.dtype, params.get_device(), stream)
+        stride = width
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise ValueError("out has the wrong dtype")
+        have, _, stride = _rows_of(out, width, "out")
+        if have != n and width:
+            raise ValueError("out must have a row for every id")
+    dev = _same_device(params, ids, out)
+    _call(lib.adasum_embedding, dev, stream, params.data_ptr(), _dtype_code(params), offset, rows, width, ids.data_ptr(), id_type, n, scale,
+          out.data_ptr(), _dtype_code(out), stride)
+    return out
+
+
+def adasum_embedding_grad_workspace_bytes(rows: int, width: int, n_ids: int, dtype) -> int:
+    n = C.c_size_t(0)
+    check(load().adasum_embedding_grad_workspace_bytes(rows, width, n_ids, _code_of(dtype), C.byref(n)))
+    return int(n.value)
+
+
+def adasum_embedding_grad(dy, ids, grad, offset: int, rows: int, *, scale: float = 1.0, accumulate: bool = False, workspace=None,
+                          stream=None):
+    """Writes (or, with ``accumulate``, adds) the gradient of a table of ``rows`` rows, ``scale`` times the sums of the rows of ``dy``
+    ([*ids.shape, width]) with one id, at ``offset`` of the flat buffer ``grad``.  Returns ``grad``."""
+    lib = load()
+    n, width, stride = _rows_of(dy, None, "dy")
+    id_type = _id_type(ids)
+    if ids.numel() != n and width:
+        raise ValueError("dy must have a row for every id")
+    _flat(grad, offset, rows * width, "grad")
+    dev = _same_device(grad, dy, ids)
+    code = _dtype_code(dy)
+    if workspace is None:
+        workspace = _scratch(None, adasum_embedding_grad_workspace_bytes(rows, width, n, dy.dtype), dev, stream)
+    else:
+        workspace = _scratch(workspace, 0, dev, stream)
+    _call(lib.adasum_embedding_grad, dev, stream, dy.data_ptr(), code, stride, ids.data_ptr(), id_type, n, scale, grad.data_ptr(),
+          _dtype_code(grad), offset, rows, width, 1 if accumulate else 0, _address(workspace),
+          0 if workspace is None else workspace.numel() * workspace.element_size())
+    return grad
+
+
+class Checkpoint:
+    """``rows`` x ``width`` activations of ``dtype`` in 8 bits (see ``include/adasum.h`` for the layout of ``data``, a 1-D tensor
+    of bytes, made here when None)."""
+
+    def __init__(self, rows: int, width: int, dtype, *, device=None, data=None):
+        import torch
+        n = C.c_size_t(0)
+        check(load().adasum_checkpoint_bytes(rows, width, C.byref(n)))
+        if dtype not in (torch.float32, torch.bfloat16, torch.float16):
+            raise ValueError("checkpoints hold float32, bfloat16 or float16 activations")
+        if data is None:
+            data = torch.empty(n.value, dtype=torch.int8, device="cuda" if device is None else device)
+        elif data.dim() != 1 or data.element_size() != 1 or data.numel() != n.value or not data.is_contiguous():
+            raise ValueError(f"data must be a contiguous 1-D tensor of {n.value} bytes")
+        self.rows, self.width, self.dtype, self.data = rows, width, dtype, data
+
+
+def adasum_checkpoint_store(x, *, out: Optional[Checkpoint] = None, stream=None) -> Checkpoint:
+    """Keeps ``x`` ([..., width]) in 8 bits.  Returns the checkpoint (made here when None)."""
+    lib = load()
+    n, width, stride = _rows_of(x, None, "x")
+    if out is None:
+        size = C.c_size_t(0)
+        check(lib.adasum_checkpoint_bytes(n, width, C.byref(size)))
+        import torch
+        out = Checkpoint(n, width, x.dtype, data=_empty(size.value, torch.int8, x.get_device(), stream))
+    elif (out.rows, out.width, out.dtype) != (n, width, x.dtype):
+        raise ValueError("the checkpoint was made for another shape or dtype")
+    dev = _same_device(x, out.data)
+    _call(lib.adasum_checkpoint_store, dev, stream, x.data_ptr(), _dtype_code(x), stride, n, width, out.data.data_ptr())
+    return out
+
+
+def adasum_checkpoint_load(checkpoint: Checkpoint, *, out=None, stream=None):
+    """What a checkpoint keeps, [rows, width] in its dtype or that of ``out``."""
+    if out is None:
+        out = _empty((checkpoint.rows, checkpoint.width), checkpoint.dtype, checkpoint.data.get_device(), stream)
+    n, width, stride = _rows_of(out, checkpoint.width, "out")
+    if n != checkpoint.rows and width:
+        raise ValueError("out must have a row for every one of the checkpoint")
+    dev = _same_device(checkpoint.data, out)
+    _call(load().adasum_checkpoint_load, dev, stream, checkpoint.data.data_ptr(), checkpoint.rows, checkpoint.width, out.data_ptr(),
+          _dtype_code(out), stride)
+    return out
+
+
+def adasum_checkpoint_act_grad(checkpoint: Checkpoint, dy, act: str, *, out=None, stream=None):
+    """``dy`` times the slope of the activation function ``act`` ("relu", "gelu", "gelu_tanh", "silu") at the kept input.  ``out``
+    may be ``dy``."""
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {', '.join(ACTS)}")
+    n, width, stride = _rows_of(dy, checkpoint.width, "dy")
+    if n != checkpoint.rows and width:
+        raise ValueError("dy must have a row for every one of the checkpoint")
+    if out is None:
+        out = _empty(tuple(dy.shape), dy.dtype, dy.get_device(), stream)
+    m, _, out_stride = _rows_of(out, width, "out")
+    if (m != n and width) or out.dtype != dy.dtype:
+        raise ValueError("out must have the rows and dtype of dy")
+    dev = _same_device(checkpoint.data, dy, out)
+    _call(load().adasum_checkpoint_act_grad, dev, stream, checkpoint.data.data_ptr(), n, width, ACTS[act], dy.data_ptr(), _dtype_code(dy),
+          stride, out.data_ptr(), out_stride)
+    return out
+
+
+def adasum_checkpoint_weight_grad_workspace_bytes(rows: int, width: int, outputs: int, dtype) -> int:
+    n = C.c_size_t(0)
+    check(load().adasum_checkpoint_weight_grad_workspace_bytes(rows, width, outputs, _code_of(dtype), C.byref(n)))
+    return int(n.value)
+
+
+def adasum_checkpoint_weight_grad(checkpoint: Checkpoint, dy, grad, offset: int, *, bias_offset: Optional[int] = None,
+                                  accumulate: bool = False, workspace=None, stream=None):
+    """Writes (or adds) the gradient of a linear layer's weight, [outputs, width], at ``offset`` of the flat buffer ``grad``, and that
+    of its bias at ``bias_offset`` (None: it has none), from the kept input and ``dy`` ([..., outputs]).  Returns ``grad``."""
+    import torch
+    lib = load()
+    n, outputs, stride = _rows_of(dy, None, "dy")
+    width = checkpoint.width
+    if n != checkpoint.rows and outputs:
+        raise ValueError("dy must have a row for every one of the checkpoint")
+    if dy.dtype == torch.float16 and checkpoint.dtype != torch.float16:
+        raise ValueError("a float16 dy needs a checkpoint of float16 activations")
+    _flat(grad, offset, outputs * width, "grad")
+    if bias_offset is not None:
+        _flat(grad, bias_offset, outputs, "grad")
+    dev = _same_device(grad, checkpoint.data, dy)
+    code = _dtype_code(dy)
+    if workspace is None:
+        workspace = _scratch(None, adasum_checkpoint_weight_grad_workspace_bytes(checkpoint.rows, width, outputs, dy.dtype), dev, stream)
+    else:
+        workspace = _scratch(workspace, 0, dev, stream)
+    _call(lib.adasum_checkpoint_weight_grad, dev, stream, checkpoint.data.data_ptr(), checkpoint.rows, width, dy.data_ptr(), code, stride,
+          outputs, grad.data_ptr(), _dtype_code(grad), offset, -1 if bias_offset is None else bias_offset, 1 if accumulate else 0,
+          _address(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+    return grad
 
 
 # ---- planning (host only) ---------------------------------------------------------

@@ -1572,6 +1572,12 @@ int reduce_noalloc_impl(const void* const* grads, int K, const int64_t* layer_of
 }
 
 }  // namespace
+
+int hip_failure(int hip_error) {
+    g_last_hip_error = hip_error;
+    return hip_error == static_cast<int>(hipErrorOutOfMemory) ? ADASUM_ERR_OUT_OF_MEMORY : ADASUM_ERR_HIP;
+}
+
 }  // namespace adasum
 
 using namespace adasum;

@@ -1,0 +1,235 @@
+// gfx950 kernels of activation checkpoints in 8 bits: store, load, and the gradient through an activation function whose input is
+// a checkpoint.  (The gradients of a linear layer from one are in adasum_weight_grad.hip.)
+//
+// All three stream: a lane takes eight channels of a row, four lanes a block of 32 that shares an exponent.  The exponent comes
+// from the bits of the block's largest magnitude, scaling by a power of two is exact, and the sum with 3 * 2^22 rounds to nearest
+// even and leaves the whole number in the low byte.
+#include <hip/hip_runtime.h>
+
+#include "adasum_layers.h"
+#include "adasum_rows.h"
+
+namespace adasum {
+namespace {
+
+constexpr int kG = 8;            // channels of a lane
+constexpr int kThreadsRow = 256;
+
+__device__ __forceinline__ unsigned quad_max(unsigned v) {
+    v = max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0xb1, 0xf, 0xf, true)));   // lanes 1 0 3 2
+    return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4e, 0xf, 0xf, true)));   // 2 3 0 1
+}
+
+// 2^e; NaN for the mark of a block that is not finite.
+__device__ __forceinline__ float step_of(int e) {
+    return __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
+}
+
+__device__ __forceinline__ void kept_values(float (&x)[kG], u32x2 q, float step) {
+    const unsigned w[2] = {q.x, q.y};
+#pragma unroll
+    for (int i = 0; i < kG; ++i) x[i] = static_cast<float>(static_cast<signed char>(w[i / 4] >> (8 * (i % 4)))) * step;
+}
+
+template <int ACT>
+__device__ __forceinline__ float slope(float x) {
+    if constexpr (ACT == ADASUM_ACT_RELU) {
+        return x != x ? x : x > 0.f ? 1.f : 0.f;
+    } else if constexpr (ACT == ADASUM_ACT_GELU) {
+        return 0.5f * erfcf(x * -0.70710678118654752f) + x * expf(-0.5f * x * x) * 0.39894228040143268f;
+    } else if constexpr (ACT == ADASUM_ACT_GELU_TANH) {
+        // beyond 30 the slope is 0 or 1 to the last bit, and the cube may overflow
+        const float y = x > 30.f ? 30.f : x < -30.f ? -30.f : x;
+        const float z = 1.5957691216057308f * (y + 0.044715f * y * y * y);
+        const float h = 1.f / (1.f + expf(-z)), other = 1.f / (1.f + expf(z));
+        return h + y * h * other * 1.5957691216057308f * (1.f + 3 * 0.044715f * y * y);
+    } else {
+        const float h = 1.f / (1.f + expf(-x)), other = 1.f / (1.f + expf(x));
+        return h + x * h * other;
+    }
+}
+
+// The rows of a workgroup: f(row, channel) for every eight channels up to the pitch, ITEMS of them in flight.
+struct RowWork {
+    long long rows;
+    int tokens;          // rows of a workgroup
+    Divider granules;    // of a row
+};
+
+template <typename T, int ITEMS>
+__global__ void __launch_bounds__(kThreadsRow)
+store_kernel(const T* __restrict__ x, long long stride, int width, long long pitch, signed char* __restrict__ q, signed char* __restrict__ e,
+             RowWork work) {
+    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
+         first += static_cast<long long>(gridDim.x) * work.tokens) {
+        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+        for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
+            float v[ITEMS][kG];
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    load_some<kG>(v[k], x + (first + t) * stride + at, width - static_cast<int>(at));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                // (n and the step are multiples of four: the lanes of a block are here together)
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    unsigned most = 0;
+#pragma unroll
+                    for (int i = 0; i < kG; ++i) most = max(most, __float_as_uint(v[k][i]) & 0x7fffffffu);
+                    most = quad_max(most);
+                    const bool bad = most >= 0x7f800000u;
+                    const int exponent = max(static_cast<int>(most >> 23) - 133, -120);
+                    const float scale = __uint_as_float(static_cast<unsigned>(127 - exponent) << 23);
+                    unsigned b[kG];
+#pragma unroll
+                    for (int i = 0; i < kG; ++i) {
+                        const float y = fminf(fmaxf(v[k][i] * scale, -127.f), 127.f);
+                        b[i] = __float_as_uint(y + 12582912.f) & 0xffu;
+                    }
+                    u32x2 packed;
+                    packed.x = bad ? 0u : b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
+                    packed.y = bad ? 0u : b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
+                    const long long row = first + t;
+                    *reinterpret_cast<u32x2*>(q + row * pitch + at) = packed;
+                    if ((g & 3) == 0) e[row * (pitch / kBlock) + at / kBlock] = static_cast<signed char>(bad ? -128 : exponent);
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int ITEMS>
+__global__ void __launch_bounds__(kThreadsRow)
+load_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, T* __restrict__ out,
+            long long stride, RowWork work) {
+    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
+         first += static_cast<long long>(gridDim.x) * work.tokens) {
+        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+        for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
+            u32x2 kept[ITEMS];
+            int exponent[ITEMS];
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    kept[k] = *reinterpret_cast<const u32x2*>(q + (first + t) * pitch + at);
+                    exponent[k] = e[(first + t) * (pitch / kBlock) + at / kBlock];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    float v[kG];
+                    kept_values(v, kept[k], step_of(exponent[k]));
+                    store_some<kG>(out + (first + t) * stride + at, v, width - static_cast<int>(at));
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int ACT, int ITEMS>
+__global__ void __launch_bounds__(kThreadsRow)
+act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, const T* dy,
+                long long dy_stride, T* dx, long long dx_stride, RowWork work) {
+    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
+         first += static_cast<long long>(gridDim.x) * work.tokens) {
+        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+        for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
+            u32x2 kept[ITEMS];
+            int exponent[ITEMS];
+            float d[ITEMS][kG];
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    kept[k] = *reinterpret_cast<const u32x2*>(q + (first + t) * pitch + at);
+                    exponent[k] = e[(first + t) * (pitch / kBlock) + at / kBlock];
+                    load_some<kG>(d[k], dy + (first + t) * dy_stride + at, width - static_cast<int>(at));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    float v[kG];
+                    kept_values(v, kept[k], step_of(exponent[k]));
+#pragma unroll
+                    for (int i = 0; i < kG; ++i) v[i] = d[k][i] * slope<ACT>(v[i]);
+                    store_some<kG>(dx + (first + t) * dx_stride + at, v, width - static_cast<int>(at));
+                }
+            }
+        }
+    }
+}
+
+struct RowGrid {
+    RowWork work;
+    int64_t groups;
+    bool large;
+};
+RowGrid row_grid(int64_t rows, int64_t pitch) {
+    RowGrid r;
+    const int64_t granules = pitch / kG;
+    r.large = rows * granules > (1 << 18);
+    const int64_t per_group = r.large ? 4 * kThreadsRow : kThreadsRow;
+    const int64_t tokens = granules >= per_group ? 1 : per_group / granules;
+    r.work.rows = rows;
+    r.work.tokens = static_cast<int>(tokens);
+    r.work.granules = make_divider(static_cast<unsigned>(granules));
+    r.groups = at_most_groups((rows + tokens - 1) / tokens);
+    return r;
+}
+
+}  // namespace
+
+int launch_store(const void* x, int dtype, int64_t x_stride, const Kept& to, void* stream) {
+    const RowGrid g = row_grid(to.rows, to.pitch);
+    return with_type(dtype, [&](auto t) -> int {
+        typedef decltype(t) T;
+        const auto kernel = g.large ? store_kernel<T, 4> : store_kernel<T, 1>;
+        return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x), x_stride, to.width, to.pitch,
+            reinterpret_cast<signed char*>(const_cast<int8_t*>(to.q)), reinterpret_cast<signed char*>(const_cast<int8_t*>(to.e)), g.work);
+    });
+}
+
+int launch_load(const Kept& k, void* out, int dtype, int64_t out_stride, void* stream) {
+    const RowGrid g = row_grid(k.rows, k.pitch);
+    return with_type(dtype, [&](auto t) -> int {
+        typedef decltype(t) T;
+        const auto kernel = g.large ? load_kernel<T, 4> : load_kernel<T, 1>;
+        return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+            static_cast<T*>(out), out_stride, g.work);
+    });
+}
+
+int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t dy_stride, void* dx, int64_t dx_stride, void* stream) {
+    const RowGrid g = row_grid(k.rows, k.pitch);
+    return with_type(dtype, [&](auto t) -> int {
+        typedef decltype(t) T;
+        auto go = [&](auto small, auto large) -> int {
+            const auto kernel = g.large ? large : small;
+            return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+                static_cast<const T*>(dy), dy_stride, static_cast<T*>(dx), dx_stride, g.work);
+        };
+        switch (act) {
+            case ADASUM_ACT_RELU: return go(act_grad_kernel<T, ADASUM_ACT_RELU, 1>, act_grad_kernel<T, ADASUM_ACT_RELU, 4>);
+            case ADASUM_ACT_GELU: return go(act_grad_kernel<T, ADASUM_ACT_GELU, 1>, act_grad_kernel<T, ADASUM_ACT_GELU, 4>);
+            case ADASUM_ACT_GELU_TANH: return go(act_grad_kernel<T, ADASUM_ACT_GELU_TANH, 1>, act_grad_kernel<T, ADASUM_ACT_GELU_TANH, 4>);
+            default: return go(act_grad_kernel<T, ADASUM_ACT_SILU, 1>, act_grad_kernel<T, ADASUM_ACT_SILU, 4>);
+        }
+    });
+}
+
+}  // namespace adasum

@@ -1,0 +1,398 @@
+// gfx950 kernels of embedding tables that lie in a worker's flat buffer: rows looked up, and the table's gradient by sorted tokens.
+#include <hip/hip_runtime.h>
+
+#include "adasum_layers.h"
+#include "adasum_rows.h"
+
+namespace adasum {
+namespace {
+
+__device__ __forceinline__ long long id_at(const Ids& ids, int64_t t) {
+    return ids.wide ? static_cast<const int64_t*>(ids.p)[t] : static_cast<long long>(static_cast<const int32_t*>(ids.p)[t]);
+}
+
+// ---- rows of the table -----------------------------------------------------------
+//
+// out[t] = scale * table[ids[t]]: every byte moves once, nothing is computed to speak of.  A workgroup takes consecutive tokens, a
+// lane G elements of a row at a time (16 bytes of the narrower type).
+template <typename T, typename U, int ITEMS>
+__global__ void __launch_bounds__(256)
+lookup_kernel(const T* __restrict__ table, long long rows, int width, Ids ids, typename Traits<T>::acc_t scale, U* __restrict__ out,
+              long long out_stride, int tokens, Divider granules) {
+    typedef typename Traits<T>::acc_t A;
+    constexpr int G = 16 / (sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U));
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * tokens; first < ids.n; first += static_cast<int64_t>(gridDim.x) * tokens) {
+    const int here = static_cast<int>(min(static_cast<int64_t>(tokens), ids.n - first));
+    const unsigned work = static_cast<unsigned>(here) * granules.d;
+    for (unsigned base = threadIdx.x; base < work; base += 256 * ITEMS) {
+        A v[ITEMS][G];
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const unsigned g = base + 256 * k;
+            if (g < work) {
+                const unsigned t = divide(g, granules), at = (g - t * granules.d) * G;
+                const long long id = id_at(ids, first + t);
+                if (id >= 0 && id < rows) {
+                    load_some<G>(v[k], table + id * width + at, width - static_cast<int>(at));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) v[k][i] = A(0);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ITEMS; ++k) {
+            const unsigned g = base + 256 * k;
+            if (g < work) {
+                const unsigned t = divide(g, granules), at = (g - t * granules.d) * G;
+#pragma unroll
+                for (int i = 0; i < G; ++i) v[k][i] *= scale;
+                store_some<G>(out + (first + t) * out_stride + at, v[k], width - static_cast<int>(at));
+            }
+        }
+    }
+    }
+}
+
+// ---- sorting the tokens -----------------------------------------------------------
+//
+// Workgroup j lists the tokens whose id lies in its range of rows, in the order of their ids and, for one id, of the tokens.  It
+// reads all ids twice (they stay in L2): once to count how many lie below its range, which is where its list starts, and how many
+// tokens of a sixteenth of the input every row has; then, with the places that follow from those counts, to write.  No workgroup
+// waits for another.  Workgroups behind the last one clear the table meanwhile.
+constexpr int kSortThreads = 1024;
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kClearBytes = 64 * kSortThreads;   // per workgroup
+
+__global__ void __launch_bounds__(kSortThreads)
+sort_kernel(Ids ids, int rows, int per_group, int groups, int* __restrict__ total, int* __restrict__ place, int* __restrict__ row,
+            char* __restrict__ clear, long long clear_bytes) {
+    extern __shared__ int counts[];   // [wave][row of the range], then what the scan needs
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (static_cast<int>(blockIdx.x) >= groups) {
+        const unsigned zero[4] = {0, 0, 0, 0};
+        for (long long from = static_cast<long long>(blockIdx.x - groups) * kClearBytes; from < clear_bytes;
+             from += static_cast<long long>(gridDim.x - groups) * kClearBytes) {
+#pragma unroll
+            for (int k = 0; k < kClearBytes / 16 / kSortThreads; ++k) {
+                const long long at = from + 16ll * (k * kSortThreads + static_cast<int>(threadIdx.x));
+                if (at + 16 <= clear_bytes) {
+                    store_words_any(clear + at, zero);
+                } else {
+                    for (long long b = at; b < clear_bytes; b += 2) *reinterpret_cast<unsigned short*>(clear + b) = 0;
+                }
+            }
+        }
+        return;
+    }
+    const long long lo = static_cast<long long>(blockIdx.x) * per_group, hi = min(lo + per_group, static_cast<long long>(rows));
+    const int mine = static_cast<int>(hi - lo);
+    int* const scan = counts + kSortWaves * per_group;
+    for (int i = threadIdx.x; i < kSortWaves * per_group; i += kSortThreads) counts[i] = 0;
+    __syncthreads();
+    const int64_t segment = ((ids.n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+    const int64_t begin = min(segment * wave, ids.n), end = min(begin + segment, ids.n);
+    // (volatile: the lanes of a wave read what one of them has written)
+    volatile int* const my_counts = counts + wave * per_group;
+    int below = 0;
+#pragma unroll 4
+    for (int64_t t = begin + lane; t < end; t += 64) {
+        const long long id = id_at(ids, t);
+        below += id >= 0 && id < lo;
+        if (id >= lo && id < hi) atomicAdd(counts + wave * per_group + static_cast<int>(id - lo), 1);
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m, 64);
+    if (lane == 0) scan[wave] = below;
+    __syncthreads();
+    int base = 0;
+    for (int w = 0; w < kSortWaves; ++w) base += scan[w];
+    // one row of the range per thread (per_group is at most kSortThreads): its tokens, and those of the rows before it
+    const int r = threadIdx.x;
+    int sum = 0;
+    if (r < mine)
+        for (int w = 0; w < kSortWaves; ++w) sum += counts[w * per_group + r];
+    int upto = sum;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int before = __shfl_up(upto, m, 64);
+        if (lane >= m) upto += before;
+    }
+    __syncthreads();
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    int at = base + upto - sum;
+    for (int w = 0; w < wave; ++w) at += scan[w];
+    if (r < mine)
+        for (int w = 0; w < kSortWaves; ++w) {
+            const int n = counts[w * per_group + r];
+            counts[w * per_group + r] = at;
+            at += n;
+        }
+    if (blockIdx.x == static_cast<unsigned>(groups) - 1 && r == mine - 1) *total = at;
+    __syncthreads();
+    for (int64_t t0 = begin; t0 < end; t0 += 64) {
+        const int64_t t = t0 + lane;
+        const long long id = t < end ? id_at(ids, t) : -1;
+        const int bin = id >= lo && id < hi ? static_cast<int>(id - lo) : -1;
+        unsigned long long left = __ballot(bin >= 0);
+        while (left != 0) {
+            const int leader = __ffsll(left) - 1;
+            const int b = __shfl(bin, leader, 64);
+            const unsigned long long same = __ballot(bin == b);
+            if (bin == b) {
+                const int p = my_counts[b] + __popcll(same & ((1ull << lane) - 1));
+                place[p] = static_cast<int>(t);
+                row[p] = static_cast<int>(id);
+            }
+            // (a wave's LDS operations are done in order: the reads above come before this write)
+            if (lane == leader) my_counts[b] = my_counts[b] + __popcll(same);
+            left &= ~same;
+        }
+    }
+}
+
+// ---- sums over runs of equal ids ----------------------------------------------------
+
+// A wave's look at a chunk of sorted tokens: index i stands for place i - kRun of the chunk, 0 <= i < 3 kRun.
+struct Window {
+    int row0, row1;               // of index lane, and of index 64 + lane (lanes below kRun)
+    unsigned long long start;     // bit i: a run starts at index i (i < 64)
+    unsigned later;               // the same for index 64 + i
+    __device__ __forceinline__ int row_at(int i) const {
+        return i < 64 ? __builtin_amdgcn_readlane(row0, i) : __builtin_amdgcn_readlane(row1, i - 64);
+    }
+};
+__device__ __forceinline__ Window look(const int* row, int total, int64_t chunk, int lane) {
+    Window w;
+    const int64_t p0 = chunk * kRun - kRun + lane, p1 = p0 + 64;
+    w.row0 = p0 >= 0 && p0 < total ? row[p0] : p0 < 0 ? -1 : -2;
+    w.row1 = lane < kRun && p1 < total ? row[p1] : -2;
+    const int left = __shfl_up(w.row0, 1, 64), last = __shfl(w.row0, 63, 64);
+    w.start = __ballot(lane > 0 && w.row0 != left);
+    const int left1 = __shfl_up(w.row1, 1, 64);
+    w.later = static_cast<unsigned>(__ballot(lane < kRun && w.row1 != (lane == 0 ? last : left1)));
+    return w;
+}
+// Whether the run that starts at index a (a < 64) has more than kRun tokens.
+__device__ __forceinline__ bool is_long(const Window& w, int a) { return w.row_at(a + kRun) == w.row_at(a); }
+
+// One wave: chunk `chunk`, the elements of `slice`.
+template <typename D, typename T>
+__device__ __forceinline__ void
+sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long long dy_stride, int width, int total,
+          const int* __restrict__ place, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, int accumulate,
+          typename Traits<D>::acc_t* __restrict__ parts) {
+    typedef typename Traits<D>::acc_t A;
+    constexpr int G = Traits<D>::VEC;
+    static_assert(kRun == 32, "the window of a chunk is 96 places");
+    const Window w = look(row, total, chunk, lane);
+    const int there = static_cast<int>(min(static_cast<long long>(kRun), total - chunk * kRun));
+    // the tokens of indices kRun .. kRun + 63
+    const int64_t pp = chunk * kRun + lane;
+    const int token = pp < total ? place[pp] : 0;
+    int from = kRun, until = kRun + there;
+    // runs that start here (behind the last token is no run)
+    const unsigned starts = static_cast<unsigned>(w.start >> kRun) & (there == kRun ? ~0u : (1u << there) - 1);
+    bool carried = false;   // the first run is a long one that comes from the chunk before
+    if (!(starts & 1)) {
+        const unsigned before = static_cast<unsigned>(w.start);
+        const int a = before != 0 ? 31 - __builtin_clz(before) : -1;
+        carried = a < 0 || is_long(w, a);
+        if (!carried) {
+            if (starts == 0) return;   // all of the chunk belongs to a run that the wave before has
+            from = kRun + __builtin_ctz(starts);
+        }
+    }
+    // the last run that starts here: whole if it is not long, else as far as the chunk goes
+    bool open = false;
+    if (starts != 0) {
+        open = is_long(w, kRun + 31 - __builtin_clz(starts));
+        // (not long: the next run, or the end of the tokens, is in the window)
+        if (!open && there == kRun) until = 64 + __builtin_ctz(w.later | 0x80000000u);
+    }
+    const int at = (slice * 64 + lane) * G;
+    const int have = width - at;
+    A sum[G];
+#pragma unroll
+    for (int i = 0; i < G; ++i) sum[i] = A(0);
+    bool first_run = carried;
+    for (int i0 = from; i0 < until; i0 += 8) {
+        A v[8][G];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (i0 + k < until && have > 0) {
+                const int t = __builtin_amdgcn_readlane(token, i0 + k - kRun);
+                load_some<G>(v[k], dy + static_cast<long long>(t) * dy_stride + at, have);
+            }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = i0 + k;
+            if (i < until && have > 0) {
+#pragma unroll
+                for (int j = 0; j < G; ++j) sum[j] += v[k][j];
+                const bool ends = i + 1 == until || (i + 1 < 64 ? (w.start >> (i + 1)) & 1 : (w.later >> (i + 1 - 64)) & 1);
+                if (ends) {
+                    const bool goes_on = open && i + 1 == until;
+                    if (first_run || goes_on) {
+                        // (the one that comes from before and goes on lies in the first place)
+                        store_some<G>(parts + (2 * chunk + (first_run ? 0 : 1)) * width + at, sum, have);
+                    } else {
+                        T* const to = grad + static_cast<long long>(w.row_at(i)) * width + at;
+#pragma unroll
+                        for (int j = 0; j < G; ++j) sum[j] *= scale;
+                        if (accumulate) {
+                            A old[G];
+                            load_some<G>(old, to, have);
+#pragma unroll
+                            for (int j = 0; j < G; ++j) sum[j] += old[j];
+                        }
+                        store_some<G>(to, sum, have);
+                    }
+#pragma unroll
+                    for (int j = 0; j < G; ++j) sum[j] = A(0);
+                    first_run = false;
+                }
+            }
+        }
+    }
+}
+
+template <typename D, typename T>
+__global__ void __launch_bounds__(256)
+sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, const int* __restrict__ total_p, const int* __restrict__ place,
+           const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, int accumulate,
+           typename Traits<D>::acc_t* __restrict__ parts, int slices, long long n_chunks) {
+    const int lane = threadIdx.x & 63;
+    const int total = *total_p;
+    const long long units = min(n_chunks, (static_cast<long long>(total) + kRun - 1) / kRun) * slices;
+    for (long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += 4ll * gridDim.x)
+        sum_chunk<D, T>(unit / slices, static_cast<int>(unit % slices), lane, dy, dy_stride, width, total, place, row, scale, grad,
+                        accumulate, parts);
+}
+// The parts of long runs, four waves of a workgroup taking a quarter of a run's chunks each.
+template <typename D, typename T>
+__global__ void __launch_bounds__(256)
+join_kernel(int width, const int* __restrict__ total_p, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
+            int accumulate, const typename Traits<D>::acc_t* __restrict__ parts, int slices) {
+    typedef typename Traits<D>::acc_t A;
+    constexpr int G = Traits<D>::VEC;
+    __shared__ double half[4][64 * G];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int total = *total_p;
+    const long long units = static_cast<long long>(total) / kRun * slices;   // (a long run starts in a chunk that is full)
+    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const long long chunk = unit / slices;
+    const int slice = static_cast<int>(unit - chunk * slices);
+    const Window w = look(row, total, chunk, lane);
+    const unsigned starts = static_cast<unsigned>(w.start >> 32);
+    if (starts == 0) continue;
+    const int a = kRun + 31 - __builtin_clz(starts);
+    if (!is_long(w, a)) continue;
+    const int key = w.row_at(a);
+    // the last chunk that begins with this row, 64 chunks a look
+    long long last = chunk + 1;
+    for (;;) {
+        const long long c = last + 1 + lane;
+        const unsigned long long same = __ballot(c * kRun < total && row[c * kRun < total ? c * kRun : 0] == key);
+        const int run = same == ~0ull ? 64 : __ffsll(~same) - 1;
+        last += run;
+        if (run < 64) break;
+    }
+    const int at = (slice * 64 + lane) * G, have = width - at;
+    const long long n = last - chunk + 1;
+    double sum[G];
+#pragma unroll
+    for (int j = 0; j < G; ++j) sum[j] = 0;
+    if (have > 0) {
+#pragma unroll 4
+        for (long long c = n * wave / 4; c < n * (wave + 1) / 4; ++c) {
+            A v[G];
+            load_some<G>(v, parts + (2 * (chunk + c) + (c == 0 ? 1 : 0)) * width + at, have);
+#pragma unroll
+            for (int j = 0; j < G; ++j) sum[j] += v[j];
+        }
+    }
+    __syncthreads();   // (all have read what the last round left there)
+#pragma unroll
+    for (int j = 0; j < G; ++j) half[wave][j * 64 + lane] = sum[j];
+    __syncthreads();
+    if (wave != 0 || have <= 0) continue;
+    T* const to = grad + static_cast<long long>(key) * width + at;
+    A v[G], old[G];
+    if (accumulate) load_some<G>(old, to, have);
+#pragma unroll
+    for (int j = 0; j < G; ++j) {
+        double s = sum[j] + half[1][j * 64 + lane];
+        s += half[2][j * 64 + lane];
+        s += half[3][j * 64 + lane];
+        s *= scale;
+        v[j] = static_cast<A>(accumulate ? s + old[j] : s);
+    }
+    store_some<G>(to, v, have);
+    }
+}
+
+int slices_of(int64_t width, int dtype) {
+    const int per = 64 * 16 / elem_bytes(dtype);
+    return static_cast<int>((width + per - 1) / per);
+}
+
+}  // namespace
+
+EmbeddingLayout embedding_layout(int64_t width, int64_t n_ids, int dtype) {
+    EmbeddingLayout l;
+    l.chunks = (n_ids + kRun - 1) / kRun;
+    l.off_place = 256;
+    l.off_row = align_up(l.off_place + 4 * static_cast<size_t>(n_ids), 256);
+    l.off_parts = align_up(l.off_row + 4 * static_cast<size_t>(n_ids), 256);
+    l.total = l.off_parts + static_cast<size_t>(l.chunks) * 2 * width * (dtype == ADASUM_F64 ? 8 : 4);
+    return l;
+}
+
+int launch_lookup(int dtype, int out_dtype, const void* table, int64_t rows, int64_t width, const Ids& ids, double scale, void* out,
+                  int64_t out_stride, void* stream) {
+    return with_types(dtype, out_dtype, [&](auto t, auto u) -> int {
+        typedef decltype(t) T;
+        typedef decltype(u) U;
+        constexpr int G = 16 / (sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U));
+        const int64_t granules = (width + G - 1) / G;
+        const bool large = ids.n * granules > (1 << 18);
+        const int64_t per_block = large ? 1024 : 256;
+        const int64_t tokens = granules >= per_block ? 1 : per_block / granules;
+        const int64_t blocks = (ids.n + tokens - 1) / tokens;
+        const auto kernel = large ? lookup_kernel<T, U, 4> : lookup_kernel<T, U, 1>;
+        return launch(kernel, at_most_groups(blocks), 1, 256, 0, stream, static_cast<const T*>(table), rows, width, ids, scale,
+                      static_cast<U*>(out), out_stride, tokens, make_divider(static_cast<unsigned>(granules)));
+    });
+}
+
+int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
+    const int64_t clear_bytes = g.accumulate ? 0 : g.rows * g.width * elem_bytes(g.grad_dtype);
+    int* const total = reinterpret_cast<int*>(g.ws + g.lay.off_total);
+    int* const place = reinterpret_cast<int*>(g.ws + g.lay.off_place);
+    int* const row = reinterpret_cast<int*>(g.ws + g.lay.off_row);
+    const int64_t per_group = sort_rows(g.rows);
+    const int64_t groups = g.ids.n == 0 ? 0 : (g.rows + per_group - 1) / per_group;
+    const int64_t clearing = at_most_groups((clear_bytes + kClearBytes - 1) / kClearBytes);
+    if (groups + clearing == 0) return 0;
+    const size_t lds = sizeof(int) * (static_cast<size_t>(kSortWaves) * per_group + kSortWaves);
+    const int rc = launch(sort_kernel, groups + clearing, 1, kSortThreads, lds, stream, g.ids, g.rows, per_group, groups, total, place, row,
+                          static_cast<char*>(g.grad), clear_bytes);
+    if (rc != 0 || g.ids.n == 0) return rc;
+    return with_types(g.dtype, g.grad_dtype, [&](auto d, auto t) -> int {
+        typedef decltype(d) D;
+        typedef decltype(t) T;
+        typedef typename Traits<D>::acc_t A;
+        const int slices = slices_of(g.width, g.dtype);
+        const int64_t units = g.lay.chunks * slices;
+        A* const parts = reinterpret_cast<A*>(g.ws + g.lay.off_parts);
+        const int rc2 = launch(sum_kernel<D, T>, at_most_groups((units + 3) / 4), 1, 256, 0, stream, static_cast<const D*>(g.dy), g.dy_stride,
+                               g.width, total, place, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, slices, g.lay.chunks);
+        if (rc2 != 0) return rc2;
+        return launch(join_kernel<D, T>, at_most_groups(units), 1, 256, 0, stream, g.width, total, row, g.scale, static_cast<T*>(g.grad),
+                      g.accumulate, parts, slices);
+    });
+}
+
+}  // namespace adasum

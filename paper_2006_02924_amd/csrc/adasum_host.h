@@ -74,6 +74,9 @@ inline bool dtype_pair_ok(int in, int out) {
 inline bool is_pow2(long long v) { return v > 0 && (v & (v - 1)) == 0; }
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// What a failing HIP call or launch leaves for adasum_last_hip_error, and the code to return (adasum_api.cpp).
+int hip_failure(int hip_error);
+
 // ---- planning (pure host code) ----------------------------------------------
 
 // Validates a layer table; returns ADASUM_OK or an error code.

@@ -1,0 +1,151 @@
+// Device code shared by the operators on rows: 16-byte accesses at any element's alignment, values in fp32 or fp64.
+#pragma once
+
+#include <tuple>
+
+#include "adasum_device.h"
+
+namespace adasum {
+namespace {
+
+// Launches a kernel and says how that went, whatever error an earlier call of this thread left behind.
+template <typename... P, typename... A>
+int launch(void (*kernel)(P...), int64_t groups, int64_t parts, int threads, size_t lds, void* stream, const A&... args) {
+    std::tuple<P...> values(static_cast<P>(args)...);
+    return std::apply(
+        [&](P&... v) {
+            void* pointers[] = {const_cast<void*>(reinterpret_cast<const void*>(&v))...};
+            return static_cast<int>(hipLaunchKernel(reinterpret_cast<const void*>(kernel),
+                                                    dim3(static_cast<unsigned>(groups), static_cast<unsigned>(parts)), dim3(threads), pointers,
+                                                    lds, static_cast<hipStream_t>(stream)));
+        },
+        values);
+}
+// Workgroups of a launch at most: the kernels go round.
+constexpr int64_t kMostGroups = 1 << 20;
+inline int64_t at_most_groups(int64_t groups) { return groups < kMostGroups ? groups : kMostGroups; }
+
+// A row may start anywhere (a layer of a flat buffer, a slice of a wider matrix): the memory system takes 16-byte accesses at
+// every element's alignment, the type only has to say so.
+typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+
+template <typename T, int G>
+__device__ __forceinline__ void load_any(Granule<T, G>& r, const T* p) {
+    constexpr int NW = Granule<T, G>::NW;
+    if constexpr (NW == 2) {
+        const u32x2_any q = *reinterpret_cast<const u32x2_any*>(p);
+        r.w[0] = q.x;
+        r.w[1] = q.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < NW / 4; ++i) {
+            const u32x4_any q = *(reinterpret_cast<const u32x4_any*>(p) + i);
+            r.w[4 * i + 0] = q.x;
+            r.w[4 * i + 1] = q.y;
+            r.w[4 * i + 2] = q.z;
+            r.w[4 * i + 3] = q.w;
+        }
+    }
+}
+
+template <int NW>
+__device__ __forceinline__ void store_words_any(void* p, const unsigned int (&w)[NW]) {
+    if constexpr (NW == 2) {
+        u32x2_any q;
+        q.x = w[0];
+        q.y = w[1];
+        *reinterpret_cast<u32x2_any*>(p) = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < NW / 4; ++i) {
+            u32x4_any q;
+            q.x = w[4 * i + 0];
+            q.y = w[4 * i + 1];
+            q.z = w[4 * i + 2];
+            q.w = w[4 * i + 3];
+            *(reinterpret_cast<u32x4_any*>(p) + i) = q;
+        }
+    }
+}
+
+__device__ __forceinline__ unsigned int bits_of(bf16_t, float v) { return f32_to_bf16_rne(v); }
+__device__ __forceinline__ unsigned int bits_of(f16_t, float v) { return f32_to_f16_bits(v); }
+
+// G values to consecutive elements of T.
+template <int G, typename T, typename A>
+__device__ __forceinline__ void store_any(T* p, const A (&v)[G]) {
+    unsigned int w[Granule<T, G>::NW];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < G / 2; ++i) w[i] = bits_of(T{}, v[2 * i]) | (bits_of(T{}, v[2 * i + 1]) << 16);
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < G; ++i) w[i] = __float_as_uint(v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const long long b = __double_as_longlong(v[i]);
+            w[2 * i] = static_cast<unsigned int>(b);
+            w[2 * i + 1] = static_cast<unsigned int>(b >> 32);
+        }
+    }
+    store_words_any(p, w);
+}
+
+// `there` (1 .. G) elements of T as values, zeros behind them.
+template <int G, typename T, typename A>
+__device__ __forceinline__ void load_some(A (&v)[G], const T* p, int there) {
+    if (there >= G) {
+        Granule<T, G> r;
+        load_any(r, p);
+        unpack(r, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < G; ++i) v[i] = i < there ? load_elem(p + i) : A(0);
+    }
+}
+template <int G, typename T, typename A>
+__device__ __forceinline__ void store_some(T* p, const A (&v)[G], int there) {
+    if (there >= G) {
+        store_any<G>(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (i < there) store_elem(p + i, v[i]);
+    }
+}
+
+// Division of numbers below 2^31 by a fixed one, by a multiplication: q = (n * m) >> (32 + s) with
+// m = ceil(2^(32 + s) / d), 2^s >= d; the product is taken with a 33-bit m (its top bit is always set).
+struct Divider {
+    unsigned d, m, s;
+};
+inline Divider make_divider(unsigned d) {
+    Divider r{d, 0, 0};
+    while ((1ull << r.s) < d) ++r.s;
+    const unsigned long long top = (1ull << 32) * ((1ull << r.s) - d) / d + 1;
+    r.m = static_cast<unsigned>(top);
+    return r;
+}
+__device__ __forceinline__ unsigned divide(unsigned n, const Divider& v) {
+    return static_cast<unsigned>((static_cast<unsigned long long>(__umulhi(n, v.m)) + n) >> v.s);
+}
+
+// f(type of a, type of b) for storage types that go together.
+template <typename F>
+int with_type(int dtype, F&& f) {
+    switch (dtype) {
+        case ADASUM_F32: return f(float{});
+        case ADASUM_BF16: return f(bf16_t{});
+        default: return f(f16_t{});
+    }
+}
+template <typename F>
+int with_types(int a, int b, F&& f) {
+    if (a == ADASUM_F64) return f(double{}, double{});
+    return with_type(a, [&](auto ta) { return with_type(b, [&](auto tb) { return f(ta, tb); }); });
+}
+
+}  // namespace
+}  // namespace adasum

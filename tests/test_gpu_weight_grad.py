@@ -1,0 +1,196 @@
+"""Gradients of a linear layer's weight and bias from the checkpoint of its input, against their definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from layer_grads_util import DTYPES, f64, half_step, least, within
+from paper_2006_02924_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+KEPT = ["f32", "bf16", "f16"]
+
+
+def rand(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed))
+
+
+def check(got, want, mag, n, out, old=0.0):
+    # the products are exact; a matrix instruction adds sixteen of them to what it holds, with at most four roundings of at most a whole
+    # step of fp32 (three times as many instructions for fp32's three parts); a few more roundings where pieces are joined
+    tol = (3 * (n / 4 + 8) + 32) * 2.0 ** -23 * (mag + np.abs(old))
+    within(got, want + old, tol + half_step(out) * (np.abs(want + old) + tol) + least(out))
+
+
+def run(seed, n, outputs, width, dtype, out, lead, gap, bias=True, accumulate=False):
+    x = rand(seed, n, width) * torch.exp2(torch.randint(-6, 4, (n, 1), generator=torch.Generator().manual_seed(seed)).float())
+    kept = B.adasum_checkpoint_store(x.to(dtype).cuda())
+    dy = torch.full((n, outputs + gap), float("nan"), dtype=dtype)
+    dy[:, :outputs] = (rand(seed + 1, n, outputs) * 0.1).to(dtype)
+    dev = dy.cuda()[:, :outputs]
+    size = outputs * width
+    flat = (rand(seed + 2, lead + size + outputs + 7) if accumulate else torch.full((lead + size + outputs + 7,), 5.0)).to(out).cuda()
+    before = f64(flat)
+    B.adasum_checkpoint_weight_grad(kept, dev, flat, lead, bias_offset=lead + size if bias else None, accumulate=accumulate)
+    v, d = f64(B.adasum_checkpoint_load(kept)), f64(dev)
+    got = f64(flat)
+    end = lead + size + (outputs if bias else 0)
+    assert np.array_equal(got[:lead], before[:lead]) and np.array_equal(got[end:], before[end:])
+    old = before[lead:lead + size].reshape(outputs, width) if accumulate else np.zeros((outputs, width))
+    check(got[lead:lead + size].reshape(outputs, width), d.T @ v, np.abs(d).T @ np.abs(v), n, out, old)
+    if bias:
+        old = before[lead + size:end] if accumulate else np.zeros(outputs)
+        check(got[lead + size:end], d.sum(0), np.abs(d).sum(0), n, out, old)
+
+
+@pytest.mark.parametrize("dtype", KEPT)
+@pytest.mark.parametrize("out", KEPT)
+@pytest.mark.parametrize("n, outputs, width, lead, gap", [(1, 1, 1, 0, 0), (3, 5, 33, 1, 3), (32, 128, 128, 0, 0), (33, 129, 257, 8, 8),
+                                                          (64, 256, 256, 0, 0), (200, 100, 1000, 3, 0), (1000, 40, 24, 5, 1)])
+def test_every_pair_of_types(dtype, out, n, outputs, width, lead, gap):
+    run(n, n, outputs, width, DTYPES[dtype], DTYPES[out], lead, gap)
+
+
+@pytest.mark.parametrize("dtype, out", [("bf16", "bf16"), ("f32", "f32"), ("f16", "f32")])
+@pytest.mark.parametrize("n, outputs, width", [(64, 300, 300), (129, 512, 40), (4097, 130, 66), (2500, 257, 513), (8192, 64, 64), (777, 1024, 1024),
+                                               (1, 700, 600), (300, 2, 4096), (300, 4096, 2)])
+def test_pieces_and_edges(dtype, out, n, outputs, width):
+    run(n + 1, n, outputs, width, DTYPES[dtype], DTYPES[out], 0, 0, bias=n % 2 == 1)
+    run(n + 2, n, outputs, width, DTYPES[dtype], DTYPES[out], 9, 2, accumulate=True)
+
+
+def test_no_tokens():
+    flat = torch.ones(100, device="cuda")
+    kept = B.Checkpoint(0, 8, torch.float32, device="cuda")
+    dy = torch.empty(0, 10, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy, flat, 4, bias_offset=84, accumulate=True)
+    assert (flat == 1).all()
+    B.adasum_checkpoint_weight_grad(kept, dy, flat, 4, bias_offset=84)
+    assert (flat[4:94] == 0).all() and (flat[:4] == 1).all() and (flat[94:] == 1).all()
+
+
+@pytest.mark.parametrize("dtype", KEPT)
+def test_infinities_and_nan_stay_in_their_rows_and_columns(dtype):
+    dtype = DTYPES[dtype]
+    x, dy = rand(1, 300, 200).to(dtype), rand(2, 300, 150).to(dtype)
+    x[100, 70] = float("nan")               # channels 64 .. 95 of that token
+    x[100, 130] = float("inf")              # channels 128 .. 159
+    dy[7, 33] = float("inf")
+    dy[8, 34] = float("nan")
+    flat = torch.zeros(150 * 200 + 150, device="cuda")
+    kept = B.adasum_checkpoint_store(x.cuda())
+    B.adasum_checkpoint_weight_grad(kept, dy.cuda(), flat, 0, bias_offset=30000)
+    w, b = flat[:30000].view(150, 200).cpu(), flat[30000:].cpu()
+    v = B.adasum_checkpoint_load(kept).cpu().double()
+    bad = torch.zeros(150, 200, dtype=torch.bool)
+    bad[:, 64:96] = bad[:, 128:160] = True
+    bad[33] = bad[34] = True
+    assert not torch.isfinite(w[bad]).any() and torch.isfinite(w[~bad]).all()
+    want = dy.double()[7, 33] * v[7]        # an infinity with a finite number's sign, NaN with zero
+    cols = ~bad[0]
+    assert torch.equal(torch.nan_to_num(w[33, cols], nan=7.0), torch.nan_to_num(want[cols], nan=7.0).float().clamp(-3.4028234663852886e38, 3.4028234663852886e38))
+    assert torch.isinf(b[33]) and torch.isnan(b[34]) and torch.isfinite(b[:33]).all() and torch.isfinite(b[35:]).all()
+
+
+def test_a_broadcast_gradient():
+    """The gradient of a sum over tokens: one row, seen by every token (stride 0)."""
+    x = rand(3, 500, 100)
+    one = rand(4, 1, 70).cuda()
+    kept = B.adasum_checkpoint_store(x.cuda())
+    flat = torch.empty(70 * 100 + 70, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, one.expand(500, 70), flat, 0, bias_offset=7000)
+    v, d = f64(B.adasum_checkpoint_load(kept)), f64(one)
+    check(f64(flat[:7000]).reshape(70, 100), d.T @ v.sum(0)[None], np.abs(d).T @ np.abs(v).sum(0)[None], 500, torch.float32)
+    check(f64(flat[7000:]), 500 * d[0], 500 * np.abs(d[0]), 500, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_and_small_values(dtype):
+    """Products near the ends of fp32's range."""
+    for sx, sd in ((2.0 ** 90, 2.0 ** 20), (2.0 ** -60, 2.0 ** -40), (2.0 ** -100, 2.0 ** 100), (2.0 ** 100, 2.0 ** -100)):
+        x, dy = (rand(5, 100, 64) * sx).to(DTYPES[dtype]), (rand(6, 100, 64) * sd).to(DTYPES[dtype])
+        kept = B.adasum_checkpoint_store(x.cuda())
+        flat = torch.empty(64 * 64, device="cuda")
+        B.adasum_checkpoint_weight_grad(kept, dy.cuda(), flat, 0)
+        v, d = f64(B.adasum_checkpoint_load(kept)), f64(dy)
+        check(f64(flat).reshape(64, 64), d.T @ v, np.abs(d).T @ np.abs(v), 100, torch.float32)
+
+
+def test_small_fp16_values():
+    """fp16's smallest numbers count in the products."""
+    x, dy = (rand(7, 64, 64) * 2.0 ** -18).half(), (rand(8, 64, 64) * 2.0 ** -17).half()
+    kept = B.adasum_checkpoint_store(x.cuda())
+    flat = torch.empty(64 * 64, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy.cuda(), flat, 0)
+    v, d = f64(B.adasum_checkpoint_load(kept)), f64(dy)
+    check(f64(flat).reshape(64, 64), d.T @ v, np.abs(d).T @ np.abs(v), 64, torch.float32)
+
+
+def test_gradient_against_differences():
+    """The layer is linear in its weight: the difference quotient of the sum of dy * (W x + b) along a direction."""
+    x, dy = rand(9, 60, 50).cuda(), rand(10, 60, 40).cuda()
+    kept = B.adasum_checkpoint_store(x)
+    v = B.adasum_checkpoint_load(kept).double()
+    flat = torch.empty(40 * 50 + 40, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy, flat, 0, bias_offset=2000)
+    w, along = rand(11, 2040).double().cuda(), rand(12, 2040).double().cuda()
+
+    def loss(p):
+        return float(((v @ p[:2000].view(40, 50).t().contiguous() + p[2000:]) * dy.double()).sum())
+
+    h = 2.0 ** -8
+    slope = (loss(w + h * along) - loss(w - h * along)) / (2 * h)
+    # 60 x 40 terms of some 50 values; fp32 sums of 60 products, 2040 of them
+    assert abs(slope - float((flat.double() * along).sum())) < 2400 * 50 * 9 * 2.0 ** -50 / h + 2040 * 9 * 60 * 9 * 2.0 ** -23
+
+
+def test_the_same_every_time_captured_and_on_another_stream():
+    n, outputs, width = 3000, 200, 300
+    x, dy = rand(13, n, width).bfloat16().cuda(), rand(14, n, outputs).bfloat16().cuda()
+    kept = B.adasum_checkpoint_store(x)
+    size = outputs * width + outputs
+    eager, flat = torch.empty(size, device="cuda"), torch.empty(size, device="cuda")
+    work = torch.empty(B.adasum_checkpoint_weight_grad_workspace_bytes(n, width, outputs, dy.dtype), dtype=torch.uint8, device="cuda")
+
+    def go(to, **kw):
+        B.adasum_checkpoint_weight_grad(kept, dy, to, 0, bias_offset=outputs * width, **kw)
+
+    go(eager)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    go(flat, stream=side)
+    side.synchronize()
+    assert torch.equal(flat, eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go(flat, workspace=work)
+    for rep in range(3):
+        dy.copy_(rand(20 + rep, n, outputs))
+        work.fill_(255)
+        go(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(flat, eager), rep
+
+
+def test_rows_beyond_32_bits():
+    n, width, outputs = (1 << 20) + 5, 2080, 33
+    kept = B.Checkpoint(n, width, torch.bfloat16, device="cuda", data=None)
+    kept.data.zero_()
+    kept.data[(n - 1) * width:n * width] = 3
+    dy = torch.zeros(n, 2112, dtype=torch.bfloat16, device="cuda")[:, :outputs]
+    dy[n - 1] = 2.0
+    dy[0] = 1.0
+    flat = torch.empty(outputs * width + outputs, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy, flat, 0, bias_offset=outputs * width)
+    assert (flat[:outputs * width] == 6).all() and (flat[outputs * width:] == 3).all()
+
+
+def test_the_binding_refuses_wrong_shapes():
+    kept = B.adasum_checkpoint_store(torch.zeros(4, 40, device="cuda"))
+    dy, flat = torch.zeros(4, 16, device="cuda"), torch.zeros(656, device="cuda")
+    for bad in (lambda: B.adasum_checkpoint_weight_grad(kept, dy[:3], flat, 0), lambda: B.adasum_checkpoint_weight_grad(kept, dy, flat, 17),
+                lambda: B.adasum_checkpoint_weight_grad(kept, dy, flat, 0, bias_offset=641),
+                lambda: B.adasum_checkpoint_weight_grad(kept, dy.half(), flat, 0), lambda: B.adasum_checkpoint_weight_grad(kept, dy.t(), flat, 0),
+                lambda: B.adasum_checkpoint_weight_grad(kept, dy, flat.view(8, 82), 0)):
+        with pytest.raises(ValueError):
+            bad()
