@@ -92,11 +92,11 @@ int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t d
 
 // ---- weight gradients (adasum_weight_grad.hip) ----------------------------------
 
-// How the sum over the tokens is cut: `parts` pieces of `steps` steps of kStepTokens tokens.
-constexpr int kGradTile = 128;
-constexpr int kStepTokens = 32;
+// A workgroup computes a square of the weight, `tile` wide, over one of `parts` parts of the tokens, each `steps` steps of the kernel,
+// `tokens` in all.
 struct WeightSplit {
-    int64_t parts = 1, steps = 0;
+    int tile = 0;
+    int64_t parts = 1, steps = 0, tokens = 0;
     size_t off_bias = 0;      // fp32 [parts][outputs], behind fp32 [parts][outputs][width]
     size_t total = 0;
 };

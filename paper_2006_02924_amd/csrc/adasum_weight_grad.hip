@@ -23,104 +23,279 @@ __device__ __forceinline__ f32x16 mfma(f16_t, u32x4 a, u32x4 b, f32x16 c) {
 template <typename T> struct Products { typedef T type; static constexpr int planes = 1; };
 template <> struct Products<float> { typedef bf16_t type; static constexpr int planes = 3; };
 
-__device__ __forceinline__ void part_of(float x, unsigned (&p)[3]) {
-    const unsigned a = __float_as_uint(x);
-    p[0] = a >> 16;
-    if ((a & 0x7f800000u) == 0x7f800000u) {
-        if ((a & 0x7fffffu) != 0) p[0] |= 0x40u;
-        p[1] = p[2] = 0;
-        return;
-    }
-    const float r = x - __uint_as_float(a & 0xffff0000u);
+struct Parts3 {
+    unsigned p[3];
+};
+__device__ __forceinline__ Parts3 parts_of(unsigned a) {
+    const bool finite = (a & 0x7f800000u) != 0x7f800000u;
+    const float x = __uint_as_float(a);
+    const float r = finite ? x - __uint_as_float(a & 0xffff0000u) : 0.f;
     const unsigned b = __float_as_uint(r);
-    p[1] = b >> 16;
-    p[2] = __float_as_uint(r - __uint_as_float(b & 0xffff0000u)) >> 16;
+    Parts3 s;
+    s.p[0] = x != x ? 0x7fc0u : a >> 16;
+    s.p[1] = b >> 16;
+    s.p[2] = __float_as_uint(r - __uint_as_float(b & 0xffff0000u)) >> 16;
+    return s;
 }
 
-constexpr int kPad = 8;
-constexpr int kRowLds = kStepTokens + kPad;
+// Two values that their type holds exactly.
+__device__ __forceinline__ unsigned exact_pair(bf16_t, float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ unsigned exact_pair(f16_t, float a, float b) {
+    return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
 
-// A workgroup of four waves: 128 x 128 of dW over the steps of one part of the tokens, each wave a quarter.  Both operands are staged
-// with the tokens innermost, as the matrix cores want them.
-template <typename D, typename T>
-__global__ void __launch_bounds__(256)
-weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
-                   const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ grad, int accumulate,
-                   float* __restrict__ parts, long long steps, int tiles_i) {
-    typedef typename Products<D>::type E;
-    constexpr int P = Products<D>::planes;
-    __shared__ __align__(16) unsigned short as[P][kGradTile][kRowLds];
-    __shared__ __align__(16) unsigned short bs[kGradTile][kRowLds];
-    const int o0 = static_cast<int>(blockIdx.x / tiles_i) * kGradTile, i0 = static_cast<int>(blockIdx.x % tiles_i) * kGradTile;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wo = (wave >> 1) * 64, wi = (wave & 1) * 64;
-    const int st = threadIdx.x >> 3, sc = (threadIdx.x & 7) * 16;   // what this lane stages: a token, 16 channels
-    f32x16 acc[2][2] = {};
-    const long long t_begin = static_cast<long long>(blockIdx.y) * steps * kStepTokens;
-    const long long t_end = min(rows, t_begin + steps * kStepTokens);
-    for (long long t0 = t_begin; t0 < t_end; t0 += kStepTokens) {
-        const long long t = t0 + st;
-        __syncthreads();
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+
+// Workgroup `b` of n as the eight dies see it: consecutive workgroups go to dies in turn, and those of one die should share operands.
+__device__ __forceinline__ unsigned die_order(unsigned b, unsigned n) {
+    const unsigned die = b & 7, at = b >> 3, each = n >> 3, more = n & 7;
+    return die * each + (die < more ? die : more) + at;
+}
+
+// What a workgroup does, by the edge of its square of dW (TILE) and the storage type of dy.
+template <typename D, int TILE>
+struct GradShape {
+    static constexpr int planes = Products<D>::planes;
+    static constexpr int step = planes == 3 ? 32 : 64;          // tokens of a step
+    static constexpr int subs = step / 16;                      // matrix instructions' share of it
+    static constexpr int frags = TILE / 64;                     // 32 x 32 blocks of a wave along either edge
+    // LDS: [token][channel], rows TILE channels and 64 bytes apart, so that the transposing read's four rows of 32 bytes lie in
+    // different banks
+    static constexpr int pitch = 2 * TILE + 64;
+    static constexpr int plane_bytes = step * pitch;
+    static constexpr int buffer_bytes = (planes + 1) * plane_bytes;
+    // 256 lanes stage eight channels of dy, and sixteen of x, of a token at a time
+    static constexpr int a_rows = 256 / (TILE / 8), b_rows = 256 / (TILE / 16);
+    static constexpr int a_passes = step / a_rows, b_passes = step / b_rows;
+    static constexpr int lds_bytes = 2 * buffer_bytes;
+};
+
+// Eight elements of dy, and sixteen of x, to LDS (zeros where there is no such token).
+template <typename D>
+__device__ __forceinline__ void to_lds(char* at, int plane_bytes, const Granule<D, 8>& g, bool there) {
+    if constexpr (sizeof(D) == 2) {
+        u32x4 w;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float v[8];
-            const int o = o0 + sc + 8 * h;
-            load_some<8>(v, dy + t * dy_stride + o, t < t_end ? outputs - o : 0);
+        for (int i = 0; i < 4; ++i) w[i] = there ? g.w[i] : 0u;
+        *reinterpret_cast<u32x4*>(at) = w;
+    } else {
+        Parts3 s[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if constexpr (P == 3) {
-                    unsigned p[3];
-                    part_of(v[j], p);
+        for (int i = 0; i < 8; ++i) s[i] = parts_of(there ? g.w[i] : 0u);
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) as[k][sc + 8 * h + j][st] = static_cast<unsigned short>(p[k]);
-                } else {
-                    as[0][sc + 8 * h + j][st] = static_cast<unsigned short>(bits_of(E{}, v[j]));
-                }
-            }
-        }
-        const int i = i0 + sc;
-        u32x4 kept = {0, 0, 0, 0};
-        float step = 0.f;
-        if (t < t_end && i < pitch) {
-            kept = *reinterpret_cast<const u32x4*>(q + t * pitch + i);
-            const int ex = e[t * (pitch / kBlock) + i / kBlock];
-            step = __uint_as_float(ex == -128 ? 0x7fc00000u : static_cast<unsigned>(ex + 127) << 23);
-        }
+        for (int k = 0; k < 3; ++k) {
+            u32x4 w;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float x = static_cast<float>(static_cast<signed char>(kept[j / 4] >> (8 * (j % 4)))) * step;
-            bs[sc + j][st] = static_cast<unsigned short>(bits_of(E{}, x));
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k0 = 0; k0 < kStepTokens; k0 += 16) {
-            u32x4 b[2];
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-                b[n] = *reinterpret_cast<const u32x4*>(&bs[wi + 32 * n + (lane & 31)][k0 + 8 * (lane >> 5)]);
-#pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const u32x4 a = *reinterpret_cast<const u32x4*>(&as[p][wo + 32 * m + (lane & 31)][k0 + 8 * (lane >> 5)]);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) acc[m][n] = mfma(E{}, a, b[n], acc[m][n]);
-                }
+            for (int i = 0; i < 4; ++i) w[i] = s[2 * i].p[k] | s[2 * i + 1].p[k] << 16;
+            *reinterpret_cast<u32x4*>(at + k * plane_bytes) = w;
         }
     }
+}
+template <typename E>
+__device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) {
+    const float step = !there ? 0.f : __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int h = 0; h < 2; ++h) {
+        u32x4 w;
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int i = 0; i < 4; ++i) {
+            const unsigned word = q[2 * h + i / 2] >> (16 * (i & 1));
+            const float a = static_cast<float>(static_cast<signed char>(word)) * step;
+            const float b = static_cast<float>(static_cast<signed char>(word >> 8)) * step;
+            w[i] = exact_pair(E{}, a, b);
+        }
+        *reinterpret_cast<u32x4*>(at + 16 * h) = w;
+    }
+}
+
+// A workgroup of four waves: TILE x TILE of dW over one part of the tokens, each wave a quarter.
+//
+// Both operands lie with the tokens in rows, and the matrix cores want eight tokens of a channel in a lane: a step of both is staged in
+// LDS as it lies in memory (x as the values it stands for), and read with the transposing LDS read.  While a step is multiplied out of
+// one buffer, the next one, which is in registers by then, is written into the other and the loads of the one after are issued, a
+// part of them beside every sixteen tokens' products.  One barrier a step.
+template <typename D, typename T, int TILE>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE == 256 ? 1 : 2)))
+weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
+                   const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ grad, int accumulate,
+                   float* __restrict__ parts, long long steps, unsigned tiles_o, unsigned tiles_i) {
+    typedef typename Products<D>::type E;
+    typedef GradShape<D, TILE> S;
+    constexpr int P = S::planes, F = S::frags;
+    extern __shared__ __align__(16) char lds[];
+    const unsigned n = die_order(blockIdx.x, gridDim.x), tile = n % (tiles_o * tiles_i), part = n / (tiles_o * tiles_i);
+    const int o0 = static_cast<int>(tile / tiles_i) * TILE, i0 = static_cast<int>(tile % tiles_i) * TILE;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wo = (wave >> 1) * (TILE / 2), wi = (wave & 1) * (TILE / 2);
+    const long long t_begin = part * steps * S::step, t_end = min(rows, t_begin + steps * S::step);
+    const int whole = static_cast<int>((t_end - t_begin) / S::step);
+
+    // what this lane stages.  Lanes behind the last channel load the first ones again: what comes of them is not stored.
+    const int a_row = threadIdx.x / (TILE / 8), a_col = threadIdx.x % (TILE / 8) * 8;
+    const int b_row = threadIdx.x / (TILE / 16), b_col = threadIdx.x % (TILE / 16) * 16;
+    const int o = o0 + a_col, i = i0 + b_col < pitch ? i0 + b_col : 0;
+    const int a_there = outputs - o;          // elements of this lane's eight that exist
+    const int o_safe = a_there >= 8 ? o : 0;
+    const D* a_at = dy + (t_begin + a_row) * dy_stride + o_safe;
+    const signed char* b_at = q + (t_begin + b_row) * pitch + i;
+    const signed char* e_at = e + (t_begin + b_row) * (pitch / kBlock) + i / kBlock;
+    char* const a_lds = lds + a_row * S::pitch + a_col * 2;
+    char* const b_lds = lds + P * S::plane_bytes + b_row * S::pitch + b_col * 2;
+    // what it reads: of a run of 16 lanes, four lanes one token's sixteen channels
+    const int r_row = 8 * (lane >> 5) + ((lane & 15) >> 2), r_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    const char* const a_read = lds + r_row * S::pitch + (wo + r_col) * 2;
+    const char* const b_read = lds + P * S::plane_bytes + r_row * S::pitch + (wi + r_col) * 2;
+
+    f32x16 acc[F][F] = {};
+    Granule<D, 8> a_reg[S::a_passes];
+    u32x4 b_reg[S::b_passes];
+    int e_reg[S::b_passes];
+
+    auto load_a = [&](int k) { load_any(a_reg[k], a_at + k * S::a_rows * dy_stride); };
+    auto load_b = [&](int k) {
+        b_reg[k] = *reinterpret_cast<const u32x4*>(b_at + k * S::b_rows * pitch);
+        e_reg[k] = e_at[k * S::b_rows * (pitch / kBlock)];
+    };
+    auto write_a = [&](int k, int buffer, bool there) {
+        to_lds<D>(a_lds + buffer * S::buffer_bytes + k * S::a_rows * S::pitch, S::plane_bytes, a_reg[k], there);
+    };
+    auto write_b = [&](int k, int buffer, bool there) {
+        to_lds(E{}, b_lds + buffer * S::buffer_bytes + k * S::b_rows * S::pitch, b_reg[k], e_reg[k], there);
+    };
+    auto next = [&] {
+        a_at += S::step * dy_stride;
+        b_at += S::step * pitch;
+        e_at += S::step * (pitch / kBlock);
+    };
+    auto fragment = [&](const char* at) -> u32x4 {
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * S::pitch));
+        u32x4 f;
+        f.x = __builtin_bit_cast(u32x2, lo).x;
+        f.y = __builtin_bit_cast(u32x2, lo).y;
+        f.z = __builtin_bit_cast(u32x2, hi).x;
+        f.w = __builtin_bit_cast(u32x2, hi).y;
+        return f;
+    };
+    auto multiply = [&](int sub, int buffer) {
+        const int from = buffer * S::buffer_bytes + sub * 16 * S::pitch;
+        u32x4 b[F];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int o = o0 + wo + 32 * m + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, i = i0 + wi + 32 * n + (lane & 31);
-                if (o < outputs && i < width) {
-                    const long long at = static_cast<long long>(o) * width + i;
+        for (int k = 0; k < F; ++k) b[k] = fragment(b_read + from + 64 * k);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int m = 0; m < F; ++m) {
+                const u32x4 a = fragment(a_read + from + p * S::plane_bytes + 64 * m);
+#pragma unroll
+                for (int k = 0; k < F; ++k) acc[m][k] = mfma(E{}, b[k], a, acc[m][k]);
+            }
+    };
+
+    const bool ragged = o0 + TILE > outputs && (outputs & 7) != 0;
+    if (whole > 0 && !ragged) {
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k) load_a(k);
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k) load_b(k);
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k) write_a(k, 0, true);
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k) write_b(k, 0, true);
+        if (whole > 1) next();
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k) load_a(k);
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k) load_b(k);
+        __syncthreads();
+        for (int s = 0; s < whole; ++s) {
+            const int buffer = s & 1;
+            if (s + 2 < whole) next();     // (else the last whole step is loaded again, and not used)
+#pragma unroll
+            for (int sub = 0; sub < S::subs; ++sub) {
+                multiply(sub, buffer);
+#pragma unroll
+                for (int k = 0; k < S::a_passes; ++k)
+                    if (k * S::subs / S::a_passes == sub) {
+                        write_a(k, buffer ^ 1, true);
+                        load_a(k);
+                    }
+#pragma unroll
+                for (int k = 0; k < S::b_passes; ++k)
+                    if (k * S::subs / S::b_passes == sub) {
+                        write_b(k, buffer ^ 1, true);
+                        load_b(k);
+                    }
+            }
+            __syncthreads();
+        }
+    }
+    // the steps that are left: the last one, which may be short; all of them where the outputs end inside a lane's eight
+    for (int s = ragged ? 0 : whole; t_begin + static_cast<long long>(s) * S::step < t_end; ++s) {
+        const long long t0 = t_begin + static_cast<long long>(s) * S::step;
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k) {
+            const long long t = t0 + k * S::a_rows + a_row;
+            Granule<D, 8> g;
+#pragma unroll
+            for (int w = 0; w < Granule<D, 8>::NW; ++w) g.w[w] = 0;
+            if (t < t_end) {
+                const D* const at = dy + t * dy_stride + o;
+                if (a_there >= 8) {
+                    load_any(g, at);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < a_there) {
+                            if constexpr (sizeof(D) == 2) g.w[j / 2] |= static_cast<unsigned>(at[j].v) << (16 * (j & 1));
+                            else g.w[j] = __float_as_uint(at[j]);
+                        }
+                }
+            }
+            a_reg[k] = g;
+        }
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k) {
+            const long long t = min(t0 + k * S::b_rows + b_row, t_end - 1);
+            b_reg[k] = *reinterpret_cast<const u32x4*>(q + t * pitch + i);
+            e_reg[k] = e[t * (pitch / kBlock) + i / kBlock];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k) write_a(k, 0, true);
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k) write_b(k, 0, t0 + k * S::b_rows + b_row < t_end);
+        __syncthreads();
+#pragma unroll
+        for (int sub = 0; sub < S::subs; ++sub) multiply(sub, 0);
+    }
+
+    // a lane holds four consecutive channels of one output
+#pragma unroll
+    for (int m = 0; m < F; ++m)
+#pragma unroll
+        for (int k = 0; k < F; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int to = o0 + wo + 32 * m + (lane & 31), ti = i0 + wi + 32 * k + 8 * r + 4 * (lane >> 5);
+                if (to < outputs && ti < width) {
+                    float v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = acc[m][k][4 * r + j];
+                    const long long at = static_cast<long long>(to) * width + ti;
                     if (parts != nullptr) {
-                        parts[static_cast<long long>(blockIdx.y) * outputs * width + at] = acc[m][n][r];
+                        store_some<4>(parts + static_cast<long long>(part) * outputs * width + at, v, width - ti);
                     } else {
-                        store_elem(grad + at, accumulate ? acc[m][n][r] + load_elem(grad + at) : acc[m][n][r]);
+                        if (accumulate) {
+                            float old[4];
+                            load_some<4>(old, grad + at, width - ti);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[j] += old[j];
+                        }
+                        store_some<4>(grad + at, v, width - ti);
                     }
                 }
             }
@@ -165,14 +340,16 @@ int join(const float* parts, int64_t n_parts, int64_t n, T* out, int accumulate,
 }  // namespace
 
 WeightSplit weight_split(int64_t rows, int64_t width, int64_t outputs, int dtype) {
-    (void)dtype;
     WeightSplit s;
-    const int64_t tiles = ((outputs + kGradTile - 1) / kGradTile) * ((width + kGradTile - 1) / kGradTile);
-    const int64_t steps = (rows + kStepTokens - 1) / kStepTokens;
-    int64_t parts = tiles > 0 ? 512 / tiles : 1;
-    if (parts > steps / 8) parts = steps / 8;
+    auto tiles_of = [&](int edge) { return ((outputs + edge - 1) / edge) * ((width + edge - 1) / edge); };
+    s.tile = 256;
+    const int64_t step = dtype == ADASUM_F32 ? 32 : 64, tiles = tiles_of(s.tile);
+    const int64_t steps = (rows + step - 1) / step;
+    int64_t parts = tiles > 0 ? 256 / tiles : 1;
+    if (parts > steps / 4) parts = steps / 4;
     if (parts < 1) parts = 1;
     s.steps = (steps + parts - 1) / parts;
+    s.tokens = s.steps * step;
     s.parts = s.steps > 0 ? (steps + s.steps - 1) / s.steps : 1;
     if (s.parts > 1) {
         s.off_bias = align_up(static_cast<size_t>(s.parts) * outputs * width * 4, 256);
@@ -192,19 +369,24 @@ int launch_weight_grad(const WeightGrad& g, void* stream) {
             float* const parts = split ? reinterpret_cast<float*>(g.ws) : nullptr;
             float* const bias_parts = split ? reinterpret_cast<float*>(g.ws + g.split.off_bias) : nullptr;
             const D* const dy = static_cast<const D*>(g.dy);
-            const int64_t tiles_o = (g.outputs + kGradTile - 1) / kGradTile, tiles_i = (g.x.width + kGradTile - 1) / kGradTile;
+            const int64_t tiles_o = (g.outputs + g.split.tile - 1) / g.split.tile, tiles_i = (g.x.width + g.split.tile - 1) / g.split.tile;
             int rc = 0;
             if (tiles_i > 0) {
                 T* const grad = static_cast<T*>(g.grad);
-                rc = launch(weight_grad_kernel<D, T>, tiles_o * tiles_i, g.split.parts, 256, 0, stream, reinterpret_cast<const signed char*>(g.x.q),
+                const bool wide = g.split.tile == 256;
+                const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
+                const auto kernel = wide ? weight_grad_kernel<D, T, 256> : weight_grad_kernel<D, T, 128>;
+                rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+                if (rc != 0) return rc;
+                rc = launch(kernel, tiles_o * tiles_i * g.split.parts, 1, 256, lds, stream, reinterpret_cast<const signed char*>(g.x.q),
                             reinterpret_cast<const signed char*>(g.x.e), g.x.rows, g.x.width, g.x.pitch, dy, g.dy_stride, g.outputs, grad,
-                            g.accumulate, parts, g.split.steps, tiles_i);
+                            g.accumulate, parts, g.split.steps, tiles_o, tiles_i);
                 if (rc == 0 && split) rc = join(parts, g.split.parts, g.outputs * g.x.width, grad, g.accumulate, stream);
             }
             if (rc != 0 || g.bias == nullptr) return rc;
             T* const bias = static_cast<T*>(g.bias);
             rc = launch(bias_kernel<D, T>, (g.outputs + 63) / 64, g.split.parts, 256, 0, stream, g.x.rows, dy, g.dy_stride, g.outputs, bias,
-                        g.accumulate, bias_parts, g.split.steps * kStepTokens);
+                        g.accumulate, bias_parts, g.split.tokens);
             return rc == 0 && split ? join(bias_parts, g.split.parts, g.outputs, bias, g.accumulate, stream) : rc;
         }
     });
