@@ -97,14 +97,17 @@ __device__ __forceinline__ void to_lds(char* at, int plane_bytes, const Granule<
 template <typename E>
 __device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) {
     const float step = !there ? 0.f : __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
+    unsigned word[4] = {q.x, q.y, q.z, q.w};
+    // (here and not before: the compiler would take the bytes apart where they are loaded, and wait for the load there)
+    asm volatile("" : "+v"(word[0]), "+v"(word[1]), "+v"(word[2]), "+v"(word[3]));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         u32x4 w;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const unsigned word = q[2 * h + i / 2] >> (16 * (i & 1));
-            const float a = static_cast<float>(static_cast<signed char>(word)) * step;
-            const float b = static_cast<float>(static_cast<signed char>(word >> 8)) * step;
+            const unsigned from = word[2 * h + i / 2];
+            const float a = static_cast<float>(static_cast<signed char>(i & 1 ? from >> 16 : from)) * step;
+            const float b = static_cast<float>(static_cast<signed char>(i & 1 ? from >> 24 : from >> 8)) * step;
             w[i] = exact_pair(E{}, a, b);
         }
         *reinterpret_cast<u32x4*>(at + 16 * h) = w;
@@ -180,57 +183,77 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         f.w = __builtin_bit_cast(u32x2, hi).y;
         return f;
     };
-    auto multiply = [&](int sub, int buffer) {
+    u32x4 fa[2][F], fb[2][F];
+    auto read = [&](int set, int sub, int buffer) {
         const int from = buffer * S::buffer_bytes + sub * 16 * S::pitch;
-        u32x4 b[F];
 #pragma unroll
-        for (int k = 0; k < F; ++k) b[k] = fragment(b_read + from + 64 * k);
+        for (int k = 0; k < F; ++k) fb[set][k] = fragment(b_read + from + 64 * k);
+#pragma unroll
+        for (int k = 0; k < F; ++k) fa[set][k] = fragment(a_read + from + 64 * k);
+    };
+    // (the first part of dy is in registers already; the others of fp32 follow)
+    auto multiply = [&](int set, int sub, int buffer) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int m = 0; m < F; ++m) {
-                const u32x4 a = fragment(a_read + from + p * S::plane_bytes + 64 * m);
+                const u32x4 a = p == 0 ? fa[set][m] : fragment(a_read + buffer * S::buffer_bytes + sub * 16 * S::pitch + p * S::plane_bytes + 64 * m);
 #pragma unroll
-                for (int k = 0; k < F; ++k) acc[m][k] = mfma(E{}, b[k], a, acc[m][k]);
+                for (int k = 0; k < F; ++k) acc[m][k] = mfma(E{}, fb[set][k], a, acc[m][k]);
             }
     };
 
     const bool ragged = o0 + TILE > outputs && (outputs & 7) != 0;
+    // which passes are staged beside which sixteen tokens' products: all before the last ones, which the barrier comes before
+    auto staged = [&](int sub, auto&& a, auto&& b) {
+#pragma unroll
+        for (int k = 0; k < S::a_passes; ++k)
+            if (k * (S::subs - 1) / S::a_passes == sub) a(k);
+#pragma unroll
+        for (int k = 0; k < S::b_passes; ++k)
+            if (k * (S::subs - 1) / S::b_passes == sub) b(k);
+    };
     if (whole > 0 && !ragged) {
 #pragma unroll
-        for (int k = 0; k < S::a_passes; ++k) load_a(k);
+        for (int sub = 0; sub < S::subs; ++sub) staged(sub, load_a, load_b);
 #pragma unroll
-        for (int k = 0; k < S::b_passes; ++k) load_b(k);
-#pragma unroll
-        for (int k = 0; k < S::a_passes; ++k) write_a(k, 0, true);
-#pragma unroll
-        for (int k = 0; k < S::b_passes; ++k) write_b(k, 0, true);
+        for (int sub = 0; sub < S::subs; ++sub)
+            staged(sub, [&](int k) { write_a(k, 0, true); }, [&](int k) { write_b(k, 0, true); });
         if (whole > 1) next();
+        // (the loads are in flight in the order in which the loop issues them: what waits for one waits for no later one)
 #pragma unroll
-        for (int k = 0; k < S::a_passes; ++k) load_a(k);
-#pragma unroll
-        for (int k = 0; k < S::b_passes; ++k) load_b(k);
+        for (int sub = 0; sub < S::subs; ++sub) {
+            __builtin_amdgcn_sched_barrier(0);
+            staged(sub, load_a, load_b);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         __syncthreads();
+        read(0, 0, 0);
         for (int s = 0; s < whole; ++s) {
             const int buffer = s & 1;
             if (s + 2 < whole) next();     // (else the last whole step is loaded again, and not used)
 #pragma unroll
             for (int sub = 0; sub < S::subs; ++sub) {
-                multiply(sub, buffer);
-#pragma unroll
-                for (int k = 0; k < S::a_passes; ++k)
-                    if (k * S::subs / S::a_passes == sub) {
-                        write_a(k, buffer ^ 1, true);
-                        load_a(k);
-                    }
-#pragma unroll
-                for (int k = 0; k < S::b_passes; ++k)
-                    if (k * S::subs / S::b_passes == sub) {
-                        write_b(k, buffer ^ 1, true);
-                        load_b(k);
-                    }
+                __builtin_amdgcn_sched_barrier(0);
+                // the next sixteen tokens' operands, of the next step's buffer behind the last ones
+                if (sub + 1 < S::subs) {
+                    read((sub + 1) & 1, sub + 1, buffer);
+                } else {
+                    __syncthreads();
+                    read(0, 0, buffer ^ 1);
+                }
+                multiply(sub & 1, sub, buffer);
+                staged(sub,
+                       [&](int k) {
+                           write_a(k, buffer ^ 1, true);
+                           load_a(k);
+                       },
+                       [&](int k) {
+                           write_b(k, buffer ^ 1, true);
+                           load_b(k);
+                       });
             }
-            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     // the steps that are left: the last one, which may be short; all of them where the outputs end inside a lane's eight
@@ -270,7 +293,10 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         for (int k = 0; k < S::b_passes; ++k) write_b(k, 0, t0 + k * S::b_rows + b_row < t_end);
         __syncthreads();
 #pragma unroll
-        for (int sub = 0; sub < S::subs; ++sub) multiply(sub, 0);
+        for (int sub = 0; sub < S::subs; ++sub) {
+            read(0, sub, 0);
+            multiply(0, sub, 0);
+        }
     }
 
     // a lane holds four consecutive channels of one output
