@@ -372,9 +372,9 @@ ADASUM_API int adasum_embedding_grad(const void* dy, int dtype, int64_t dy_strid
  * row (the last may be shorter) share an exponent e:
  *   e = floor(log2(max |x|)) - 6, but at least -120 (also for a block of zeros);
  *   q = x / 2^e rounded to nearest even, and to at most 127 in magnitude;   x is kept as q * 2^e.
- * That is off by at most half of 2^e (all of it where |x| / 2^e > 127), which is at most 2^-7 (2^-6) of the block's
- * largest value, and by at most 2^-121 in blocks below 2^-114.  q * 2^e has seven significant bits: it is a value of the type that x had, so that what follows computes
- * with exactly what is kept.  A block with an infinity or NaN in it is kept as NaN (e = -128).
+ * That is off by at most half of 2^e, 2^-7 of the block's largest value (where |x| / 2^e > 127.5 by up to all of it), and by
+ * at most 2^-121 in blocks that stay below 2^-114.  q * 2^e has seven significant bits: it is a value of the type that x had,
+ * so that what follows computes with exactly what is kept.  A block with an infinity or NaN in it is kept as NaN (e = -128).
  * Layout: rows x pitch bytes of q (int8; pitch = width rounded up to a whole block, zeros behind the last
  * channel), then rows x (pitch / 32) bytes of e (int8): adasum_checkpoint_bytes in all, 16-byte aligned.
  * rows at most 2^31 - 65536, width at most 2^24.
@@ -404,8 +404,9 @@ ADASUM_API int adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows, 
  *   grad[offset + o * width + i]  (+)= sum_t dy[t][o] * x[t][i]
  *   grad[bias_offset + o]         (+)= sum_t dy[t][o]           (bias_offset < 0: no bias)
  * The products are exact (matrix cores; fp32 dy as three bf16 parts) and summed in fp32.  With `dtype`
- * ADASUM_F16 the kept values must be fp16's own: a checkpoint of fp16 activations (others are rounded to
- * fp16).  rows, width and outputs as above; outputs at most 2^24.
+ * ADASUM_F16 the kept values must be fp16's own: a checkpoint of fp16 activations (others are cut to
+ * fp16).  rows and width as above; outputs at most 2^24.  A layer without inputs (width 0) has no bias here
+ * (ADASUM_ERR_INVALID_ARG).
  */
 ADASUM_API int adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t width, int64_t outputs,
                                                              int dtype, size_t* bytes);

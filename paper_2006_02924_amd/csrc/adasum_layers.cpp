@@ -206,7 +206,8 @@ int adasum_checkpoint_weight_grad(const void* checkpoint, int64_t rows, int64_t 
     ADASUM_CHECK(check_flat(grad, offset, outputs * width));
     const bool with_bias = bias_offset >= 0;
     if (with_bias) ADASUM_CHECK(check_flat(grad, bias_offset, outputs));
-    if (outputs == 0 || (width == 0 && !with_bias)) return ADASUM_OK;
+    if (outputs == 0) return ADASUM_OK;
+    if (width == 0) return with_bias ? ADASUM_ERR_INVALID_ARG : ADASUM_OK;
     WeightGrad g{};
     g.split = weight_split(rows, width, outputs, dtype);
     ADASUM_CHECK(check_workspace(workspace, workspace_bytes, g.split.total));

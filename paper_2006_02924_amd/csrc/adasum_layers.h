@@ -96,8 +96,8 @@ int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t d
 // `tokens` in all.
 struct WeightSplit {
     int tile = 0;
-    int64_t parts = 1, steps = 0, tokens = 0;
-    size_t off_bias = 0;      // fp32 [parts][outputs], behind fp32 [parts][outputs][width]
+    int64_t parts = 1, steps = 0;
+    size_t off_bias = 0;      // fp32 [parts][outputs], behind fp32 [parts][outputs][width] (with more than one part)
     size_t total = 0;
 };
 WeightSplit weight_split(int64_t rows, int64_t width, int64_t outputs, int dtype);

@@ -46,6 +46,29 @@ __device__ __forceinline__ unsigned exact_pair(f16_t, float a, float b) {
     return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
+// c and the sum of eight values.  The instruction multiplies with one, exactly, and adds with truncation: a step's run of them is then
+// added to the rest with rounding.
+__device__ __forceinline__ float plus_eight(bf16_t, u32x4 a, float c) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    const pair one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned w = a[i];
+        c = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair, w), one, c, false);
+    }
+    return c;
+}
+__device__ __forceinline__ float plus_eight(f16_t, u32x4 a, float c) {
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    const pair one = {static_cast<_Float16>(1.f), static_cast<_Float16>(1.f)};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned w = a[i];
+        c = __builtin_amdgcn_fdot2(__builtin_bit_cast(pair, w), one, c, false);
+    }
+    return c;
+}
+
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
@@ -124,7 +147,8 @@ template <typename D, typename T, int TILE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE == 256 ? 1 : 2)))
 weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
                    const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ grad, int accumulate,
-                   float* __restrict__ parts, long long steps, unsigned tiles_o, unsigned tiles_i) {
+                   float* __restrict__ parts, long long steps, unsigned tiles_o, unsigned tiles_i, T* __restrict__ bias,
+                   float* __restrict__ bias_parts) {
     typedef typename Products<D>::type E;
     typedef GradShape<D, TILE> S;
     constexpr int P = S::planes, F = S::frags;
@@ -153,6 +177,8 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     const char* const b_read = lds + P * S::plane_bytes + r_row * S::pitch + (wi + r_col) * 2;
 
     f32x16 acc[F][F] = {};
+    // dy's sums over this lane's tokens, of a step and of all (every workgroup and wave along the weight's rows has them, one stores them)
+    float run[F] = {}, total[F] = {};
     Granule<D, 8> a_reg[S::a_passes];
     u32x4 b_reg[S::b_passes];
     int e_reg[S::b_passes];
@@ -177,10 +203,11 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 4 * S::pitch));
         u32x4 f;
-        f.x = __builtin_bit_cast(u32x2, lo).x;
-        f.y = __builtin_bit_cast(u32x2, lo).y;
-        f.z = __builtin_bit_cast(u32x2, hi).x;
-        f.w = __builtin_bit_cast(u32x2, hi).y;
+        const u32x2 l = __builtin_bit_cast(u32x2, lo), h = __builtin_bit_cast(u32x2, hi);
+        f.x = l.x;
+        f.y = l.y;
+        f.z = h.x;
+        f.w = h.y;
         return f;
     };
     u32x4 fa[2][F], fb[2][F];
@@ -200,10 +227,18 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
                 const u32x4 a = p == 0 ? fa[set][m] : fragment(a_read + buffer * S::buffer_bytes + sub * 16 * S::pitch + p * S::plane_bytes + 64 * m);
 #pragma unroll
                 for (int k = 0; k < F; ++k) acc[m][k] = mfma(E{}, fb[set][k], a, acc[m][k]);
+                run[m] = plus_eight(E{}, a, run[m]);
             }
     };
 
     const bool ragged = o0 + TILE > outputs && (outputs & 7) != 0;
+    auto end_run = [&] {
+#pragma unroll
+        for (int m = 0; m < F; ++m) {
+            total[m] += run[m];
+            run[m] = 0.f;
+        }
+    };
     // which passes are staged beside which sixteen tokens' products: all before the last ones, which the barrier comes before
     auto staged = [&](int sub, auto&& a, auto&& b) {
 #pragma unroll
@@ -253,6 +288,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
                            load_b(k);
                        });
             }
+            end_run();
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -297,8 +333,20 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             read(0, sub, 0);
             multiply(0, sub, 0);
         }
+        end_run();
     }
 
+    if (bias != nullptr && i0 == 0 && wi == 0) {
+#pragma unroll
+        for (int m = 0; m < F; ++m) {
+            const float v = total[m] + __shfl_xor(total[m], 32, 64);
+            const int at = o0 + wo + 32 * m + lane;
+            if (lane < 32 && at < outputs) {
+                if (bias_parts != nullptr) bias_parts[static_cast<long long>(part) * outputs + at] = v;
+                else store_elem(bias + at, accumulate ? v + load_elem(bias + at) : v);
+            }
+        }
+    }
     // a lane holds four consecutive channels of one output
 #pragma unroll
     for (int m = 0; m < F; ++m)
@@ -327,40 +375,35 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             }
 }
 
-// dy's sums: a workgroup takes 64 outputs over one part of the tokens.
-template <typename D, typename T>
-__global__ void __launch_bounds__(256)
-bias_kernel(long long rows, const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ bias, int accumulate,
-            float* __restrict__ parts, long long tokens) {
-    __shared__ double sums[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int o = static_cast<int>(blockIdx.x) * 64 + lane;
-    const long long t_begin = blockIdx.y * tokens, t_end = min(rows, t_begin + tokens);
-    double sum = 0;
-    if (o < outputs)
-        for (long long t = t_begin + wave; t < t_end; t += 4) sum += load_elem(dy + t * dy_stride + o);
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave != 0 || o >= outputs) return;
-    const float s = static_cast<float>(sums[0][lane] + sums[1][lane] + (sums[2][lane] + sums[3][lane]));
-    if (parts != nullptr) parts[static_cast<long long>(blockIdx.y) * outputs + o] = s;
-    else store_elem(bias + o, accumulate ? s + load_elem(bias + o) : s);
-}
-
-// out (+)= the sum of the parts, in their order.
+// out (+)= the sum of the parts, in their order: the weight's in the first `groups` workgroups, the bias's in the others.
 template <typename T>
-__global__ void __launch_bounds__(256)
-join_parts_kernel(const float* __restrict__ parts, int n_parts, long long n, T* __restrict__ out, int accumulate) {
-    for (long long at = blockIdx.x * 256ll + threadIdx.x; at < n; at += 256ll * gridDim.x) {
-        float s = 0.f;
-        for (int p = 0; p < n_parts; ++p) s += parts[p * n + at];
-        store_elem(out + at, accumulate ? s + load_elem(out + at) : s);
+struct Joined {
+    const float* parts;
+    int n_parts;
+    long long n;
+    T* out;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) join_parts_kernel(Joined<T> weight, int groups, Joined<T> bias, int accumulate) {
+    const bool first = static_cast<int>(blockIdx.x) < groups;
+    const Joined<T> j = first ? weight : bias;
+    const long long block = first ? blockIdx.x : blockIdx.x - groups, blocks = first ? groups : gridDim.x - groups;
+    for (long long at = 4 * (block * 256 + threadIdx.x); at < j.n; at += 1024 * blocks) {
+        const int there = static_cast<int>(min(4ll, j.n - at));
+        float s[4] = {}, v[4];
+#pragma unroll 4
+        for (int p = 0; p < j.n_parts; ++p) {
+            load_some<4>(v, j.parts + p * j.n + at, there);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] += v[k];
+        }
+        if (accumulate) {
+            load_some<4>(v, j.out + at, there);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] += v[k];
+        }
+        store_some<4>(j.out + at, s, there);
     }
-}
-
-template <typename T>
-int join(const float* parts, int64_t n_parts, int64_t n, T* out, int accumulate, void* stream) {
-    return launch(join_parts_kernel<T>, at_most_groups((n + 255) / 256), 1, 256, 0, stream, parts, n_parts, n, out, accumulate);
 }
 
 }  // namespace
@@ -375,7 +418,6 @@ WeightSplit weight_split(int64_t rows, int64_t width, int64_t outputs, int dtype
     if (parts > steps / 4) parts = steps / 4;
     if (parts < 1) parts = 1;
     s.steps = (steps + parts - 1) / parts;
-    s.tokens = s.steps * step;
     s.parts = s.steps > 0 ? (steps + s.steps - 1) / s.steps : 1;
     if (s.parts > 1) {
         s.off_bias = align_up(static_cast<size_t>(s.parts) * outputs * width * 4, 256);
@@ -391,29 +433,26 @@ int launch_weight_grad(const WeightGrad& g, void* stream) {
         if constexpr (sizeof(D) == 8 || sizeof(T) == 8) {
             return static_cast<int>(hipErrorInvalidValue);   // (refused before)
         } else {
-            const bool split = g.split.parts > 1;
-            float* const parts = split ? reinterpret_cast<float*>(g.ws) : nullptr;
-            float* const bias_parts = split ? reinterpret_cast<float*>(g.ws + g.split.off_bias) : nullptr;
-            const D* const dy = static_cast<const D*>(g.dy);
-            const int64_t tiles_o = (g.outputs + g.split.tile - 1) / g.split.tile, tiles_i = (g.x.width + g.split.tile - 1) / g.split.tile;
-            int rc = 0;
-            if (tiles_i > 0) {
-                T* const grad = static_cast<T*>(g.grad);
-                const bool wide = g.split.tile == 256;
-                const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
-                const auto kernel = wide ? weight_grad_kernel<D, T, 256> : weight_grad_kernel<D, T, 128>;
-                rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-                if (rc != 0) return rc;
-                rc = launch(kernel, tiles_o * tiles_i * g.split.parts, 1, 256, lds, stream, reinterpret_cast<const signed char*>(g.x.q),
-                            reinterpret_cast<const signed char*>(g.x.e), g.x.rows, g.x.width, g.x.pitch, dy, g.dy_stride, g.outputs, grad,
-                            g.accumulate, parts, g.split.steps, tiles_o, tiles_i);
-                if (rc == 0 && split) rc = join(parts, g.split.parts, g.outputs * g.x.width, grad, g.accumulate, stream);
-            }
-            if (rc != 0 || g.bias == nullptr) return rc;
+            const WeightSplit& w = g.split;
+            float* const parts = w.parts > 1 ? reinterpret_cast<float*>(g.ws) : nullptr;
+            float* const bias_parts = w.parts > 1 ? reinterpret_cast<float*>(g.ws + w.off_bias) : nullptr;
+            T* const grad = static_cast<T*>(g.grad);
             T* const bias = static_cast<T*>(g.bias);
-            rc = launch(bias_kernel<D, T>, (g.outputs + 63) / 64, g.split.parts, 256, 0, stream, g.x.rows, dy, g.dy_stride, g.outputs, bias,
-                        g.accumulate, bias_parts, g.split.tokens);
-            return rc == 0 && split ? join(bias_parts, g.split.parts, g.outputs, bias, g.accumulate, stream) : rc;
+            // (a layer without inputs has a bias all the same)
+            const int64_t tiles_o = (g.outputs + w.tile - 1) / w.tile, tiles_i = g.x.width > 0 ? (g.x.width + w.tile - 1) / w.tile : 1;
+            const bool wide = w.tile == 256;
+            const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
+            const auto kernel = wide ? weight_grad_kernel<D, T, 256> : weight_grad_kernel<D, T, 128>;
+            int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            if (rc != 0) return rc;
+            rc = launch(kernel, tiles_o * tiles_i * w.parts, 1, 256, lds, stream, reinterpret_cast<const signed char*>(g.x.q),
+                        reinterpret_cast<const signed char*>(g.x.e), g.x.rows, g.x.width, g.x.pitch, static_cast<const D*>(g.dy), g.dy_stride,
+                        g.outputs, grad, g.accumulate, parts, w.steps, tiles_o, tiles_i, bias, bias_parts);
+            if (rc != 0 || parts == nullptr) return rc;
+            const Joined<T> weights{parts, static_cast<int>(w.parts), g.outputs * g.x.width, grad};
+            const Joined<T> sums{bias_parts, static_cast<int>(w.parts), bias != nullptr ? g.outputs : 0, bias};
+            const int64_t groups = at_most_groups((weights.n + 1023) / 1024);
+            return launch(join_parts_kernel<T>, groups + (sums.n + 1023) / 1024, 1, 256, 0, stream, weights, groups, sums, g.accumulate);
         }
     });
 }

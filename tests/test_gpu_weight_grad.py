@@ -119,10 +119,30 @@ def test_small_fp16_values():
     """fp16's smallest numbers count in the products."""
     x, dy = (rand(7, 64, 64) * 2.0 ** -18).half(), (rand(8, 64, 64) * 2.0 ** -17).half()
     kept = B.adasum_checkpoint_store(x.cuda())
-    flat = torch.empty(64 * 64, device="cuda")
-    B.adasum_checkpoint_weight_grad(kept, dy.cuda(), flat, 0)
+    flat = torch.empty(64 * 64 + 64, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy.cuda(), flat, 0, bias_offset=64 * 64)
     v, d = f64(B.adasum_checkpoint_load(kept)), f64(dy)
-    check(f64(flat).reshape(64, 64), d.T @ v, np.abs(d).T @ np.abs(v), 64, torch.float32)
+    check(f64(flat[:4096]).reshape(64, 64), d.T @ v, np.abs(d).T @ np.abs(v), 64, torch.float32)
+    check(f64(flat[4096:]), d.sum(0), np.abs(d).sum(0), 64, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", KEPT)
+def test_long_sums_of_one_sign(dtype):
+    """Roundings that all go one way would show here: 40000 tokens, all of them positive."""
+    dtype = DTYPES[dtype]
+    n = 40000
+    x = (rand(15, n, 40).abs() + 0.5).to(dtype).cuda()
+    dy = (rand(16, n, 70).abs() + 0.5).to(dtype).cuda()
+    kept = B.adasum_checkpoint_store(x)
+    flat = torch.empty(70 * 41, device="cuda")
+    B.adasum_checkpoint_weight_grad(kept, dy, flat, 0, bias_offset=70 * 40)
+    v, d = f64(B.adasum_checkpoint_load(kept)), f64(dy)
+    # the matrix cores' own additions may all go one way: one step of fp32 for every sixteen products (three times as many for fp32) of a
+    # part; the bias's do in runs of a step's 16 additions at most, beyond which they are rounded (a random walk, twelve times its length's root)
+    w = d.T @ v
+    within(f64(flat[:2800]).reshape(70, 40), w, w * (3 * n / 16) * 2.0 ** -23)
+    b = d.sum(0)
+    within(f64(flat[2800:]), b, b * (3 * 16 + 12 * (n / 64) ** 0.5) * 2.0 ** -23)
 
 
 def test_gradient_against_differences():

@@ -120,6 +120,7 @@ def test_nothing_to_do_needs_no_device(lib):
     assert act_grad(lib, rows=0, kept=None, dy=None, dx=None) == B.OK
     assert weight_grad(lib, outputs=0, dy=None, grad=None) == B.OK
     assert weight_grad(lib, width=0, kept=None, grad=None, bias=-1) == B.OK
+    assert weight_grad(lib, width=0, kept=None) == B.ERR_INVALID_ARG          # a layer without inputs has no bias here
 
 
 @pytest.mark.parametrize("rows, width, want", [(0, 5, 0), (3, 0, 0), (1, 1, 33), (2, 32, 66), (2, 33, 132), (7, 1023, 7 * 32 * 33)])
