@@ -81,17 +81,20 @@ __device__ __forceinline__ unsigned die_order(unsigned b, unsigned n) {
 // What a workgroup does, by the edge of its square of dW (TILE) and the storage type of dy.
 template <typename D, int TILE>
 struct GradShape {
+    // waves along the outputs and the channels, and the 32 x 32 blocks each has along them
+    static constexpr int waves_o = TILE == 256 ? 4 : 2, waves_i = 2;
+    static constexpr int frags_o = TILE / 32 / waves_o, frags_i = TILE / 32 / waves_i;
+    static constexpr int threads = 64 * waves_o * waves_i;
     static constexpr int planes = Products<D>::planes;
     static constexpr int step = planes == 3 ? 32 : 64;          // tokens of a step
     static constexpr int subs = step / 16;                      // matrix instructions' share of it
-    static constexpr int frags = TILE / 64;                     // 32 x 32 blocks of a wave along either edge
     // LDS: [token][channel], rows TILE channels and 64 bytes apart, so that the transposing read's four rows of 32 bytes lie in
     // different banks
     static constexpr int pitch = 2 * TILE + 64;
     static constexpr int plane_bytes = step * pitch;
     static constexpr int buffer_bytes = (planes + 1) * plane_bytes;
-    // 256 lanes stage eight channels of dy, and sixteen of x, of a token at a time
-    static constexpr int a_rows = 256 / (TILE / 8), b_rows = 256 / (TILE / 16);
+    // a lane stages eight channels of dy, and sixteen of x, of a token at a time
+    static constexpr int a_rows = threads / (TILE / 8), b_rows = threads / (TILE / 16);
     static constexpr int a_passes = step / a_rows, b_passes = step / b_rows;
     static constexpr int lds_bytes = 2 * buffer_bytes;
 };
@@ -144,19 +147,19 @@ __device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) 
 // one buffer, the next one, which is in registers by then, is written into the other and the loads of the one after are issued, a
 // part of them beside every sixteen tokens' products.  One barrier a step.
 template <typename D, typename T, int TILE>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TILE == 256 ? 1 : 2)))
+__global__ void __launch_bounds__((GradShape<D, TILE>::threads), 2)
 weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
                    const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ grad, int accumulate,
                    float* __restrict__ parts, long long steps, unsigned tiles_o, unsigned tiles_i, T* __restrict__ bias,
                    float* __restrict__ bias_parts) {
     typedef typename Products<D>::type E;
     typedef GradShape<D, TILE> S;
-    constexpr int P = S::planes, F = S::frags;
+    constexpr int P = S::planes, FO = S::frags_o, FI = S::frags_i;
     extern __shared__ __align__(16) char lds[];
     const unsigned n = die_order(blockIdx.x, gridDim.x), tile = n % (tiles_o * tiles_i), part = n / (tiles_o * tiles_i);
     const int o0 = static_cast<int>(tile / tiles_i) * TILE, i0 = static_cast<int>(tile % tiles_i) * TILE;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wo = (wave >> 1) * (TILE / 2), wi = (wave & 1) * (TILE / 2);
+    const int wo = wave / S::waves_i * (32 * FO), wi = wave % S::waves_i * (32 * FI);
     const long long t_begin = part * steps * S::step, t_end = min(rows, t_begin + steps * S::step);
     const int whole = static_cast<int>((t_end - t_begin) / S::step);
 
@@ -176,9 +179,9 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     const char* const a_read = lds + r_row * S::pitch + (wo + r_col) * 2;
     const char* const b_read = lds + P * S::plane_bytes + r_row * S::pitch + (wi + r_col) * 2;
 
-    f32x16 acc[F][F] = {};
+    f32x16 acc[FO][FI] = {};
     // dy's sums over this lane's tokens, of a step and of all (every workgroup and wave along the weight's rows has them, one stores them)
-    float run[F] = {}, total[F] = {};
+    float run[FO] = {}, total[FO] = {};
     Granule<D, 8> a_reg[S::a_passes];
     u32x4 b_reg[S::b_passes];
     int e_reg[S::b_passes];
@@ -210,23 +213,27 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         f.w = h.y;
         return f;
     };
-    u32x4 fa[2][F], fb[2][F];
+        // two sets of operands: the next sixteen tokens' are read beside this one's products.  (With fp32's three parts there is enough to
+    // do beside one set's reads: 117 us for 122, 4096 x 1024 x 4096.)
+    constexpr int SETS = P == 3 ? 1 : 2;
+    u32x4 fa[SETS][FO], fb[SETS][FI];
     auto read = [&](int set, int sub, int buffer) {
         const int from = buffer * S::buffer_bytes + sub * 16 * S::pitch;
 #pragma unroll
-        for (int k = 0; k < F; ++k) fb[set][k] = fragment(b_read + from + 64 * k);
+        for (int k = 0; k < FI; ++k) fb[set % SETS][k] = fragment(b_read + from + 64 * k);
 #pragma unroll
-        for (int k = 0; k < F; ++k) fa[set][k] = fragment(a_read + from + 64 * k);
+        for (int m = 0; m < FO; ++m) fa[set % SETS][m] = fragment(a_read + from + 64 * m);
     };
     // (the first part of dy is in registers already; the others of fp32 follow)
     auto multiply = [&](int set, int sub, int buffer) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int m = 0; m < F; ++m) {
-                const u32x4 a = p == 0 ? fa[set][m] : fragment(a_read + buffer * S::buffer_bytes + sub * 16 * S::pitch + p * S::plane_bytes + 64 * m);
+            for (int m = 0; m < FO; ++m) {
+                const u32x4 a = p == 0 ? fa[set % SETS][m]
+                                       : fragment(a_read + buffer * S::buffer_bytes + sub * 16 * S::pitch + p * S::plane_bytes + 64 * m);
 #pragma unroll
-                for (int k = 0; k < F; ++k) acc[m][k] = mfma(E{}, fb[set][k], a, acc[m][k]);
+                for (int k = 0; k < FI; ++k) acc[m][k] = mfma(E{}, fb[set % SETS][k], a, acc[m][k]);
                 run[m] = plus_eight(E{}, a, run[m]);
             }
     };
@@ -234,7 +241,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     const bool ragged = o0 + TILE > outputs && (outputs & 7) != 0;
     auto end_run = [&] {
 #pragma unroll
-        for (int m = 0; m < F; ++m) {
+        for (int m = 0; m < FO; ++m) {
             total[m] += run[m];
             run[m] = 0.f;
         }
@@ -243,10 +250,10 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     auto staged = [&](int sub, auto&& a, auto&& b) {
 #pragma unroll
         for (int k = 0; k < S::a_passes; ++k)
-            if (k * (S::subs - 1) / S::a_passes == sub) a(k);
+            if (k * (S::subs - (SETS == 2)) / S::a_passes == sub) a(k);
 #pragma unroll
         for (int k = 0; k < S::b_passes; ++k)
-            if (k * (S::subs - 1) / S::b_passes == sub) b(k);
+            if (k * (S::subs - (SETS == 2)) / S::b_passes == sub) b(k);
     };
     if (whole > 0 && !ragged) {
 #pragma unroll
@@ -263,21 +270,25 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         }
         __builtin_amdgcn_sched_barrier(0);
         __syncthreads();
-        read(0, 0, 0);
+        if constexpr (SETS == 2) read(0, 0, 0);
         for (int s = 0; s < whole; ++s) {
             const int buffer = s & 1;
             if (s + 2 < whole) next();     // (else the last whole step is loaded again, and not used)
 #pragma unroll
             for (int sub = 0; sub < S::subs; ++sub) {
                 __builtin_amdgcn_sched_barrier(0);
-                // the next sixteen tokens' operands, of the next step's buffer behind the last ones
-                if (sub + 1 < S::subs) {
-                    read((sub + 1) & 1, sub + 1, buffer);
+                if constexpr (SETS == 2) {
+                    // the next sixteen tokens' operands, of the next step's buffer behind the last ones
+                    if (sub + 1 < S::subs) {
+                        read(sub + 1, sub + 1, buffer);
+                    } else {
+                        __syncthreads();
+                        read(0, 0, buffer ^ 1);
+                    }
                 } else {
-                    __syncthreads();
-                    read(0, 0, buffer ^ 1);
+                    read(0, sub, buffer);
                 }
-                multiply(sub & 1, sub, buffer);
+                multiply(sub, sub, buffer);
                 staged(sub,
                        [&](int k) {
                            write_a(k, buffer ^ 1, true);
@@ -289,6 +300,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
                        });
             }
             end_run();
+            if constexpr (SETS == 1) __syncthreads();
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -338,7 +350,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
 
     if (bias != nullptr && i0 == 0 && wi == 0) {
 #pragma unroll
-        for (int m = 0; m < F; ++m) {
+        for (int m = 0; m < FO; ++m) {
             const float v = total[m] + __shfl_xor(total[m], 32, 64);
             const int at = o0 + wo + 32 * m + lane;
             if (lane < 32 && at < outputs) {
@@ -349,9 +361,9 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     }
     // a lane holds four consecutive channels of one output
 #pragma unroll
-    for (int m = 0; m < F; ++m)
+    for (int m = 0; m < FO; ++m)
 #pragma unroll
-        for (int k = 0; k < F; ++k)
+        for (int k = 0; k < FI; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int to = o0 + wo + 32 * m + (lane & 31), ti = i0 + wi + 32 * k + 8 * r + 4 * (lane >> 5);
@@ -375,7 +387,8 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             }
 }
 
-// out (+)= the sum of the parts, in their order: the weight's in the first `groups` workgroups, the bias's in the others.
+// out (+)= the sum of the parts, in a fixed order: the weight's in the first `groups` workgroups, the bias's in the others.  WAYS waves
+// share the parts of 256 elements, where there are many parts of few.
 template <typename T>
 struct Joined {
     const float* parts;
@@ -383,47 +396,84 @@ struct Joined {
     long long n;
     T* out;
 };
-template <typename T>
+template <typename T, int WAYS>
 __global__ void __launch_bounds__(256) join_parts_kernel(Joined<T> weight, int groups, Joined<T> bias, int accumulate) {
+    __shared__ float shared[WAYS][WAYS > 1 ? 256 : 1];
     const bool first = static_cast<int>(blockIdx.x) < groups;
     const Joined<T> j = first ? weight : bias;
     const long long block = first ? blockIdx.x : blockIdx.x - groups, blocks = first ? groups : gridDim.x - groups;
-    for (long long at = 4 * (block * 256 + threadIdx.x); at < j.n; at += 1024 * blocks) {
+    const int way = WAYS > 1 ? threadIdx.x >> 6 : 0, lane = WAYS > 1 ? threadIdx.x & 63 : threadIdx.x;
+    constexpr int kElems = 1024 / WAYS;
+    for (long long base = block * kElems; base < j.n; base += kElems * blocks) {
+        const long long at = base + 4 * lane;
         const int there = static_cast<int>(min(4ll, j.n - at));
         float s[4] = {}, v[4];
+        if (there > 0) {
 #pragma unroll 4
-        for (int p = 0; p < j.n_parts; ++p) {
-            load_some<4>(v, j.parts + p * j.n + at, there);
+            for (int p = way; p < j.n_parts; p += WAYS) {
+                load_some<4>(v, j.parts + p * j.n + at, there);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[k] += v[k];
+                for (int k = 0; k < 4; ++k) s[k] += v[k];
+            }
         }
-        if (accumulate) {
-            load_some<4>(v, j.out + at, there);
+        if constexpr (WAYS > 1) {
+            __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[k] += v[k];
+            for (int k = 0; k < 4; ++k) shared[way][4 * lane + k] = s[k];
+            __syncthreads();
+            if (way != 0) continue;
+#pragma unroll
+            for (int w = 1; w < WAYS; ++w)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] += shared[w][4 * lane + k];
         }
-        store_some<4>(j.out + at, s, there);
+        if (there > 0) {
+            if (accumulate) {
+                load_some<4>(v, j.out + at, there);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[k] += v[k];
+            }
+            store_some<4>(j.out + at, s, there);
+        }
     }
 }
 
 }  // namespace
 
+// The edge of a workgroup's square and the number of parts, by what a call would take (microseconds): a fixed time, the steps of a
+// workgroup, and the second launch where there are parts.  A workgroup of edge 256 has a compute unit to itself, two of edge 128 share
+// one.  Measured, a step takes 1.8 us (fp32: 2.5) with edge 256; with edge 128, which reads more for its products, 0.85 (1.25)
+// alone on its compute unit and 1.4 (1.95) beside another.  Examples (bf16, edge / parts): 256 x 2048 x 1000 10.3 us with 128 / 1, 17.3
+// with 256 / 1, 18.8 with 128 / 2; 2048 x 1024 x 1024 23 with 128 / 4, 30 with 256 / 8; 16384 x 1024 x 1024 54 with 256 / 16, 56
+// with 128 / 8; 16384 x 1024 x 4096 139 with 256 / 4, 200 with 128 / 2; 65536 x 64 x 64 21.5 with 128 / 128, 27.3 with 256 / 128.
 WeightSplit weight_split(int64_t rows, int64_t width, int64_t outputs, int dtype) {
-    WeightSplit s;
-    auto tiles_of = [&](int edge) { return ((outputs + edge - 1) / edge) * ((width + edge - 1) / edge); };
-    s.tile = 256;
-    const int64_t step = dtype == ADASUM_F32 ? 32 : 64, tiles = tiles_of(s.tile);
-    const int64_t steps = (rows + step - 1) / step;
-    int64_t parts = tiles > 0 ? 256 / tiles : 1;
-    if (parts > steps / 4) parts = steps / 4;
-    if (parts < 1) parts = 1;
-    s.steps = (steps + parts - 1) / parts;
-    s.parts = s.steps > 0 ? (steps + s.steps - 1) / s.steps : 1;
-    if (s.parts > 1) {
-        s.off_bias = align_up(static_cast<size_t>(s.parts) * outputs * width * 4, 256);
-        s.total = s.off_bias + static_cast<size_t>(s.parts) * outputs * 4;
+    const bool f32 = dtype == ADASUM_F32;
+    const int64_t step = f32 ? 32 : 64, steps = (rows + step - 1) / step;
+    static constexpr int kCounts[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16, 20, 24, 32, 48, 64, 96, 128, 192, 256};
+    WeightSplit best;
+    double least = 0;
+    for (int tile : {256, 128}) {
+        const int64_t tiles = ((outputs + tile - 1) / tile) * ((width + tile - 1) / tile);
+        for (int count : kCounts) {
+            if (count > 1 && count > steps) break;
+            const int64_t each = (steps + count - 1) / count, parts = each > 0 ? (steps + each - 1) / each : 1, groups = tiles * parts;
+            const double a_step = tile == 256 ? (f32 ? 2.5 : 1.8) : groups <= 256 ? (f32 ? 1.25 : 0.85) : (f32 ? 1.95 : 1.4);
+            const int64_t slots = tile == 256 || groups <= 256 ? 256 : 512;
+            double time = (tile == 256 ? 12.0 : 8.6) + static_cast<double>((groups + slots - 1) / slots) * static_cast<double>(each) * a_step;
+            if (parts > 1) time += 5.0 + 0.02 * static_cast<double>(parts) + 0.9e-6 * static_cast<double>(parts) * static_cast<double>(outputs * width);
+            if (best.tile == 0 || time < least) {
+                least = time;
+                best.tile = tile;
+                best.parts = parts;
+                best.steps = each;
+            }
+        }
     }
-    return s;
+    if (best.parts > 1) {
+        best.off_bias = align_up(static_cast<size_t>(best.parts) * outputs * width * 4, 256);
+        best.total = best.off_bias + static_cast<size_t>(best.parts) * outputs * 4;
+    }
+    return best;
 }
 
 int launch_weight_grad(const WeightGrad& g, void* stream) {
@@ -442,17 +492,20 @@ int launch_weight_grad(const WeightGrad& g, void* stream) {
             const int64_t tiles_o = (g.outputs + w.tile - 1) / w.tile, tiles_i = g.x.width > 0 ? (g.x.width + w.tile - 1) / w.tile : 1;
             const bool wide = w.tile == 256;
             const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
+            const int threads = wide ? GradShape<D, 256>::threads : GradShape<D, 128>::threads;
             const auto kernel = wide ? weight_grad_kernel<D, T, 256> : weight_grad_kernel<D, T, 128>;
             int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
             if (rc != 0) return rc;
-            rc = launch(kernel, tiles_o * tiles_i * w.parts, 1, 256, lds, stream, reinterpret_cast<const signed char*>(g.x.q),
+            rc = launch(kernel, tiles_o * tiles_i * w.parts, 1, threads, lds, stream, reinterpret_cast<const signed char*>(g.x.q),
                         reinterpret_cast<const signed char*>(g.x.e), g.x.rows, g.x.width, g.x.pitch, static_cast<const D*>(g.dy), g.dy_stride,
                         g.outputs, grad, g.accumulate, parts, w.steps, tiles_o, tiles_i, bias, bias_parts);
             if (rc != 0 || parts == nullptr) return rc;
             const Joined<T> weights{parts, static_cast<int>(w.parts), g.outputs * g.x.width, grad};
             const Joined<T> sums{bias_parts, static_cast<int>(w.parts), bias != nullptr ? g.outputs : 0, bias};
-            const int64_t groups = at_most_groups((weights.n + 1023) / 1024);
-            return launch(join_parts_kernel<T>, groups + (sums.n + 1023) / 1024, 1, 256, 0, stream, weights, groups, sums, g.accumulate);
+            const bool few = w.parts >= 8 && weights.n < (1 << 19);
+            const int64_t elems = few ? 256 : 1024, groups = at_most_groups((weights.n + elems - 1) / elems);
+            return launch(few ? join_parts_kernel<T, 4> : join_parts_kernel<T, 1>, groups + (sums.n + elems - 1) / elems, 1, 256, 0, stream,
+                          weights, groups, sums, g.accumulate);
         }
     });
 }
