@@ -62,11 +62,21 @@ lookup_kernel(const T* __restrict__ table, long long rows, int width, Ids ids, t
 // waits for another.  Workgroups behind the last one clear the table meanwhile.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortBatch = 16;                   // ids a lane has in flight
 constexpr int kClearBytes = 64 * kSortThreads;   // per workgroup
 
+// An id as a number that is below 2^31 - 65536 for every row there may be, and far above for ids that name none.
+__device__ __forceinline__ unsigned row_of(const Ids& ids, int64_t t) {
+    if (ids.wide) {
+        const u32x2 id = static_cast<const u32x2*>(ids.p)[t];
+        return id.y == 0 ? id.x : ~0u;
+    }
+    return static_cast<const unsigned*>(ids.p)[t];
+}
+
 __global__ void __launch_bounds__(kSortThreads)
-sort_kernel(Ids ids, int rows, int per_group, int groups, int* __restrict__ total, int* __restrict__ place, int* __restrict__ row,
-            char* __restrict__ clear, long long clear_bytes) {
+sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restrict__ totals, int* __restrict__ place,
+            int* __restrict__ row, char* __restrict__ clear, long long clear_bytes) {
     extern __shared__ int counts[];   // [wave][row of the range], then what the scan needs
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (static_cast<int>(blockIdx.x) >= groups) {
@@ -85,21 +95,30 @@ sort_kernel(Ids ids, int rows, int per_group, int groups, int* __restrict__ tota
         }
         return;
     }
-    const long long lo = static_cast<long long>(blockIdx.x) * per_group, hi = min(lo + per_group, static_cast<long long>(rows));
-    const int mine = static_cast<int>(hi - lo);
+    const unsigned lo = blockIdx.x * per_group, mine = min(per_group, rows - lo);
     int* const scan = counts + kSortWaves * per_group;
-    for (int i = threadIdx.x; i < kSortWaves * per_group; i += kSortThreads) counts[i] = 0;
+    for (unsigned i = threadIdx.x; i < kSortWaves * per_group; i += kSortThreads) counts[i] = 0;
     __syncthreads();
     const int64_t segment = ((ids.n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const int64_t begin = min(segment * wave, ids.n), end = min(begin + segment, ids.n);
     // (volatile: the lanes of a wave read what one of them has written)
     volatile int* const my_counts = counts + wave * per_group;
+    unsigned batch[kSortBatch];
+    auto load = [&](int64_t from) {
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k) {
+            const int64_t t = from + 64 * k + lane;
+            batch[k] = t < end ? row_of(ids, t) : ~0u;
+        }
+    };
     int below = 0;
-#pragma unroll 4
-    for (int64_t t = begin + lane; t < end; t += 64) {
-        const long long id = id_at(ids, t);
-        below += id >= 0 && id < lo;
-        if (id >= lo && id < hi) atomicAdd(counts + wave * per_group + static_cast<int>(id - lo), 1);
+    for (int64_t from = begin; from < end; from += 64 * kSortBatch) {
+        load(from);
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k) {
+            below += batch[k] < lo;
+            if (batch[k] - lo < mine) atomicAdd(counts + wave * per_group + (batch[k] - lo), 1);
+        }
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) below += __shfl_xor(below, m, 64);
@@ -108,7 +127,7 @@ sort_kernel(Ids ids, int rows, int per_group, int groups, int* __restrict__ tota
     int base = 0;
     for (int w = 0; w < kSortWaves; ++w) base += scan[w];
     // one row of the range per thread (per_group is at most kSortThreads): its tokens, and those of the rows before it
-    const int r = threadIdx.x;
+    const unsigned r = threadIdx.x;
     int sum = 0;
     if (r < mine)
         for (int w = 0; w < kSortWaves; ++w) sum += counts[w * per_group + r];
@@ -129,25 +148,31 @@ sort_kernel(Ids ids, int rows, int per_group, int groups, int* __restrict__ tota
             counts[w * per_group + r] = at;
             at += n;
         }
-    if (blockIdx.x == static_cast<unsigned>(groups) - 1 && r == mine - 1) *total = at;
+    if (blockIdx.x == static_cast<unsigned>(groups) - 1 && r == mine - 1) {
+        totals[0] = at;
+        totals[1] = 0;   // runs that sum_kernel lists
+    }
     __syncthreads();
-    for (int64_t t0 = begin; t0 < end; t0 += 64) {
-        const int64_t t = t0 + lane;
-        const long long id = t < end ? id_at(ids, t) : -1;
-        const int bin = id >= lo && id < hi ? static_cast<int>(id - lo) : -1;
-        unsigned long long left = __ballot(bin >= 0);
-        while (left != 0) {
-            const int leader = __ffsll(left) - 1;
-            const int b = __shfl(bin, leader, 64);
-            const unsigned long long same = __ballot(bin == b);
-            if (bin == b) {
-                const int p = my_counts[b] + __popcll(same & ((1ull << lane) - 1));
-                place[p] = static_cast<int>(t);
-                row[p] = static_cast<int>(id);
+    const bool kept = end - begin <= 64 * kSortBatch;   // the ids are in registers still
+    for (int64_t from = begin; from < end; from += 64 * kSortBatch) {
+        if (!kept) load(from);
+#pragma unroll
+        for (int k = 0; k < kSortBatch; ++k) {
+            const unsigned b_mine = batch[k] - lo;
+            unsigned long long left = __ballot(b_mine < mine);
+            while (left != 0) {
+                const int leader = __ffsll(left) - 1;
+                const unsigned b = __builtin_amdgcn_readlane(b_mine, leader);
+                const unsigned long long same = __ballot(b_mine == b);
+                if (b_mine == b) {
+                    const int p = my_counts[b] + __popcll(same & ((1ull << lane) - 1));
+                    place[p] = static_cast<int>(from) + 64 * k + lane;
+                    row[p] = static_cast<int>(batch[k]);
+                }
+                // (a wave's LDS operations are done in order: the reads above come before this write)
+                if (lane == leader) my_counts[b] = my_counts[b] + __popcll(same);
+                left &= ~same;
             }
-            // (a wave's LDS operations are done in order: the reads above come before this write)
-            if (lane == leader) my_counts[b] = my_counts[b] + __popcll(same);
-            left &= ~same;
         }
     }
 }
@@ -177,12 +202,14 @@ __device__ __forceinline__ Window look(const int* row, int total, int64_t chunk,
 // Whether the run that starts at index a (a < 64) has more than kRun tokens.
 __device__ __forceinline__ bool is_long(const Window& w, int a) { return w.row_at(a + kRun) == w.row_at(a); }
 
-// One wave: chunk `chunk`, the elements of `slice`.
-template <typename D, typename T>
+// One wave: chunk `chunk`, the elements of `slice`; FULL: every lane's G elements exist.  `longs`: a count, then the chunks in which a
+// run of more than kRun tokens starts, in no certain order.
+constexpr int kBatch = 8;   // rows of dy in flight, twice
+template <typename D, typename T, bool FULL, bool ADD>
 __device__ __forceinline__ void
 sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long long dy_stride, int width, int total,
-          const int* __restrict__ place, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, int accumulate,
-          typename Traits<D>::acc_t* __restrict__ parts) {
+          const int* __restrict__ place, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
+          typename Traits<D>::acc_t* __restrict__ parts, int* __restrict__ longs, int* __restrict__ listed) {
     typedef typename Traits<D>::acc_t A;
     constexpr int G = Traits<D>::VEC;
     static_assert(kRun == 32, "the window of a chunk is 96 places");
@@ -210,44 +237,51 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
         open = is_long(w, kRun + 31 - __builtin_clz(starts));
         // (not long: the next run, or the end of the tokens, is in the window)
         if (!open && there == kRun) until = 64 + __builtin_ctz(w.later | 0x80000000u);
+        if (open && slice == 0 && lane == 0) listed[atomicAdd(longs, 1)] = static_cast<int>(chunk);
     }
     const int at = (slice * 64 + lane) * G;
-    const int have = width - at;
+    const int have = FULL ? G : width - at;
+    auto ends_at = [&](int i) { return i + 1 == until || (i + 1 < 64 ? (w.start >> (i + 1)) & 1 : (w.later >> (i + 1 - 64)) & 1); };
+    auto goes_on = [&](int i) { return open && i + 1 == until; };
     A sum[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) sum[i] = A(0);
     bool first_run = carried;
-    for (int i0 = from; i0 < until; i0 += 8) {
-        A v[8][G];
+    Granule<D, G> v[2][kBatch];
+    Granule<T, G> old[2][ADD ? kBatch : 1];
+    auto load = [&](int set, int i0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (i0 + k < until && have > 0) {
+        for (int k = 0; k < kBatch; ++k)
+            if (i0 + k < until) {
                 const int t = __builtin_amdgcn_readlane(token, i0 + k - kRun);
-                load_some<G>(v[k], dy + static_cast<long long>(t) * dy_stride + at, have);
+                load_part<FULL>(v[set][k], dy + static_cast<long long>(t) * dy_stride + at, have);
+                if constexpr (ADD)
+                    if (ends_at(i0 + k)) load_part<FULL>(old[set][k], grad + static_cast<long long>(w.row_at(i0 + k)) * width + at, have);
             }
+    };
+    auto take = [&](int set, int i0) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kBatch; ++k) {
             const int i = i0 + k;
-            if (i < until && have > 0) {
+            if (i < until) {
+                A x[G];
+                unpack(v[set][k], x);
 #pragma unroll
-                for (int j = 0; j < G; ++j) sum[j] += v[k][j];
-                const bool ends = i + 1 == until || (i + 1 < 64 ? (w.start >> (i + 1)) & 1 : (w.later >> (i + 1 - 64)) & 1);
-                if (ends) {
-                    const bool goes_on = open && i + 1 == until;
-                    if (first_run || goes_on) {
+                for (int j = 0; j < G; ++j) sum[j] += x[j];
+                if (ends_at(i)) {
+                    if (first_run || goes_on(i)) {
                         // (the one that comes from before and goes on lies in the first place)
-                        store_some<G>(parts + (2 * chunk + (first_run ? 0 : 1)) * width + at, sum, have);
+                        store_part<FULL, G>(parts + (2 * chunk + (first_run ? 0 : 1)) * width + at, sum, have);
                     } else {
-                        T* const to = grad + static_cast<long long>(w.row_at(i)) * width + at;
 #pragma unroll
                         for (int j = 0; j < G; ++j) sum[j] *= scale;
-                        if (accumulate) {
-                            A old[G];
-                            load_some<G>(old, to, have);
+                        if constexpr (ADD) {
+                            A o[G];
+                            unpack(old[set][k], o);
 #pragma unroll
-                            for (int j = 0; j < G; ++j) sum[j] += old[j];
+                            for (int j = 0; j < G; ++j) sum[j] += o[j];
                         }
-                        store_some<G>(to, sum, have);
+                        store_part<FULL, G>(grad + static_cast<long long>(w.row_at(i)) * width + at, sum, have);
                     }
 #pragma unroll
                     for (int j = 0; j < G; ++j) sum[j] = A(0);
@@ -255,81 +289,85 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
                 }
             }
         }
+    };
+    load(0, from);
+    for (int i0 = from; i0 < until; i0 += 2 * kBatch) {
+        load(1, i0 + kBatch);
+        take(0, i0);
+        load(0, i0 + 2 * kBatch);
+        take(1, i0 + kBatch);
     }
 }
 
-template <typename D, typename T>
+template <typename D, typename T, bool ADD>
 __global__ void __launch_bounds__(256)
-sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, const int* __restrict__ total_p, const int* __restrict__ place,
-           const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, int accumulate,
-           typename Traits<D>::acc_t* __restrict__ parts, int slices, long long n_chunks) {
+sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, int* __restrict__ totals, const int* __restrict__ place,
+           const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, typename Traits<D>::acc_t* __restrict__ parts,
+           int* __restrict__ listed, int slices, long long n_chunks) {
     const int lane = threadIdx.x & 63;
-    const int total = *total_p;
+    const int total = totals[0];
     const long long units = min(n_chunks, (static_cast<long long>(total) + kRun - 1) / kRun) * slices;
-    for (long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += 4ll * gridDim.x)
-        sum_chunk<D, T>(unit / slices, static_cast<int>(unit % slices), lane, dy, dy_stride, width, total, place, row, scale, grad,
-                        accumulate, parts);
+    for (long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += 4ll * gridDim.x) {
+        const int slice = static_cast<int>(unit % slices);
+        if ((slice + 1) * 64 * Traits<D>::VEC <= width)
+            sum_chunk<D, T, true, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
+        else
+            sum_chunk<D, T, false, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
+    }
 }
-// The parts of long runs, four waves of a workgroup taking a quarter of a run's chunks each.
+
+// The parts of long runs.  A compute unit alone reads little, so a workgroup takes 64 elements only: sixteen groups of sixteen lanes
+// share a run's chunks, four elements a lane.
 template <typename D, typename T>
 __global__ void __launch_bounds__(256)
-join_kernel(int width, const int* __restrict__ total_p, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
-            int accumulate, const typename Traits<D>::acc_t* __restrict__ parts, int slices) {
+join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
+            int accumulate, const typename Traits<D>::acc_t* __restrict__ parts, const int* __restrict__ listed) {
     typedef typename Traits<D>::acc_t A;
-    constexpr int G = Traits<D>::VEC;
-    __shared__ double half[4][64 * G];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int total = *total_p;
-    const long long units = static_cast<long long>(total) / kRun * slices;   // (a long run starts in a chunk that is full)
+    __shared__ double shared[16][64];
+    const int lane = threadIdx.x & 63, group = threadIdx.x >> 4, col = 4 * (threadIdx.x & 15);
+    const int total = totals[0];
+    const long long slices = (width + 63) / 64, units = totals[1] * slices, n_chunks = (static_cast<long long>(total) + kRun - 1) / kRun;
     for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const long long chunk = unit / slices;
-    const int slice = static_cast<int>(unit - chunk * slices);
-    const Window w = look(row, total, chunk, lane);
-    const unsigned starts = static_cast<unsigned>(w.start >> 32);
-    if (starts == 0) continue;
-    const int a = kRun + 31 - __builtin_clz(starts);
-    if (!is_long(w, a)) continue;
-    const int key = w.row_at(a);
-    // the last chunk that begins with this row, 64 chunks a look
-    long long last = chunk + 1;
-    for (;;) {
-        const long long c = last + 1 + lane;
-        const unsigned long long same = __ballot(c * kRun < total && row[c * kRun < total ? c * kRun : 0] == key);
-        const int run = same == ~0ull ? 64 : __ffsll(~same) - 1;
-        last += run;
-        if (run < 64) break;
-    }
-    const int at = (slice * 64 + lane) * G, have = width - at;
-    const long long n = last - chunk + 1;
-    double sum[G];
-#pragma unroll
-    for (int j = 0; j < G; ++j) sum[j] = 0;
-    if (have > 0) {
-#pragma unroll 4
-        for (long long c = n * wave / 4; c < n * (wave + 1) / 4; ++c) {
-            A v[G];
-            load_some<G>(v, parts + (2 * (chunk + c) + (c == 0 ? 1 : 0)) * width + at, have);
-#pragma unroll
-            for (int j = 0; j < G; ++j) sum[j] += v[j];
+        const long long chunk = listed[unit / slices];
+        const Window w = look(row, total, chunk, lane);
+        const int key = w.row_at(kRun + 31 - __builtin_clz(static_cast<unsigned>(w.start >> 32)));
+        // the last chunk that begins with this row (the next one does): the chunks up to `lo` do, those from `hi` on do not
+        long long lo = chunk + 1, hi = n_chunks;
+        while (hi - lo > 1) {
+            const long long step = (hi - lo + 63) / 64, c = lo + (lane + 1) * step;
+            const unsigned long long same = __ballot(c < hi && row[c < hi ? c * kRun : 0] == key);
+            const int yes = same == ~0ull ? 64 : __ffsll(~same) - 1;
+            const long long next = lo + yes * step;
+            hi = min(hi, next + step);
+            lo = next;
         }
-    }
-    __syncthreads();   // (all have read what the last round left there)
+        const int at = static_cast<int>(unit % slices) * 64 + col, have = width - at;
+        const long long n = lo - chunk + 1;
+        double sum[4] = {};
+        if (have > 0) {
+#pragma unroll 8
+            for (long long c = group; c < n; c += 16) {
+                A v[4];
+                load_some<4>(v, parts + (2 * (chunk + c) + (c == 0 ? 1 : 0)) * width + at, have);
 #pragma unroll
-    for (int j = 0; j < G; ++j) half[wave][j * 64 + lane] = sum[j];
-    __syncthreads();
-    if (wave != 0 || have <= 0) continue;
-    T* const to = grad + static_cast<long long>(key) * width + at;
-    A v[G], old[G];
-    if (accumulate) load_some<G>(old, to, have);
+                for (int j = 0; j < 4; ++j) sum[j] += v[j];
+            }
+        }
+        __syncthreads();   // (all have read what the last round left there)
 #pragma unroll
-    for (int j = 0; j < G; ++j) {
-        double s = sum[j] + half[1][j * 64 + lane];
-        s += half[2][j * 64 + lane];
-        s += half[3][j * 64 + lane];
-        s *= scale;
-        v[j] = static_cast<A>(accumulate ? s + old[j] : s);
-    }
-    store_some<G>(to, v, have);
+        for (int j = 0; j < 4; ++j) shared[group][col + j] = sum[j];
+        __syncthreads();
+        if (threadIdx.x < 64) {
+            const int e = static_cast<int>(unit % slices) * 64 + lane;
+            if (e < width) {
+                double s = 0;
+#pragma unroll
+                for (int g = 0; g < 16; ++g) s += shared[g][lane];
+                s *= scale;
+                T* const to = grad + static_cast<long long>(key) * width + e;
+                store_elem(to, static_cast<A>(accumulate ? s + load_elem(to) : s));
+            }
+        }
     }
 }
 
@@ -343,7 +381,8 @@ int slices_of(int64_t width, int dtype) {
 EmbeddingLayout embedding_layout(int64_t width, int64_t n_ids, int dtype) {
     EmbeddingLayout l;
     l.chunks = (n_ids + kRun - 1) / kRun;
-    l.off_place = 256;
+    l.off_listed = 256;
+    l.off_place = align_up(l.off_listed + 4 * static_cast<size_t>(l.chunks), 256);
     l.off_row = align_up(l.off_place + 4 * static_cast<size_t>(n_ids), 256);
     l.off_parts = align_up(l.off_row + 4 * static_cast<size_t>(n_ids), 256);
     l.total = l.off_parts + static_cast<size_t>(l.chunks) * 2 * width * (dtype == ADASUM_F64 ? 8 : 4);
@@ -369,7 +408,8 @@ int launch_lookup(int dtype, int out_dtype, const void* table, int64_t rows, int
 
 int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
     const int64_t clear_bytes = g.accumulate ? 0 : g.rows * g.width * elem_bytes(g.grad_dtype);
-    int* const total = reinterpret_cast<int*>(g.ws + g.lay.off_total);
+    int* const totals = reinterpret_cast<int*>(g.ws + g.lay.off_totals);
+    int* const listed = reinterpret_cast<int*>(g.ws + g.lay.off_listed);
     int* const place = reinterpret_cast<int*>(g.ws + g.lay.off_place);
     int* const row = reinterpret_cast<int*>(g.ws + g.lay.off_row);
     const int64_t per_group = sort_rows(g.rows);
@@ -377,7 +417,7 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
     const int64_t clearing = at_most_groups((clear_bytes + kClearBytes - 1) / kClearBytes);
     if (groups + clearing == 0) return 0;
     const size_t lds = sizeof(int) * (static_cast<size_t>(kSortWaves) * per_group + kSortWaves);
-    const int rc = launch(sort_kernel, groups + clearing, 1, kSortThreads, lds, stream, g.ids, g.rows, per_group, groups, total, place, row,
+    const int rc = launch(sort_kernel, groups + clearing, 1, kSortThreads, lds, stream, g.ids, g.rows, per_group, groups, totals, place, row,
                           static_cast<char*>(g.grad), clear_bytes);
     if (rc != 0 || g.ids.n == 0) return rc;
     return with_types(g.dtype, g.grad_dtype, [&](auto d, auto t) -> int {
@@ -387,11 +427,13 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
         const int slices = slices_of(g.width, g.dtype);
         const int64_t units = g.lay.chunks * slices;
         A* const parts = reinterpret_cast<A*>(g.ws + g.lay.off_parts);
-        const int rc2 = launch(sum_kernel<D, T>, at_most_groups((units + 3) / 4), 1, 256, 0, stream, static_cast<const D*>(g.dy), g.dy_stride,
-                               g.width, total, place, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, slices, g.lay.chunks);
-        if (rc2 != 0) return rc2;
-        return launch(join_kernel<D, T>, at_most_groups(units), 1, 256, 0, stream, g.width, total, row, g.scale, static_cast<T*>(g.grad),
-                      g.accumulate, parts, slices);
+        const int rc2 = launch(g.accumulate ? sum_kernel<D, T, true> : sum_kernel<D, T, false>, at_most_groups((units + 3) / 4), 1, 256, 0, stream,
+                               static_cast<const D*>(g.dy), g.dy_stride, g.width, totals, place, row, g.scale, static_cast<T*>(g.grad), parts,
+                               listed, slices, g.lay.chunks);
+        if (rc2 != 0 || g.ids.n <= kRun) return rc2;   // (so few tokens make no long run)
+        const int64_t most = (g.ids.n / (kRun + 1)) * ((g.width + 63) / 64);
+        return launch(join_kernel<D, T>, most < 1024 ? most : 1024, 1, 256, 0, stream, g.width, totals, row, g.scale,
+                      static_cast<T*>(g.grad), g.accumulate, parts, listed);
     });
 }
 

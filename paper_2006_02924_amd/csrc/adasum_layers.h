@@ -40,7 +40,8 @@ inline int64_t sort_rows(int64_t rows) {
 // Workspace of the table's gradient (byte offsets).
 struct EmbeddingLayout {
     int64_t chunks = 0;
-    size_t off_total = 0;     // int32: tokens whose id names a row
+    size_t off_totals = 0;    // int32: tokens whose id names a row; runs of more than kRun tokens
+    size_t off_listed = 0;    // int32 [chunk]: the chunks in which those start
     size_t off_place = 0;     // int32 [n]: tokens in the order of their ids
     size_t off_row = 0;       // int32 [n]: their ids
     size_t off_parts = 0;     // [chunk][2][width]: sums of the run that comes from the chunk before, and of the one that goes on into the next

@@ -116,6 +116,35 @@ __device__ __forceinline__ void store_some(T* p, const A (&v)[G], int there) {
     }
 }
 
+// The same where FULL says that all are there, and as raw words: the values are taken out where they are used.
+template <bool FULL, typename T, int G>
+__device__ __forceinline__ void load_part(Granule<T, G>& r, const T* p, int there) {
+    if (FULL || there >= G) {
+        load_any(r, p);
+    } else {
+#pragma unroll
+        for (int w = 0; w < Granule<T, G>::NW; ++w) r.w[w] = 0;
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (i < there) {
+                if constexpr (sizeof(T) == 2) {
+                    r.w[i / 2] |= static_cast<unsigned>(p[i].v) << (16 * (i & 1));
+                } else if constexpr (sizeof(T) == 4) {
+                    r.w[i] = __float_as_uint(p[i]);
+                } else {
+                    const long long b = __double_as_longlong(p[i]);
+                    r.w[2 * i] = static_cast<unsigned>(b);
+                    r.w[2 * i + 1] = static_cast<unsigned>(b >> 32);
+                }
+            }
+    }
+}
+template <bool FULL, int G, typename T, typename A>
+__device__ __forceinline__ void store_part(T* p, const A (&v)[G], int there) {
+    if constexpr (FULL) store_any<G>(p, v);
+    else store_some<G>(p, v, there);
+}
+
 // Division of numbers below 2^31 by a fixed one, by a multiplication: q = (n * m) >> (32 + s) with
 // m = ceil(2^(32 + s) / d), 2^s >= d; the product is taken with a 33-bit m (its top bit is always set).
 struct Divider {
