@@ -65,6 +65,20 @@ constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortBatch = 16;                   // ids a lane has in flight
 constexpr int kClearBytes = 64 * kSortThreads;   // per workgroup
 
+// Zeros over the workgroups' share of the table.
+__device__ __forceinline__ void clear_table(long long block, long long blocks, char* __restrict__ clear, long long clear_bytes) {
+    const unsigned zero[4] = {0, 0, 0, 0};
+    for (long long from = block * kClearBytes; from < clear_bytes; from += blocks * kClearBytes)
+        for (int k = threadIdx.x; k < kClearBytes / 16; k += static_cast<int>(blockDim.x)) {
+            const long long at = from + 16ll * k;
+            if (at + 16 <= clear_bytes) {
+                store_words_any(clear + at, zero);
+            } else {
+                for (long long b = at; b < clear_bytes; b += 2) *reinterpret_cast<unsigned short*>(clear + b) = 0;
+            }
+        }
+}
+
 // An id as a number that is below 2^31 - 65536 for every row there may be, and far above for ids that name none.
 __device__ __forceinline__ unsigned row_of(const Ids& ids, int64_t t) {
     if (ids.wide) {
@@ -80,19 +94,7 @@ sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restr
     extern __shared__ int counts[];   // [wave][row of the range], then what the scan needs
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (static_cast<int>(blockIdx.x) >= groups) {
-        const unsigned zero[4] = {0, 0, 0, 0};
-        for (long long from = static_cast<long long>(blockIdx.x - groups) * kClearBytes; from < clear_bytes;
-             from += static_cast<long long>(gridDim.x - groups) * kClearBytes) {
-#pragma unroll
-            for (int k = 0; k < kClearBytes / 16 / kSortThreads; ++k) {
-                const long long at = from + 16ll * (k * kSortThreads + static_cast<int>(threadIdx.x));
-                if (at + 16 <= clear_bytes) {
-                    store_words_any(clear + at, zero);
-                } else {
-                    for (long long b = at; b < clear_bytes; b += 2) *reinterpret_cast<unsigned short*>(clear + b) = 0;
-                }
-            }
-        }
+        clear_table(blockIdx.x - groups, gridDim.x - groups, clear, clear_bytes);
         return;
     }
     const unsigned lo = blockIdx.x * per_group, mine = min(per_group, rows - lo);
@@ -175,6 +177,250 @@ sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restr
             }
         }
     }
+}
+
+// ---- sorting many tokens -------------------------------------------------------------
+//
+// Where the tokens are many, reading all of them in every workgroup costs more than a launch.  The rows are cut into kSortGroups equal
+// ranges.  First, workgroups of kPartTokens tokens each sort theirs by range, for themselves, and write down where each range
+// begins; what lies below a range in all of them together is where its list starts.  Then one workgroup per range gathers its tokens,
+// in order, and sorts them by row.
+//
+// Both sort in registers: a wave takes 64 tokens at a time, finds by one vote per bit which lanes have the same key, and so ranks them
+// behind those of the same key that it has seen before.
+constexpr int kRowBits = 10;
+static_assert(kGatherRows == 1 << kRowBits && kGatherRows <= kSortThreads, "a range's rows have as many bits, and a lane each");
+constexpr int kPartThreads = 512, kPartWaves = kPartThreads / 64, kPartBatch = kPartTokens / kPartThreads;
+constexpr int kGatherBatch = 8;
+constexpr int kGatherTokens = kSortThreads * kGatherBatch;   // tokens of a range that are sorted at a time
+
+// The lanes with the same key of BITS bits, among those of `valid`.
+template <int BITS>
+__device__ __forceinline__ unsigned long long same_key(unsigned key, unsigned long long valid, int bits) {
+    unsigned long long same = valid;
+#pragma unroll
+    for (int b = 0; b < BITS; ++b) {
+        if (b >= bits) break;
+        const bool one = (key >> b) & 1;
+        const unsigned long long ones = __ballot(one);
+        same &= one ? ones : ~ones;
+    }
+    return same;
+}
+
+// Sums over the lanes before this one, of every lane's value, across a workgroup of WAVES waves; the sum of all comes back in `all`.
+template <int WAVES>
+__device__ __forceinline__ int scan_before(int v, int* shared, int& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int upto = v;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const int before = __shfl_up(upto, m, 64);
+        if (lane >= m) upto += before;
+    }
+    __syncthreads();
+    if (lane == 63) shared[wave] = upto;
+    __syncthreads();
+    int sum = upto - v;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) sum += shared[w];
+        all += shared[w];
+    }
+    return sum;
+}
+
+// The tokens of each part by range: part_place / part_row[part * kPartTokens + i], and begins[range][part], the index of the part's
+// first token of that range (range kSortGroups: its tokens that name a row).
+__global__ void __launch_bounds__(kPartThreads)
+part_kernel(Ids ids, unsigned rows, Divider per_group, int n_parts, int* __restrict__ begins, int* __restrict__ part_place,
+            int* __restrict__ part_row, char* __restrict__ clear, long long clear_bytes) {
+    __shared__ int counts[kPartWaves][kSortGroups];
+    __shared__ int first[kSortGroups];
+    __shared__ int scan[kPartWaves];
+    if (static_cast<int>(blockIdx.x) >= n_parts) {
+        clear_table(blockIdx.x - n_parts, gridDim.x - n_parts, clear, clear_bytes);
+        return;
+    }
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int64_t from = static_cast<int64_t>(blockIdx.x) * kPartTokens + wave * (64 * kPartBatch) + lane;
+    unsigned id[kPartBatch];
+    int rank[kPartBatch], group[kPartBatch];
+#pragma unroll
+    for (int k = 0; k < kPartBatch; ++k) id[k] = from + 64 * k < ids.n ? row_of(ids, from + 64 * k) : ~0u;
+    for (int i = threadIdx.x; i < kPartWaves * kSortGroups; i += kPartThreads) (&counts[0][0])[i] = 0;
+    __syncthreads();
+    // (volatile: the lanes of a wave read what others of it have written)
+    volatile int* const mine = counts[wave];
+#pragma unroll
+    for (int k = 0; k < kPartBatch; ++k) {
+        const bool valid = id[k] < rows;
+        group[k] = valid ? static_cast<int>(divide(id[k], per_group)) : 0;
+        const unsigned long long same = same_key<8>(group[k], __ballot(valid), 8);
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        const int seen = mine[group[k]];
+        rank[k] = valid ? seen + before : -1;
+        if (valid && before == 0) mine[group[k]] = seen + __popcll(same);
+    }
+    __syncthreads();
+    static_assert(kSortGroups <= kPartThreads, "one range per lane");
+    const int r = threadIdx.x;
+    int sum = 0;
+    if (r < kSortGroups)
+        for (int w = 0; w < kPartWaves; ++w) {
+            const int n = counts[w][r];
+            counts[w][r] = sum;
+            sum += n;
+        }
+    int all = 0;
+    const int start = scan_before<kPartWaves>(sum, scan, all);
+    if (r < kSortGroups) {
+        first[r] = start;
+        begins[static_cast<int64_t>(r) * n_parts + blockIdx.x] = start;
+    }
+    if (r == 0) begins[static_cast<int64_t>(kSortGroups) * n_parts + blockIdx.x] = all;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPartBatch; ++k)
+        if (rank[k] >= 0) {
+            const int64_t to = static_cast<int64_t>(blockIdx.x) * kPartTokens + first[group[k]] + counts[wave][group[k]] + rank[k];
+            part_place[to] = static_cast<int>(from + 64 * k);
+            part_row[to] = static_cast<int>(id[k]);
+        }
+}
+
+// Range blockIdx.x: gathers its tokens from the parts and sorts them by row.
+__global__ void __launch_bounds__(kSortThreads)
+gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, const int* __restrict__ begins, const int* __restrict__ part_place,
+              const int* __restrict__ part_row, int* __restrict__ totals, int* __restrict__ place, int* __restrict__ row,
+              char* __restrict__ clear, long long clear_bytes) {
+    if (blockIdx.x >= kSortGroups) {
+        clear_table(blockIdx.x - kSortGroups, gridDim.x - kSortGroups, clear, clear_bytes);
+        return;
+    }
+    extern __shared__ int counts[];                 // [wave][row of the range], then [row]: where the row's next token goes
+    __shared__ int length[kSortThreads];            // of the parts in hand: tokens of this range before them
+    __shared__ int source[kSortThreads];            // where theirs begin
+    __shared__ int scan[kSortWaves];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const unsigned lo = blockIdx.x * per_group, mine_rows = lo < rows ? min(per_group, rows - lo) : 0;
+    const int* const begin_here = begins + static_cast<int64_t>(blockIdx.x) * n_parts;
+    const int* const begin_next = begin_here + n_parts;
+    int* const next = counts + kSortWaves * per_group;
+    // (volatile: the lanes of a wave read what others of it have written)
+    volatile int* const mine = counts + wave * per_group;
+    // tokens of the ranges before this one, and of this one
+    int below = 0, here = 0;
+    for (int p = threadIdx.x; p < n_parts; p += kSortThreads) {
+        below += begin_here[p];
+        here += begin_next[p] - begin_here[p];
+    }
+    int all_below = 0, all_here = 0;
+    scan_before<kSortWaves>(below, scan, all_below);
+    scan_before<kSortWaves>(here, scan, all_here);
+    if (blockIdx.x == kSortGroups - 1 && threadIdx.x == 0) {
+        totals[0] = all_below + all_here;
+        totals[1] = 0;   // runs that sum_kernel lists
+    }
+    if (all_here == 0) return;
+    for (unsigned r = threadIdx.x; r < per_group; r += kSortThreads) next[r] = 0;
+    int token[kGatherBatch], rank[kGatherBatch];
+    unsigned key[kGatherBatch];
+    // f() for every kGatherTokens tokens of the range, in order: then a wave has consecutive ones, 64 at a time
+    auto every = [&](auto&& f) {
+        for (int p0 = 0; p0 < n_parts; p0 += kSortThreads) {
+            const int p = p0 + static_cast<int>(threadIdx.x);
+            const int b = p < n_parts ? begin_here[p] : 0, n = p < n_parts ? begin_next[p] - b : 0;
+            int all = 0;
+            const int before = scan_before<kSortWaves>(n, scan, all);
+            length[threadIdx.x] = before;
+            source[threadIdx.x] = b;
+            __syncthreads();
+            for (int e0 = 0; e0 < all; e0 += kGatherTokens) {
+#pragma unroll
+                for (int k = 0; k < kGatherBatch; ++k) {
+                    const int e = e0 + wave * (64 * kGatherBatch) + 64 * k + lane;
+                    token[k] = -1;
+                    key[k] = 0;
+                    if (e < all) {
+                        // the part that has it: the last one that begins at or before it
+                        int q = 0;
+#pragma unroll
+                        for (int step = kSortThreads / 2; step > 0; step >>= 1)
+                            if (length[q + step] <= e) q += step;
+                        const int64_t from = static_cast<int64_t>(p0 + q) * kPartTokens + source[q] + (e - length[q]);
+                        token[k] = part_place[from];
+                        key[k] = static_cast<unsigned>(part_row[from]) - lo;
+                    }
+                }
+                f();
+            }
+            __syncthreads();
+        }
+    };
+    // from how many tokens the rows have to where theirs begin
+    auto rows_begin = [&] {
+        const unsigned r = threadIdx.x;
+        __syncthreads();
+        const int n = r < mine_rows ? next[r] : 0;
+        int all = 0;
+        const int before = scan_before<kSortWaves>(n, scan, all);
+        if (r < mine_rows) next[r] = all_below + before;
+        __syncthreads();
+    };
+    const bool once = all_here <= kGatherTokens && n_parts <= kSortThreads;
+    if (!once) {
+        // a hot range, whose tokens come in several batches: first count them all
+        every([&] {
+#pragma unroll
+            for (int k = 0; k < kGatherBatch; ++k) {
+                const unsigned long long valid = __ballot(token[k] >= 0);
+                if (valid == 0) continue;
+                const unsigned long long same = same_key<kRowBits>(key[k], valid, row_bits);
+                if (token[k] >= 0 && __popcll(same & ((1ull << lane) - 1)) == 0) atomicAdd(next + key[k], __popcll(same));
+            }
+        });
+        rows_begin();
+    }
+    every([&] {
+        for (unsigned i = threadIdx.x; i < kSortWaves * per_group; i += kSortThreads) counts[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kGatherBatch; ++k) {
+            const unsigned long long valid = __ballot(token[k] >= 0);
+            if (valid == 0) continue;
+            const unsigned long long same = same_key<kRowBits>(key[k], valid, row_bits);
+            const int before = __popcll(same & ((1ull << lane) - 1)), seen = mine[key[k]];
+            rank[k] = seen + before;
+            if (token[k] >= 0 && before == 0) mine[key[k]] = seen + __popcll(same);
+        }
+        __syncthreads();
+        const unsigned r = threadIdx.x;
+        if (once) {
+            if (r < mine_rows)
+                for (int w = 0; w < kSortWaves; ++w) next[r] += counts[w * per_group + r];
+            rows_begin();
+        }
+        if (r < mine_rows) {
+            int to = next[r];
+            for (int w = 0; w < kSortWaves; ++w) {
+                const int n = counts[w * per_group + r];
+                counts[w * per_group + r] = to;
+                to += n;
+            }
+            next[r] = to;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kGatherBatch; ++k)
+            if (token[k] >= 0) {
+                const int to = mine[key[k]] + rank[k];
+                place[to] = token[k];
+                row[to] = static_cast<int>(key[k] + lo);
+            }
+        __syncthreads();
+    });
 }
 
 // ---- sums over runs of equal ids ----------------------------------------------------
@@ -378,13 +624,21 @@ int slices_of(int64_t width, int dtype) {
 
 }  // namespace
 
-EmbeddingLayout embedding_layout(int64_t width, int64_t n_ids, int dtype) {
+EmbeddingLayout embedding_layout(int64_t rows, int64_t width, int64_t n_ids, int dtype) {
     EmbeddingLayout l;
     l.chunks = (n_ids + kRun - 1) / kRun;
     l.off_listed = 256;
     l.off_place = align_up(l.off_listed + 4 * static_cast<size_t>(l.chunks), 256);
     l.off_row = align_up(l.off_place + 4 * static_cast<size_t>(n_ids), 256);
-    l.off_parts = align_up(l.off_row + 4 * static_cast<size_t>(n_ids), 256);
+    size_t end = align_up(l.off_row + 4 * static_cast<size_t>(n_ids), 256);
+    if (in_parts(rows, n_ids)) {
+        const size_t n_parts = (static_cast<size_t>(n_ids) + kPartTokens - 1) / kPartTokens;
+        l.off_begins = end;
+        l.off_part_place = align_up(l.off_begins + 4 * (kSortGroups + 1) * n_parts, 256);
+        l.off_part_row = l.off_part_place + 4 * n_parts * kPartTokens;
+        end = l.off_part_row + 4 * n_parts * kPartTokens;
+    }
+    l.off_parts = end;
     l.total = l.off_parts + static_cast<size_t>(l.chunks) * 2 * width * (dtype == ADASUM_F64 ? 8 : 4);
     return l;
 }
@@ -412,13 +666,35 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
     int* const listed = reinterpret_cast<int*>(g.ws + g.lay.off_listed);
     int* const place = reinterpret_cast<int*>(g.ws + g.lay.off_place);
     int* const row = reinterpret_cast<int*>(g.ws + g.lay.off_row);
-    const int64_t per_group = sort_rows(g.rows);
-    const int64_t groups = g.ids.n == 0 ? 0 : (g.rows + per_group - 1) / per_group;
-    const int64_t clearing = at_most_groups((clear_bytes + kClearBytes - 1) / kClearBytes);
-    if (groups + clearing == 0) return 0;
-    const size_t lds = sizeof(int) * (static_cast<size_t>(kSortWaves) * per_group + kSortWaves);
-    const int rc = launch(sort_kernel, groups + clearing, 1, kSortThreads, lds, stream, g.ids, g.rows, per_group, groups, totals, place, row,
-                          static_cast<char*>(g.grad), clear_bytes);
+    char* const clear = static_cast<char*>(g.grad);
+    int rc = 0;
+    if (in_parts(g.rows, g.ids.n)) {
+        const int64_t per_group = (g.rows + kSortGroups - 1) / kSortGroups, n_parts = (g.ids.n + kPartTokens - 1) / kPartTokens;
+        int row_bits = 0;
+        while ((1 << row_bits) < per_group) ++row_bits;
+        int* const begins = reinterpret_cast<int*>(g.ws + g.lay.off_begins);
+        int* const part_place = reinterpret_cast<int*>(g.ws + g.lay.off_part_place);
+        int* const part_row = reinterpret_cast<int*>(g.ws + g.lay.off_part_row);
+        // each launch clears half of the table
+        const int64_t half = clear_bytes / 2 / kClearBytes * kClearBytes;
+        rc = launch(part_kernel, n_parts + at_most_groups((half + kClearBytes - 1) / kClearBytes), 1, kPartThreads, 0, stream, g.ids, g.rows,
+                    make_divider(static_cast<unsigned>(per_group)), n_parts, begins, part_place, part_row, clear, half);
+        if (rc != 0) return rc;
+        const size_t lds = sizeof(int) * (kSortWaves + 1) * per_group;
+        rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(gather_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                  static_cast<int>(sizeof(int) * (kSortWaves + 1) * kGatherRows)));
+        if (rc != 0) return rc;
+        rc = launch(gather_kernel, kSortGroups + at_most_groups((clear_bytes - half + kClearBytes - 1) / kClearBytes), 1, kSortThreads, lds, stream,
+                    g.rows, per_group, row_bits, n_parts, begins, part_place, part_row, totals, place, row, clear + half, clear_bytes - half);
+    } else {
+        const int64_t per_group = sort_rows(g.rows);
+        const int64_t groups = g.ids.n == 0 ? 0 : (g.rows + per_group - 1) / per_group;
+        const int64_t clearing = at_most_groups((clear_bytes + kClearBytes - 1) / kClearBytes);
+        if (groups + clearing == 0) return 0;
+        const size_t lds = sizeof(int) * (static_cast<size_t>(kSortWaves) * per_group + kSortWaves);
+        rc = launch(sort_kernel, groups + clearing, 1, kSortThreads, lds, stream, g.ids, g.rows, per_group, groups, totals, place, row, clear,
+                    clear_bytes);
+    }
     if (rc != 0 || g.ids.n == 0) return rc;
     return with_types(g.dtype, g.grad_dtype, [&](auto d, auto t) -> int {
         typedef decltype(d) D;

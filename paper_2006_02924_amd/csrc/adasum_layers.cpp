@@ -108,7 +108,7 @@ int adasum_embedding_grad_workspace_bytes(int64_t rows, int64_t width, int64_t n
     if (!known_dtype(dtype)) return ADASUM_ERR_UNSUPPORTED;
     ADASUM_CHECK(check_sizes(rows, width));
     ADASUM_CHECK(check_sizes(n_ids, width));
-    *bytes = n_ids == 0 || rows == 0 || width == 0 ? 0 : embedding_layout(width, n_ids, dtype).total;
+    *bytes = n_ids == 0 || rows == 0 || width == 0 ? 0 : embedding_layout(rows, width, n_ids, dtype).total;
     return ADASUM_OK;
 }
 
@@ -124,7 +124,7 @@ int adasum_embedding_grad(const void* dy, int dtype, int64_t dy_stride, const vo
     ADASUM_CHECK(check_rows(dy, n_ids, width, dy_stride, false));
     if (rows == 0 || width == 0) return ADASUM_OK;
     EmbeddingGrad g{};
-    if (n_ids > 0) g.lay = embedding_layout(width, n_ids, dtype);
+    if (n_ids > 0) g.lay = embedding_layout(rows, width, n_ids, dtype);
     ADASUM_CHECK(check_workspace(workspace, workspace_bytes, g.lay.total));
     g.grad = at(grad, offset, grad_dtype);
     const Range result = rows_range(g.grad, rows, width, width, grad_dtype), scratch = bytes_range(workspace, g.lay.total);

@@ -29,13 +29,18 @@ struct Ids {
 // The sorted tokens are cut into chunks of kRun.  A run (the tokens of one row) of at most kRun tokens is summed by
 // the wave in whose chunk it starts; of a longer one every chunk sums its part, and a second launch adds the parts.
 constexpr int kRun = 32;
-// Workgroups that sort: each takes an equal range of rows (at most kSortRows).
+// Workgroups that sort: each takes an equal range of rows, at most kSortRows where it reads all tokens itself and at most kGatherRows
+// where the tokens have been sorted by range before, in parts of kPartTokens.
 constexpr int kSortGroups = 256;
 constexpr int kSortRows = 512;
+constexpr int kGatherRows = 1024;
+constexpr int kPartTokens = 2048;
 inline int64_t sort_rows(int64_t rows) {
     const int64_t r = (rows + kSortGroups - 1) / kSortGroups;
     return r < 1 ? 1 : r > kSortRows ? kSortRows : r;
 }
+// Whether the tokens are sorted by range first.
+inline bool in_parts(int64_t rows, int64_t n_ids) { return n_ids > 4096 && rows <= kSortGroups * kGatherRows; }
 
 // Workspace of the table's gradient (byte offsets).
 struct EmbeddingLayout {
@@ -44,10 +49,12 @@ struct EmbeddingLayout {
     size_t off_listed = 0;    // int32 [chunk]: the chunks in which those start
     size_t off_place = 0;     // int32 [n]: tokens in the order of their ids
     size_t off_row = 0;       // int32 [n]: their ids
+    size_t off_begins = 0;    // where they are sorted by range first: int32 [range + 1][part]
+    size_t off_part_place = 0, off_part_row = 0;   // int32 [part][kPartTokens]
     size_t off_parts = 0;     // [chunk][2][width]: sums of the run that comes from the chunk before, and of the one that goes on into the next
     size_t total = 0;
 };
-EmbeddingLayout embedding_layout(int64_t width, int64_t n_ids, int dtype);
+EmbeddingLayout embedding_layout(int64_t rows, int64_t width, int64_t n_ids, int dtype);
 
 int launch_lookup(int dtype, int out_dtype, const void* table, int64_t rows, int64_t width, const Ids& ids, double scale,
                   void* out, int64_t out_stride, void* stream);
