@@ -65,6 +65,9 @@ constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortBatch = 16;                   // ids a lane has in flight
 constexpr int kClearBytes = 64 * kSortThreads;   // per workgroup
 
+// Counts in LDS that the lanes of a wave write for each other: volatile, and known to be LDS all the same.
+typedef volatile __attribute__((address_space(3))) int* lds_counts;
+
 // Zeros over the workgroups' share of the table.
 __device__ __forceinline__ void clear_table(long long block, long long blocks, char* __restrict__ clear, long long clear_bytes) {
     const unsigned zero[4] = {0, 0, 0, 0};
@@ -103,8 +106,7 @@ sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restr
     __syncthreads();
     const int64_t segment = ((ids.n + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
     const int64_t begin = min(segment * wave, ids.n), end = min(begin + segment, ids.n);
-    // (volatile: the lanes of a wave read what one of them has written)
-    volatile int* const my_counts = counts + wave * per_group;
+    const lds_counts my_counts = (lds_counts)(counts + wave * per_group);
     unsigned batch[kSortBatch];
     auto load = [&](int64_t from) {
 #pragma unroll
@@ -191,8 +193,7 @@ sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restr
 constexpr int kRowBits = 10;
 static_assert(kGatherRows == 1 << kRowBits && kGatherRows <= kSortThreads, "a range's rows have as many bits, and a lane each");
 constexpr int kPartThreads = 512, kPartWaves = kPartThreads / 64, kPartBatch = kPartTokens / kPartThreads;
-constexpr int kGatherBatch = 8;
-constexpr int kGatherTokens = kSortThreads * kGatherBatch;   // tokens of a range that are sorted at a time
+constexpr int kGatherBatch = 16;   // tokens of a lane that are in registers at most
 
 // The lanes with the same key of BITS bits, among those of `valid`.
 template <int BITS>
@@ -251,8 +252,7 @@ part_kernel(Ids ids, unsigned rows, Divider per_group, int n_parts, int* __restr
     for (int k = 0; k < kPartBatch; ++k) id[k] = from + 64 * k < ids.n ? row_of(ids, from + 64 * k) : ~0u;
     for (int i = threadIdx.x; i < kPartWaves * kSortGroups; i += kPartThreads) (&counts[0][0])[i] = 0;
     __syncthreads();
-    // (volatile: the lanes of a wave read what others of it have written)
-    volatile int* const mine = counts[wave];
+    const lds_counts mine = (lds_counts)(counts[wave]);
 #pragma unroll
     for (int k = 0; k < kPartBatch; ++k) {
         const bool valid = id[k] < rows;
@@ -308,17 +308,32 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
     const int* const begin_here = begins + static_cast<int64_t>(blockIdx.x) * n_parts;
     const int* const begin_next = begin_here + n_parts;
     int* const next = counts + kSortWaves * per_group;
-    // (volatile: the lanes of a wave read what others of it have written)
-    volatile int* const mine = counts + wave * per_group;
-    // tokens of the ranges before this one, and of this one
-    int below = 0, here = 0;
+    const lds_counts mine = (lds_counts)(counts + wave * per_group);
+    // tokens of the ranges before this one, and of those up to it
+    int below = 0, upto = 0;
     for (int p = threadIdx.x; p < n_parts; p += kSortThreads) {
         below += begin_here[p];
-        here += begin_next[p] - begin_here[p];
+        upto += begin_next[p];
     }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        below += __shfl_xor(below, m, 64);
+        upto += __shfl_xor(upto, m, 64);
+    }
+    if (lane == 0) {
+        length[wave] = below;
+        source[wave] = upto;
+    }
+    __syncthreads();
     int all_below = 0, all_here = 0;
-    scan_before<kSortWaves>(below, scan, all_below);
-    scan_before<kSortWaves>(here, scan, all_here);
+    for (int w = 0; w < kSortWaves; ++w) {
+        all_below += length[w];
+        all_here += source[w];
+    }
+    all_here -= all_below;
+    // 64 tokens of a wave at a time: how often, and how many waves have any
+    const int rounds = min(kGatherBatch, (all_here + kSortThreads - 1) / kSortThreads), at_once = kSortThreads * rounds;
+    const int ways = min(kSortWaves, (all_here + 64 * rounds - 1) / (64 * rounds));
     if (blockIdx.x == kSortGroups - 1 && threadIdx.x == 0) {
         totals[0] = all_below + all_here;
         totals[1] = 0;   // runs that sum_kernel lists
@@ -327,8 +342,9 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
     for (unsigned r = threadIdx.x; r < per_group; r += kSortThreads) next[r] = 0;
     int token[kGatherBatch], rank[kGatherBatch];
     unsigned key[kGatherBatch];
-    // f() for every kGatherTokens tokens of the range, in order: then a wave has consecutive ones, 64 at a time
+    // f(their index in the range) for every `at_once` tokens of the range, in order: then a wave has consecutive ones, 64 at a time
     auto every = [&](auto&& f) {
+        int before_parts = 0;
         for (int p0 = 0; p0 < n_parts; p0 += kSortThreads) {
             const int p = p0 + static_cast<int>(threadIdx.x);
             const int b = p < n_parts ? begin_here[p] : 0, n = p < n_parts ? begin_next[p] - b : 0;
@@ -337,13 +353,13 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
             length[threadIdx.x] = before;
             source[threadIdx.x] = b;
             __syncthreads();
-            for (int e0 = 0; e0 < all; e0 += kGatherTokens) {
+            for (int e0 = 0; e0 < all; e0 += at_once) {
 #pragma unroll
                 for (int k = 0; k < kGatherBatch; ++k) {
-                    const int e = e0 + wave * (64 * kGatherBatch) + 64 * k + lane;
+                    const int e = e0 + wave * (64 * rounds) + 64 * k + lane;
                     token[k] = -1;
                     key[k] = 0;
-                    if (e < all) {
+                    if (k < rounds && e < all) {
                         // the part that has it: the last one that begins at or before it
                         int q = 0;
 #pragma unroll
@@ -354,11 +370,24 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
                         key[k] = static_cast<unsigned>(part_row[from]) - lo;
                     }
                 }
-                f();
+                f(before_parts + e0 + wave * (64 * rounds) + lane);
             }
+            before_parts += all;
             __syncthreads();
         }
     };
+    if (per_group == 1) {
+        // a range of one row is sorted already
+        every([&](int index) {
+#pragma unroll
+            for (int k = 0; k < kGatherBatch; ++k)
+                if (token[k] >= 0) {
+                    place[all_below + index + 64 * k] = token[k];
+                    row[all_below + index + 64 * k] = static_cast<int>(lo);
+                }
+        });
+        return;
+    }
     // from how many tokens the rows have to where theirs begin
     auto rows_begin = [&] {
         const unsigned r = threadIdx.x;
@@ -369,10 +398,10 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
         if (r < mine_rows) next[r] = all_below + before;
         __syncthreads();
     };
-    const bool once = all_here <= kGatherTokens && n_parts <= kSortThreads;
+    const bool once = all_here <= at_once && n_parts <= kSortThreads;
     if (!once) {
         // a hot range, whose tokens come in several batches: first count them all
-        every([&] {
+        every([&](int) {
 #pragma unroll
             for (int k = 0; k < kGatherBatch; ++k) {
                 const unsigned long long valid = __ballot(token[k] >= 0);
@@ -383,8 +412,8 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
         });
         rows_begin();
     }
-    every([&] {
-        for (unsigned i = threadIdx.x; i < kSortWaves * per_group; i += kSortThreads) counts[i] = 0;
+    every([&](int) {
+        for (unsigned i = threadIdx.x; i < ways * per_group; i += kSortThreads) counts[i] = 0;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kGatherBatch; ++k) {
@@ -399,12 +428,12 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
         const unsigned r = threadIdx.x;
         if (once) {
             if (r < mine_rows)
-                for (int w = 0; w < kSortWaves; ++w) next[r] += counts[w * per_group + r];
+                for (int w = 0; w < ways; ++w) next[r] += counts[w * per_group + r];
             rows_begin();
         }
         if (r < mine_rows) {
             int to = next[r];
-            for (int w = 0; w < kSortWaves; ++w) {
+            for (int w = 0; w < ways; ++w) {
                 const int n = counts[w * per_group + r];
                 counts[w * per_group + r] = to;
                 to += n;
@@ -425,64 +454,78 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
 
 // ---- sums over runs of equal ids ----------------------------------------------------
 
-// A wave's look at a chunk of sorted tokens: index i stands for place i - kRun of the chunk, 0 <= i < 3 kRun.
+// A wave's look at a chunk of R sorted tokens: index i stands for place i - R of the chunk, 0 <= i < 3 R.
+template <int R>
 struct Window {
-    int row0, row1;               // of index lane, and of index 64 + lane (lanes below kRun)
+    int row0, row1;               // of index lane, and of index 64 + lane
     unsigned long long start;     // bit i: a run starts at index i (i < 64)
     unsigned later;               // the same for index 64 + i
     __device__ __forceinline__ int row_at(int i) const {
         return i < 64 ? __builtin_amdgcn_readlane(row0, i) : __builtin_amdgcn_readlane(row1, i - 64);
     }
+    // Whether the run that starts at index a (a < 2 R) has more than R tokens.
+    __device__ __forceinline__ bool is_long(int a) const { return row_at(a + R) == row_at(a); }
+    // The runs that start before the chunk, and in its first `there` tokens, as bits; the index of the first start behind a full chunk.
+    __device__ __forceinline__ unsigned before() const { return static_cast<unsigned>(start) & (~0u >> (32 - R)); }
+    __device__ __forceinline__ unsigned inside(int there) const { return static_cast<unsigned>(start >> R) & (~0u >> (32 - there)); }
+    __device__ __forceinline__ int behind() const {
+        const unsigned bits = R == 32 ? later : static_cast<unsigned>(start >> (R == 32 ? 0 : 2 * R));
+        return 2 * R + __builtin_ctz(bits | 0x80000000u);
+    }
 };
-__device__ __forceinline__ Window look(const int* row, int total, int64_t chunk, int lane) {
-    Window w;
-    const int64_t p0 = chunk * kRun - kRun + lane, p1 = p0 + 64;
+template <int R>
+__device__ __forceinline__ Window<R> look(const int* row, int total, int64_t chunk, int lane) {
+    static_assert(R == 16 || R == 32, "the window is 48 or 96 places");
+    Window<R> w;
+    const int64_t p0 = chunk * R - R + lane, p1 = p0 + 64;
     w.row0 = p0 >= 0 && p0 < total ? row[p0] : p0 < 0 ? -1 : -2;
-    w.row1 = lane < kRun && p1 < total ? row[p1] : -2;
-    const int left = __shfl_up(w.row0, 1, 64), last = __shfl(w.row0, 63, 64);
+    const int left = __shfl_up(w.row0, 1, 64);
     w.start = __ballot(lane > 0 && w.row0 != left);
-    const int left1 = __shfl_up(w.row1, 1, 64);
-    w.later = static_cast<unsigned>(__ballot(lane < kRun && w.row1 != (lane == 0 ? last : left1)));
+    w.row1 = -2;
+    w.later = 0;
+    if constexpr (R == 32) {
+        const int last = __shfl(w.row0, 63, 64);
+        if (lane < R && p1 < total) w.row1 = row[p1];
+        const int left1 = __shfl_up(w.row1, 1, 64);
+        w.later = static_cast<unsigned>(__ballot(lane < R && w.row1 != (lane == 0 ? last : left1)));
+    }
     return w;
 }
-// Whether the run that starts at index a (a < 64) has more than kRun tokens.
-__device__ __forceinline__ bool is_long(const Window& w, int a) { return w.row_at(a + kRun) == w.row_at(a); }
 
-// One wave: chunk `chunk`, the elements of `slice`; FULL: every lane's G elements exist.  `longs`: a count, then the chunks in which a
-// run of more than kRun tokens starts, in no certain order.
+// One wave: chunk `chunk`, the elements of `slice`; FULL: every lane's G elements exist.  The chunks in which a run of more than R tokens
+// starts are listed (`longs` counts them), in no certain order.
 constexpr int kBatch = 8;   // rows of dy in flight, twice
-template <typename D, typename T, bool FULL, bool ADD>
+template <int R, typename D, typename T, bool FULL, bool ADD>
 __device__ __forceinline__ void
 sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long long dy_stride, int width, int total,
           const int* __restrict__ place, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
           typename Traits<D>::acc_t* __restrict__ parts, int* __restrict__ longs, int* __restrict__ listed) {
     typedef typename Traits<D>::acc_t A;
     constexpr int G = Traits<D>::VEC;
-    static_assert(kRun == 32, "the window of a chunk is 96 places");
-    const Window w = look(row, total, chunk, lane);
-    const int there = static_cast<int>(min(static_cast<long long>(kRun), total - chunk * kRun));
-    // the tokens of indices kRun .. kRun + 63
-    const int64_t pp = chunk * kRun + lane;
+    const Window<R> w = look<R>(row, total, chunk, lane);
+    const int there = static_cast<int>(min(static_cast<long long>(R), total - chunk * R));
+    // the tokens of index R and on
+    const int64_t pp = chunk * R + lane;
     const int token = pp < total ? place[pp] : 0;
-    int from = kRun, until = kRun + there;
+    int from = R, until = R + there;
     // runs that start here (behind the last token is no run)
-    const unsigned starts = static_cast<unsigned>(w.start >> kRun) & (there == kRun ? ~0u : (1u << there) - 1);
+    const unsigned starts = w.inside(there);
     bool carried = false;   // the first run is a long one that comes from the chunk before
     if (!(starts & 1)) {
-        const unsigned before = static_cast<unsigned>(w.start);
+        const unsigned before = w.before();
         const int a = before != 0 ? 31 - __builtin_clz(before) : -1;
-        carried = a < 0 || is_long(w, a);
+        carried = a < 0 || w.is_long(a);
         if (!carried) {
             if (starts == 0) return;   // all of the chunk belongs to a run that the wave before has
-            from = kRun + __builtin_ctz(starts);
+            from = R + __builtin_ctz(starts);
         }
     }
     // the last run that starts here: whole if it is not long, else as far as the chunk goes
     bool open = false;
     if (starts != 0) {
-        open = is_long(w, kRun + 31 - __builtin_clz(starts));
+        open = w.is_long(R + 31 - __builtin_clz(starts));
         // (not long: the next run, or the end of the tokens, is in the window)
-        if (!open && there == kRun) until = 64 + __builtin_ctz(w.later | 0x80000000u);
+        if (!open && there == R) until = w.behind();
         if (open && slice == 0 && lane == 0) listed[atomicAdd(longs, 1)] = static_cast<int>(chunk);
     }
     const int at = (slice * 64 + lane) * G;
@@ -497,13 +540,13 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
     Granule<T, G> old[2][ADD ? kBatch : 1];
     auto load = [&](int set, int i0) {
 #pragma unroll
-        for (int k = 0; k < kBatch; ++k)
-            if (i0 + k < until) {
-                const int t = __builtin_amdgcn_readlane(token, i0 + k - kRun);
-                load_part<FULL>(v[set][k], dy + static_cast<long long>(t) * dy_stride + at, have);
-                if constexpr (ADD)
-                    if (ends_at(i0 + k)) load_part<FULL>(old[set][k], grad + static_cast<long long>(w.row_at(i0 + k)) * width + at, have);
-            }
+        for (int k = 0; k < kBatch; ++k) {
+            // (the last one again behind the last: a branch here would have the loads waited for at its end)
+            const int i = min(i0 + k, until - 1);
+            const int t = __builtin_amdgcn_readlane(token, i - R);
+            load_part<FULL>(v[set][k], dy + static_cast<long long>(t) * dy_stride + at, have);
+            if constexpr (ADD) load_part<FULL>(old[set][k], grad + static_cast<long long>(w.row_at(i)) * width + at, have);
+        }
     };
     auto take = [&](int set, int i0) {
 #pragma unroll
@@ -545,43 +588,44 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
     }
 }
 
-template <typename D, typename T, bool ADD>
+template <int R, typename D, typename T, bool ADD>
 __global__ void __launch_bounds__(256)
 sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, int* __restrict__ totals, const int* __restrict__ place,
            const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, typename Traits<D>::acc_t* __restrict__ parts,
            int* __restrict__ listed, int slices, long long n_chunks) {
     const int lane = threadIdx.x & 63;
     const int total = totals[0];
-    const long long units = min(n_chunks, (static_cast<long long>(total) + kRun - 1) / kRun) * slices;
+    const long long units = min(n_chunks, (static_cast<long long>(total) + R - 1) / R) * slices;
     for (long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += 4ll * gridDim.x) {
         const int slice = static_cast<int>(unit % slices);
         if ((slice + 1) * 64 * Traits<D>::VEC <= width)
-            sum_chunk<D, T, true, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
+            sum_chunk<R, D, T, true, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
         else
-            sum_chunk<D, T, false, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
+            sum_chunk<R, D, T, false, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
     }
 }
 
-// The parts of long runs.  A compute unit alone reads little, so a workgroup takes 64 elements only: sixteen groups of sixteen lanes
-// share a run's chunks, four elements a lane.
-template <typename D, typename T>
-__global__ void __launch_bounds__(256)
+// The parts of long runs.  A compute unit alone reads little, so a workgroup takes 64 elements only: groups of sixteen lanes share a
+// run's chunks, four elements a lane.
+template <int R, int THREADS, typename D, typename T>
+__global__ void __launch_bounds__(THREADS)
 join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
             int accumulate, const typename Traits<D>::acc_t* __restrict__ parts, const int* __restrict__ listed) {
     typedef typename Traits<D>::acc_t A;
-    __shared__ double shared[16][64];
+    constexpr int kJoinGroups = THREADS / 16;
+    __shared__ double shared[kJoinGroups][64];
     const int lane = threadIdx.x & 63, group = threadIdx.x >> 4, col = 4 * (threadIdx.x & 15);
     const int total = totals[0];
-    const long long slices = (width + 63) / 64, units = totals[1] * slices, n_chunks = (static_cast<long long>(total) + kRun - 1) / kRun;
+    const long long slices = (width + 63) / 64, units = totals[1] * slices, n_chunks = (static_cast<long long>(total) + R - 1) / R;
     for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const long long chunk = listed[unit / slices];
-        const Window w = look(row, total, chunk, lane);
-        const int key = w.row_at(kRun + 31 - __builtin_clz(static_cast<unsigned>(w.start >> 32)));
+        const Window<R> w = look<R>(row, total, chunk, lane);
+        const int key = w.row_at(R + 31 - __builtin_clz(w.inside(R)));
         // the last chunk that begins with this row (the next one does): the chunks up to `lo` do, those from `hi` on do not
         long long lo = chunk + 1, hi = n_chunks;
         while (hi - lo > 1) {
             const long long step = (hi - lo + 63) / 64, c = lo + (lane + 1) * step;
-            const unsigned long long same = __ballot(c < hi && row[c < hi ? c * kRun : 0] == key);
+            const unsigned long long same = __ballot(c < hi && row[c < hi ? c * R : 0] == key);
             const int yes = same == ~0ull ? 64 : __ffsll(~same) - 1;
             const long long next = lo + yes * step;
             hi = min(hi, next + step);
@@ -592,7 +636,7 @@ join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ r
         double sum[4] = {};
         if (have > 0) {
 #pragma unroll 8
-            for (long long c = group; c < n; c += 16) {
+            for (long long c = group; c < n; c += kJoinGroups) {
                 A v[4];
                 load_some<4>(v, parts + (2 * (chunk + c) + (c == 0 ? 1 : 0)) * width + at, have);
 #pragma unroll
@@ -608,7 +652,7 @@ join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ r
             if (e < width) {
                 double s = 0;
 #pragma unroll
-                for (int g = 0; g < 16; ++g) s += shared[g][lane];
+                for (int g = 0; g < kJoinGroups; ++g) s += shared[g][lane];
                 s *= scale;
                 T* const to = grad + static_cast<long long>(key) * width + e;
                 store_elem(to, static_cast<A>(accumulate ? s + load_elem(to) : s));
@@ -626,7 +670,8 @@ int slices_of(int64_t width, int dtype) {
 
 EmbeddingLayout embedding_layout(int64_t rows, int64_t width, int64_t n_ids, int dtype) {
     EmbeddingLayout l;
-    l.chunks = (n_ids + kRun - 1) / kRun;
+    l.run = n_ids <= kFewTokens ? 16 : 32;
+    l.chunks = (n_ids + l.run - 1) / l.run;
     l.off_listed = 256;
     l.off_place = align_up(l.off_listed + 4 * static_cast<size_t>(l.chunks), 256);
     l.off_row = align_up(l.off_place + 4 * static_cast<size_t>(n_ids), 256);
@@ -703,13 +748,20 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
         const int slices = slices_of(g.width, g.dtype);
         const int64_t units = g.lay.chunks * slices;
         A* const parts = reinterpret_cast<A*>(g.ws + g.lay.off_parts);
-        const int rc2 = launch(g.accumulate ? sum_kernel<D, T, true> : sum_kernel<D, T, false>, at_most_groups((units + 3) / 4), 1, 256, 0, stream,
-                               static_cast<const D*>(g.dy), g.dy_stride, g.width, totals, place, row, g.scale, static_cast<T*>(g.grad), parts,
-                               listed, slices, g.lay.chunks);
-        if (rc2 != 0 || g.ids.n <= kRun) return rc2;   // (so few tokens make no long run)
-        const int64_t most = (g.ids.n / (kRun + 1)) * ((g.width + 63) / 64);
-        return launch(join_kernel<D, T>, most < 1024 ? most : 1024, 1, 256, 0, stream, g.width, totals, row, g.scale,
-                      static_cast<T*>(g.grad), g.accumulate, parts, listed);
+        auto go = [&](auto run) -> int {
+            constexpr int R = decltype(run)::value;
+            const int rc2 = launch(g.accumulate ? sum_kernel<R, D, T, true> : sum_kernel<R, D, T, false>, at_most_groups((units + 3) / 4), 1, 256, 0,
+                                   stream, static_cast<const D*>(g.dy), g.dy_stride, g.width, totals, place, row, g.scale,
+                                   static_cast<T*>(g.grad), parts, listed, slices, g.lay.chunks);
+            if (rc2 != 0 || g.ids.n <= R) return rc2;   // (so few tokens make no long run)
+            const int64_t most = (g.ids.n / (R + 1)) * ((g.width + 63) / 64);
+            // few rows that all tokens share make few and very long runs (two rows, 16384 tokens: 9.0 us with 1024 lanes, 11.6 with 256),
+            // otherwise most of those that are long are so by little (30522 rows, 65501 tokens: 17.3 us and 7.4)
+            const bool few = g.ids.n > 256 * g.rows;
+            return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < 1024 ? most : 1024, 1, few ? 1024 : 256, 0, stream,
+                          g.width, totals, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, listed);
+        };
+        return g.lay.run == 16 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 32>{});
     });
 }
 

@@ -26,9 +26,10 @@ struct Ids {
     int64_t n;
 };
 
-// The sorted tokens are cut into chunks of kRun.  A run (the tokens of one row) of at most kRun tokens is summed by
-// the wave in whose chunk it starts; of a longer one every chunk sums its part, and a second launch adds the parts.
-constexpr int kRun = 32;
+// The sorted tokens are cut into chunks of 32, or of 16 up to kFewTokens tokens, which make too few waves otherwise.  A run (the tokens
+// of one row) that is no longer than a chunk is summed by the wave in whose chunk it starts; of a longer one every chunk sums its part,
+// and a second launch adds the parts.
+constexpr int64_t kFewTokens = 32768;
 // Workgroups that sort: each takes an equal range of rows, at most kSortRows where it reads all tokens itself and at most kGatherRows
 // where the tokens have been sorted by range before, in parts of kPartTokens.
 constexpr int kSortGroups = 256;
@@ -44,8 +45,9 @@ inline bool in_parts(int64_t rows, int64_t n_ids) { return n_ids > 4096 && rows 
 
 // Workspace of the table's gradient (byte offsets).
 struct EmbeddingLayout {
+    int run = 0;              // tokens of a chunk
     int64_t chunks = 0;
-    size_t off_totals = 0;    // int32: tokens whose id names a row; runs of more than kRun tokens
+    size_t off_totals = 0;    // int32: tokens whose id names a row; runs of more than a chunk's tokens
     size_t off_listed = 0;    // int32 [chunk]: the chunks in which those start
     size_t off_place = 0;     // int32 [n]: tokens in the order of their ids
     size_t off_row = 0;       // int32 [n]: their ids
