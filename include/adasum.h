@@ -347,7 +347,7 @@ ADASUM_API int adasum_group_combine(const void* const* x, int R,
  * Rows of an embedding table that lies at `offset` of a flat parameter buffer:
  *   out[t][:] = scale * table[ids[t]][:],   table = params[offset .. offset + rows * width)
  * An id outside [0, rows) (padding) gives a row of zeros.  `out` must not overlap params' table or ids
- * (ADASUM_ERR_ALIAS).  rows and n_ids at most 2^31 - 65536, width at most 2^24.
+ * (ADASUM_ERR_ALIAS).  rows and n_ids at most 2^31 - 65536, rows at least 1 where there are tokens, width at most 2^24.
  */
 ADASUM_API int adasum_embedding(const void* params, int dtype, int64_t offset, int64_t rows, int64_t width,
                                 const void* ids, int id_type, int64_t n_ids, double scale,

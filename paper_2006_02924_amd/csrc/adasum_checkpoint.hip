@@ -20,6 +20,11 @@ __device__ __forceinline__ unsigned quad_max(unsigned v) {
     return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4e, 0xf, 0xf, true)));   // 2 3 0 1
 }
 
+__device__ __forceinline__ unsigned low_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+    const unsigned ab = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), cd = __builtin_amdgcn_perm(d, c, 0x04000c0cu);
+    return ab | cd;
+}
+
 // 2^e; NaN for the mark of a block that is not finite.
 __device__ __forceinline__ float step_of(int e) {
     return __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
@@ -49,129 +54,134 @@ __device__ __forceinline__ float slope(float x) {
     }
 }
 
-// The rows of a workgroup: f(row, channel) for every eight channels up to the pitch, ITEMS of them in flight.
+// What a launch works on: eight channels of a row up to the pitch are a granule, ITEMS of a lane's are in flight.
 struct RowWork {
     long long rows;
-    int tokens;          // rows of a workgroup
+    int tokens;          // rows of a workgroup at a time
     Divider granules;    // of a row
 };
+// The place of a lane's granule number g of n among rows `first` and on.
+struct Place {
+    long long row;
+    int at;
+};
+__device__ __forceinline__ Place place_of(const RowWork& work, long long first, unsigned g) {
+    const unsigned t = divide(g, work.granules);
+    return {first + t, static_cast<int>((g - t * work.granules.d) * kG)};
+}
+// f(first row, granules) for every run of rows that this workgroup has.
+template <typename F>
+__device__ __forceinline__ void every_rows(const RowWork& work, F&& f) {
+    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
+         first += static_cast<long long>(gridDim.x) * work.tokens)
+        f(first, static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d);
+}
 
-template <typename T, int ITEMS>
+template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 store_kernel(const T* __restrict__ x, long long stride, int width, long long pitch, signed char* __restrict__ q, signed char* __restrict__ e,
              RowWork work) {
-    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
-         first += static_cast<long long>(gridDim.x) * work.tokens) {
-        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+    every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
-            float v[ITEMS][kG];
+            Granule<T, kG> raw[ITEMS];
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const unsigned g = base + kThreadsRow * k;
-                if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
-                    load_some<kG>(v[k], x + (first + t) * stride + at, width - static_cast<int>(at));
-                }
+                const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
+                load_row<FORM>(raw[k], x + p.row * stride, p.at, width);
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 // (n and the step are multiples of four: the lanes of a block are here together)
                 const unsigned g = base + kThreadsRow * k;
                 if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    const Place p = place_of(work, first, g);
+                    float v[kG];
+                    unpack(raw[k], v);
+                    // (channels up to the pitch that do not exist)
+#pragma unroll
+                    for (int i = 0; i < kG; ++i)
+                        if (FORM == kWhole ? p.at >= width : p.at + i >= width) v[i] = 0.f;
                     unsigned most = 0;
 #pragma unroll
-                    for (int i = 0; i < kG; ++i) most = max(most, __float_as_uint(v[k][i]) & 0x7fffffffu);
+                    for (int i = 0; i < kG; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
                     most = quad_max(most);
                     const bool bad = most >= 0x7f800000u;
                     const int exponent = max(static_cast<int>(most >> 23) - 133, -120);
                     const float scale = __uint_as_float(static_cast<unsigned>(127 - exponent) << 23);
                     unsigned b[kG];
 #pragma unroll
-                    for (int i = 0; i < kG; ++i) {
-                        const float y = fminf(fmaxf(v[k][i] * scale, -127.f), 127.f);
-                        b[i] = __float_as_uint(y + 12582912.f) & 0xffu;
-                    }
+                    for (int i = 0; i < kG; ++i) b[i] = __float_as_uint(fminf(fmaxf(v[i] * scale, -127.f), 127.f) + 12582912.f);
                     u32x2 packed;
-                    packed.x = bad ? 0u : b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24;
-                    packed.y = bad ? 0u : b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
-                    const long long row = first + t;
-                    *reinterpret_cast<u32x2*>(q + row * pitch + at) = packed;
-                    if ((g & 3) == 0) e[row * (pitch / kBlock) + at / kBlock] = static_cast<signed char>(bad ? -128 : exponent);
+                    packed.x = bad ? 0u : low_bytes(b[0], b[1], b[2], b[3]);
+                    packed.y = bad ? 0u : low_bytes(b[4], b[5], b[6], b[7]);
+                    *reinterpret_cast<u32x2*>(q + p.row * pitch + p.at) = packed;
+                    if ((g & 3) == 0) e[p.row * (pitch / kBlock) + p.at / kBlock] = static_cast<signed char>(bad ? -128 : exponent);
                 }
             }
         }
-    }
+    });
 }
 
-template <typename T, int ITEMS>
+template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 load_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, T* __restrict__ out,
             long long stride, RowWork work) {
-    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
-         first += static_cast<long long>(gridDim.x) * work.tokens) {
-        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+    every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
             u32x2 kept[ITEMS];
             int exponent[ITEMS];
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const unsigned g = base + kThreadsRow * k;
-                if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
-                    kept[k] = *reinterpret_cast<const u32x2*>(q + (first + t) * pitch + at);
-                    exponent[k] = e[(first + t) * (pitch / kBlock) + at / kBlock];
-                }
+                const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
+                kept[k] = *reinterpret_cast<const u32x2*>(q + p.row * pitch + p.at);
+                exponent[k] = e[p.row * (pitch / kBlock) + p.at / kBlock];
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 const unsigned g = base + kThreadsRow * k;
                 if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
+                    const Place p = place_of(work, first, g);
                     float v[kG];
                     kept_values(v, kept[k], step_of(exponent[k]));
-                    store_some<kG>(out + (first + t) * stride + at, v, width - static_cast<int>(at));
+                    store_row<FORM>(out + p.row * stride, v, p.at, width);
                 }
             }
         }
-    }
+    });
 }
 
-template <typename T, int ACT, int ITEMS>
+// (dy and dx may be the same rows: a lane loads what it stores before it does)
+template <typename T, int ACT, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, const T* dy,
                 long long dy_stride, T* dx, long long dx_stride, RowWork work) {
-    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
-         first += static_cast<long long>(gridDim.x) * work.tokens) {
-        const unsigned n = static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d;
+    every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
             u32x2 kept[ITEMS];
             int exponent[ITEMS];
-            float d[ITEMS][kG];
+            Granule<T, kG> raw[ITEMS];
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
-                const unsigned g = base + kThreadsRow * k;
-                if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
-                    kept[k] = *reinterpret_cast<const u32x2*>(q + (first + t) * pitch + at);
-                    exponent[k] = e[(first + t) * (pitch / kBlock) + at / kBlock];
-                    load_some<kG>(d[k], dy + (first + t) * dy_stride + at, width - static_cast<int>(at));
-                }
+                const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
+                kept[k] = *reinterpret_cast<const u32x2*>(q + p.row * pitch + p.at);
+                exponent[k] = e[p.row * (pitch / kBlock) + p.at / kBlock];
+                load_row<FORM>(raw[k], dy + p.row * dy_stride, p.at, width);
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 const unsigned g = base + kThreadsRow * k;
                 if (g < n) {
-                    const unsigned t = divide(g, work.granules), at = (g - t * work.granules.d) * kG;
-                    float v[kG];
+                    const Place p = place_of(work, first, g);
+                    float v[kG], d[kG];
                     kept_values(v, kept[k], step_of(exponent[k]));
+                    unpack(raw[k], d);
 #pragma unroll
-                    for (int i = 0; i < kG; ++i) v[i] = d[k][i] * slope<ACT>(v[i]);
-                    store_some<kG>(dx + (first + t) * dx_stride + at, v, width - static_cast<int>(at));
+                    for (int i = 0; i < kG; ++i) v[i] = d[i] * slope<ACT>(v[i]);
+                    store_row<FORM>(dx + p.row * dx_stride, v, p.at, width);
                 }
             }
         }
-    }
+    });
 }
 
 struct RowGrid {
@@ -198,9 +208,12 @@ int launch_store(const void* x, int dtype, int64_t x_stride, const Kept& to, voi
     const RowGrid g = row_grid(to.rows, to.pitch);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
-        const auto kernel = g.large ? store_kernel<T, 4> : store_kernel<T, 1>;
-        return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x), x_stride, to.width, to.pitch,
-            reinterpret_cast<signed char*>(const_cast<int8_t*>(to.q)), reinterpret_cast<signed char*>(const_cast<int8_t*>(to.e)), g.work);
+        return with_form(row_form(to.width, kG), [&](auto form) -> int {
+            constexpr RowForm F = decltype(form)::value;
+            return launch(g.large ? store_kernel<T, F, 4> : store_kernel<T, F, 1>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x),
+                          x_stride, to.width, to.pitch, reinterpret_cast<signed char*>(const_cast<int8_t*>(to.q)),
+                          reinterpret_cast<signed char*>(const_cast<int8_t*>(to.e)), g.work);
+        });
     });
 }
 
@@ -208,9 +221,14 @@ int launch_load(const Kept& k, void* out, int dtype, int64_t out_stride, void* s
     const RowGrid g = row_grid(k.rows, k.pitch);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
-        const auto kernel = g.large ? load_kernel<T, 4> : load_kernel<T, 1>;
-        return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
-            static_cast<T*>(out), out_stride, g.work);
+        auto go = [&](auto form) -> int {
+            constexpr RowForm F = decltype(form)::value;
+            return launch(g.large ? load_kernel<T, F, 4> : load_kernel<T, F, 1>, g.groups, 1, kThreadsRow, 0, stream,
+                          reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+                          static_cast<T*>(out), out_stride, g.work);
+        };
+        // (short rows are stored like ragged ones)
+        return k.width % kG == 0 ? go(std::integral_constant<RowForm, kWhole>{}) : go(std::integral_constant<RowForm, kRagged>{});
     });
 }
 
@@ -218,17 +236,21 @@ int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t d
     const RowGrid g = row_grid(k.rows, k.pitch);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
-        auto go = [&](auto small, auto large) -> int {
-            const auto kernel = g.large ? large : small;
-            return launch(kernel, g.groups, 1, kThreadsRow, 0, stream, reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
-                static_cast<const T*>(dy), dy_stride, static_cast<T*>(dx), dx_stride, g.work);
-        };
-        switch (act) {
-            case ADASUM_ACT_RELU: return go(act_grad_kernel<T, ADASUM_ACT_RELU, 1>, act_grad_kernel<T, ADASUM_ACT_RELU, 4>);
-            case ADASUM_ACT_GELU: return go(act_grad_kernel<T, ADASUM_ACT_GELU, 1>, act_grad_kernel<T, ADASUM_ACT_GELU, 4>);
-            case ADASUM_ACT_GELU_TANH: return go(act_grad_kernel<T, ADASUM_ACT_GELU_TANH, 1>, act_grad_kernel<T, ADASUM_ACT_GELU_TANH, 4>);
-            default: return go(act_grad_kernel<T, ADASUM_ACT_SILU, 1>, act_grad_kernel<T, ADASUM_ACT_SILU, 4>);
-        }
+        return with_form(row_form(k.width, kG), [&](auto form) -> int {
+            constexpr RowForm F = decltype(form)::value;
+            auto go = [&](auto chosen) -> int {
+                constexpr int ACT = decltype(chosen)::value;
+                return launch(g.large ? act_grad_kernel<T, ACT, F, 4> : act_grad_kernel<T, ACT, F, 1>, g.groups, 1, kThreadsRow, 0, stream,
+                              reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+                              static_cast<const T*>(dy), dy_stride, static_cast<T*>(dx), dx_stride, g.work);
+            };
+            switch (act) {
+                case ADASUM_ACT_RELU: return go(std::integral_constant<int, ADASUM_ACT_RELU>{});
+                case ADASUM_ACT_GELU: return go(std::integral_constant<int, ADASUM_ACT_GELU>{});
+                case ADASUM_ACT_GELU_TANH: return go(std::integral_constant<int, ADASUM_ACT_GELU_TANH>{});
+                default: return go(std::integral_constant<int, ADASUM_ACT_SILU>{});
+            }
+        });
     });
 }
 

@@ -7,50 +7,51 @@
 namespace adasum {
 namespace {
 
-__device__ __forceinline__ long long id_at(const Ids& ids, int64_t t) {
-    return ids.wide ? static_cast<const int64_t*>(ids.p)[t] : static_cast<long long>(static_cast<const int32_t*>(ids.p)[t]);
+// An id as a number that is below 2^31 - 65536 for every row there may be, and far above for ids that name none.
+__device__ __forceinline__ unsigned row_of(const Ids& ids, int64_t t) {
+    if (ids.wide) {
+        const u32x2 id = static_cast<const u32x2*>(ids.p)[t];
+        return id.y == 0 ? id.x : ~0u;
+    }
+    return static_cast<const unsigned*>(ids.p)[t];
 }
 
 // ---- rows of the table -----------------------------------------------------------
 //
 // out[t] = scale * table[ids[t]]: every byte moves once, nothing is computed to speak of.  A workgroup takes consecutive tokens, a
-// lane G elements of a row at a time (16 bytes of the narrower type).
-template <typename T, typename U, int ITEMS>
+// lane G elements of a row at a time (16 bytes of the narrower type), ITEMS of them in flight.
+template <typename T, typename U, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(256)
-lookup_kernel(const T* __restrict__ table, long long rows, int width, Ids ids, typename Traits<T>::acc_t scale, U* __restrict__ out,
+lookup_kernel(const T* __restrict__ table, unsigned rows, int width, Ids ids, typename Traits<T>::acc_t scale, U* __restrict__ out,
               long long out_stride, int tokens, Divider granules) {
     typedef typename Traits<T>::acc_t A;
     constexpr int G = 16 / (sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U));
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * tokens; first < ids.n; first += static_cast<int64_t>(gridDim.x) * tokens) {
-    const int here = static_cast<int>(min(static_cast<int64_t>(tokens), ids.n - first));
-    const unsigned work = static_cast<unsigned>(here) * granules.d;
-    for (unsigned base = threadIdx.x; base < work; base += 256 * ITEMS) {
-        A v[ITEMS][G];
+        const int here = static_cast<int>(min(static_cast<int64_t>(tokens), ids.n - first));
+        const unsigned work = static_cast<unsigned>(here) * granules.d;
+        for (unsigned base = threadIdx.x; base < work; base += 256 * ITEMS) {
+            Granule<T, G> raw[ITEMS];
+            unsigned id[ITEMS], t[ITEMS];
+            int at[ITEMS];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const unsigned g = base + 256 * k;
-            if (g < work) {
-                const unsigned t = divide(g, granules), at = (g - t * granules.d) * G;
-                const long long id = id_at(ids, first + t);
-                if (id >= 0 && id < rows) {
-                    load_some<G>(v[k], table + id * width + at, width - static_cast<int>(at));
-                } else {
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = min(base + 256 * k, work - 1);
+                t[k] = divide(g, granules);
+                at[k] = static_cast<int>((g - t[k] * granules.d) * G);
+                id[k] = row_of(ids, first + t[k]);
+            }
+            // (ids that name no row load the first one)
 #pragma unroll
-                    for (int i = 0; i < G; ++i) v[k][i] = A(0);
-                }
+            for (int k = 0; k < ITEMS; ++k) load_row<FORM>(raw[k], table + static_cast<long long>(id[k] < rows ? id[k] : 0) * width, at[k], width);
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                A v[G];
+                unpack(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < G; ++i) v[i] = id[k] < rows ? v[i] * scale : A(0);
+                if (base + 256 * k < work) store_row<FORM>(out + (first + t[k]) * out_stride, v, at[k], width);
             }
         }
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            const unsigned g = base + 256 * k;
-            if (g < work) {
-                const unsigned t = divide(g, granules), at = (g - t * granules.d) * G;
-#pragma unroll
-                for (int i = 0; i < G; ++i) v[k][i] *= scale;
-                store_some<G>(out + (first + t) * out_stride + at, v[k], width - static_cast<int>(at));
-            }
-        }
-    }
     }
 }
 
@@ -80,15 +81,6 @@ __device__ __forceinline__ void clear_table(long long block, long long blocks, c
                 for (long long b = at; b < clear_bytes; b += 2) *reinterpret_cast<unsigned short*>(clear + b) = 0;
             }
         }
-}
-
-// An id as a number that is below 2^31 - 65536 for every row there may be, and far above for ids that name none.
-__device__ __forceinline__ unsigned row_of(const Ids& ids, int64_t t) {
-    if (ids.wide) {
-        const u32x2 id = static_cast<const u32x2*>(ids.p)[t];
-        return id.y == 0 ? id.x : ~0u;
-    }
-    return static_cast<const unsigned*>(ids.p)[t];
 }
 
 __global__ void __launch_bounds__(kSortThreads)
@@ -183,8 +175,9 @@ sort_kernel(Ids ids, unsigned rows, unsigned per_group, int groups, int* __restr
 
 // ---- sorting many tokens -------------------------------------------------------------
 //
-// Where the tokens are many, reading all of them in every workgroup costs more than a launch.  The rows are cut into kSortGroups equal
-// ranges.  First, workgroups of kPartTokens tokens each sort theirs by range, for themselves, and write down where each range
+// Where the tokens are many, reading all of them in every workgroup costs more than a launch.  (Equal ids must come to lie together, the
+// order of the rows does not matter.)  A row belongs to the range that its lowest bits say: vocabularies often are in the order of
+// frequency.  First, workgroups of kPartTokens tokens each sort theirs by range, for themselves, and write down where each range
 // begins; what lies below a range in all of them together is where its list starts.  Then one workgroup per range gathers its tokens,
 // in order, and sorts them by row.
 //
@@ -235,7 +228,7 @@ __device__ __forceinline__ int scan_before(int v, int* shared, int& all) {
 // The tokens of each part by range: part_place / part_row[part * kPartTokens + i], and begins[range][part], the index of the part's
 // first token of that range (range kSortGroups: its tokens that name a row).
 __global__ void __launch_bounds__(kPartThreads)
-part_kernel(Ids ids, unsigned rows, Divider per_group, int n_parts, int* __restrict__ begins, int* __restrict__ part_place,
+part_kernel(Ids ids, unsigned rows, int n_parts, int* __restrict__ begins, int* __restrict__ part_place,
             int* __restrict__ part_row, char* __restrict__ clear, long long clear_bytes) {
     __shared__ int counts[kPartWaves][kSortGroups];
     __shared__ int first[kSortGroups];
@@ -256,7 +249,7 @@ part_kernel(Ids ids, unsigned rows, Divider per_group, int n_parts, int* __restr
 #pragma unroll
     for (int k = 0; k < kPartBatch; ++k) {
         const bool valid = id[k] < rows;
-        group[k] = valid ? static_cast<int>(divide(id[k], per_group)) : 0;
+        group[k] = valid ? static_cast<int>(id[k] % kSortGroups) : 0;
         const unsigned long long same = same_key<8>(group[k], __ballot(valid), 8);
         const int before = __popcll(same & ((1ull << lane) - 1));
         const int seen = mine[group[k]];
@@ -292,7 +285,7 @@ part_kernel(Ids ids, unsigned rows, Divider per_group, int n_parts, int* __restr
 
 // Range blockIdx.x: gathers its tokens from the parts and sorts them by row.
 __global__ void __launch_bounds__(kSortThreads)
-gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, const int* __restrict__ begins, const int* __restrict__ part_place,
+gather_kernel(unsigned per_group, int row_bits, int n_parts, const int* __restrict__ begins, const int* __restrict__ part_place,
               const int* __restrict__ part_row, int* __restrict__ totals, int* __restrict__ place, int* __restrict__ row,
               char* __restrict__ clear, long long clear_bytes) {
     if (blockIdx.x >= kSortGroups) {
@@ -304,7 +297,6 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
     __shared__ int source[kSortThreads];            // where theirs begin
     __shared__ int scan[kSortWaves];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const unsigned lo = blockIdx.x * per_group, mine_rows = lo < rows ? min(per_group, rows - lo) : 0;
     const int* const begin_here = begins + static_cast<int64_t>(blockIdx.x) * n_parts;
     const int* const begin_next = begin_here + n_parts;
     int* const next = counts + kSortWaves * per_group;
@@ -342,9 +334,8 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
     for (unsigned r = threadIdx.x; r < per_group; r += kSortThreads) next[r] = 0;
     int token[kGatherBatch], rank[kGatherBatch];
     unsigned key[kGatherBatch];
-    // f(their index in the range) for every `at_once` tokens of the range, in order: then a wave has consecutive ones, 64 at a time
+    // f() for every `at_once` tokens of the range, in order: then a wave has consecutive ones, 64 at a time
     auto every = [&](auto&& f) {
-        int before_parts = 0;
         for (int p0 = 0; p0 < n_parts; p0 += kSortThreads) {
             const int p = p0 + static_cast<int>(threadIdx.x);
             const int b = p < n_parts ? begin_here[p] : 0, n = p < n_parts ? begin_next[p] - b : 0;
@@ -367,41 +358,28 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
                             if (length[q + step] <= e) q += step;
                         const int64_t from = static_cast<int64_t>(p0 + q) * kPartTokens + source[q] + (e - length[q]);
                         token[k] = part_place[from];
-                        key[k] = static_cast<unsigned>(part_row[from]) - lo;
+                        key[k] = static_cast<unsigned>(part_row[from]) / kSortGroups;
                     }
                 }
-                f(before_parts + e0 + wave * (64 * rounds) + lane);
+                f();
             }
-            before_parts += all;
             __syncthreads();
         }
     };
-    if (per_group == 1) {
-        // a range of one row is sorted already
-        every([&](int index) {
-#pragma unroll
-            for (int k = 0; k < kGatherBatch; ++k)
-                if (token[k] >= 0) {
-                    place[all_below + index + 64 * k] = token[k];
-                    row[all_below + index + 64 * k] = static_cast<int>(lo);
-                }
-        });
-        return;
-    }
     // from how many tokens the rows have to where theirs begin
     auto rows_begin = [&] {
         const unsigned r = threadIdx.x;
         __syncthreads();
-        const int n = r < mine_rows ? next[r] : 0;
+        const int n = r < per_group ? next[r] : 0;
         int all = 0;
         const int before = scan_before<kSortWaves>(n, scan, all);
-        if (r < mine_rows) next[r] = all_below + before;
+        if (r < per_group) next[r] = all_below + before;
         __syncthreads();
     };
     const bool once = all_here <= at_once && n_parts <= kSortThreads;
     if (!once) {
         // a hot range, whose tokens come in several batches: first count them all
-        every([&](int) {
+        every([&] {
 #pragma unroll
             for (int k = 0; k < kGatherBatch; ++k) {
                 const unsigned long long valid = __ballot(token[k] >= 0);
@@ -412,7 +390,7 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
         });
         rows_begin();
     }
-    every([&](int) {
+    every([&] {
         for (unsigned i = threadIdx.x; i < ways * per_group; i += kSortThreads) counts[i] = 0;
         __syncthreads();
 #pragma unroll
@@ -427,11 +405,11 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
         __syncthreads();
         const unsigned r = threadIdx.x;
         if (once) {
-            if (r < mine_rows)
+            if (r < per_group)
                 for (int w = 0; w < ways; ++w) next[r] += counts[w * per_group + r];
             rows_begin();
         }
-        if (r < mine_rows) {
+        if (r < per_group) {
             int to = next[r];
             for (int w = 0; w < ways; ++w) {
                 const int n = counts[w * per_group + r];
@@ -446,10 +424,57 @@ gather_kernel(unsigned rows, unsigned per_group, int row_bits, int n_parts, cons
             if (token[k] >= 0) {
                 const int to = mine[key[k]] + rank[k];
                 place[to] = token[k];
-                row[to] = static_cast<int>(key[k] + lo);
+                row[to] = static_cast<int>(key[k] * kSortGroups + blockIdx.x);
             }
         __syncthreads();
     });
+}
+
+// Where every range has one row only, its tokens are sorted as they are: workgroup (range, piece) moves those of the parts of its piece, a
+// wave a part.
+constexpr int kPieceParts = 4;
+__global__ void __launch_bounds__(256)
+move_kernel(int n_parts, int pieces, const int* __restrict__ begins, const int* __restrict__ part_place, int* __restrict__ totals,
+            int* __restrict__ place, int* __restrict__ row, int groups, char* __restrict__ clear, long long clear_bytes) {
+    if (static_cast<int>(blockIdx.x) >= groups) {
+        clear_table(blockIdx.x - groups, gridDim.x - groups, clear, clear_bytes);
+        return;
+    }
+    __shared__ int shared[3][4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int range = static_cast<int>(blockIdx.x) / pieces, first = static_cast<int>(blockIdx.x) % pieces * kPieceParts;
+    const int* const begin_here = begins + static_cast<int64_t>(range) * n_parts;
+    const int* const begin_next = begin_here + n_parts;
+    // tokens of the ranges before this one, of this one in the parts before, and of all ranges
+    int sums[3] = {};
+    for (int p = threadIdx.x; p < n_parts; p += 256) {
+        sums[0] += begin_here[p];
+        if (p < first) sums[1] += begin_next[p] - begin_here[p];
+        sums[2] += begins[static_cast<int64_t>(kSortGroups) * n_parts + p];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) sums[k] += __shfl_xor(sums[k], m, 64);
+        if (lane == 0) shared[k][wave] = sums[k];
+    }
+    __syncthreads();
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        totals[0] = shared[2][0] + shared[2][1] + shared[2][2] + shared[2][3];
+        totals[1] = 0;   // runs that sum_kernel lists
+    }
+    int to = 0;
+    for (int w = 0; w < 4; ++w) to += shared[0][w] + shared[1][w];
+    for (int p = first; p < min(first + kPieceParts, n_parts); ++p) {
+        const int b = begin_here[p], n = begin_next[p] - b;
+        if ((p & 3) == wave)
+#pragma unroll 8
+            for (int i = lane; i < n; i += 64) {
+                place[to + i] = part_place[static_cast<int64_t>(p) * kPartTokens + b + i];
+                row[to + i] = range;
+            }
+        to += n;
+    }
 }
 
 // ---- sums over runs of equal ids ----------------------------------------------------
@@ -492,10 +517,10 @@ __device__ __forceinline__ Window<R> look(const int* row, int total, int64_t chu
     return w;
 }
 
-// One wave: chunk `chunk`, the elements of `slice`; FULL: every lane's G elements exist.  The chunks in which a run of more than R tokens
+// One wave: chunk `chunk`, the elements of `slice`.  The chunks in which a run of more than R tokens
 // starts are listed (`longs` counts them), in no certain order.
-constexpr int kBatch = 8;   // rows of dy in flight, twice
-template <int R, typename D, typename T, bool FULL, bool ADD>
+constexpr int kBatch = 8;   // rows of dy in flight
+template <int R, typename D, typename T, RowForm FORM, bool ADD>
 __device__ __forceinline__ void
 sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long long dy_stride, int width, int total,
           const int* __restrict__ place, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
@@ -529,66 +554,56 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
         if (open && slice == 0 && lane == 0) listed[atomicAdd(longs, 1)] = static_cast<int>(chunk);
     }
     const int at = (slice * 64 + lane) * G;
-    const int have = FULL ? G : width - at;
     auto ends_at = [&](int i) { return i + 1 == until || (i + 1 < 64 ? (w.start >> (i + 1)) & 1 : (w.later >> (i + 1 - 64)) & 1); };
     auto goes_on = [&](int i) { return open && i + 1 == until; };
     A sum[G];
 #pragma unroll
     for (int i = 0; i < G; ++i) sum[i] = A(0);
     bool first_run = carried;
-    Granule<D, G> v[2][kBatch];
-    Granule<T, G> old[2][ADD ? kBatch : 1];
-    auto load = [&](int set, int i0) {
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            // (the last one again behind the last: a branch here would have the loads waited for at its end)
-            const int i = min(i0 + k, until - 1);
-            const int t = __builtin_amdgcn_readlane(token, i - R);
-            load_part<FULL>(v[set][k], dy + static_cast<long long>(t) * dy_stride + at, have);
-            if constexpr (ADD) load_part<FULL>(old[set][k], grad + static_cast<long long>(w.row_at(i)) * width + at, have);
-        }
+    Granule<D, G> v[kBatch];
+    Granule<T, G> old[ADD ? kBatch : 1];
+    auto load = [&](int k, int index) {
+        // (the last one again behind the last: a branch here would have the loads waited for at its end)
+        const int i = min(index, until - 1);
+        const int t = __builtin_amdgcn_readlane(token, i - R);
+        load_row<FORM>(v[k], dy + static_cast<long long>(t) * dy_stride, at, width);
+        if constexpr (ADD) load_row<FORM>(old[k], grad + static_cast<long long>(w.row_at(i)) * width, at, width);
     };
-    auto take = [&](int set, int i0) {
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) load(k, from + k);
+    for (int i0 = from; i0 < until; i0 += kBatch) {
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
             const int i = i0 + k;
-            if (i < until) {
-                A x[G];
-                unpack(v[set][k], x);
+            A x[G];
+            unpack(v[k], x);
 #pragma unroll
-                for (int j = 0; j < G; ++j) sum[j] += x[j];
-                if (ends_at(i)) {
-                    if (first_run || goes_on(i)) {
-                        // (the one that comes from before and goes on lies in the first place)
-                        store_part<FULL, G>(parts + (2 * chunk + (first_run ? 0 : 1)) * width + at, sum, have);
-                    } else {
+            for (int j = 0; j < G; ++j) sum[j] += x[j];
+            if (i < until && ends_at(i)) {
+                if (first_run || goes_on(i)) {
+                    // (the one that comes from before and goes on lies in the first place)
+                    store_row<FORM>(parts + (2 * chunk + (first_run ? 0 : 1)) * width, sum, at, width);
+                } else {
 #pragma unroll
-                        for (int j = 0; j < G; ++j) sum[j] *= scale;
-                        if constexpr (ADD) {
-                            A o[G];
-                            unpack(old[set][k], o);
+                    for (int j = 0; j < G; ++j) sum[j] *= scale;
+                    if constexpr (ADD) {
+                        A o[G];
+                        unpack(old[k], o);
 #pragma unroll
-                            for (int j = 0; j < G; ++j) sum[j] += o[j];
-                        }
-                        store_part<FULL, G>(grad + static_cast<long long>(w.row_at(i)) * width + at, sum, have);
+                        for (int j = 0; j < G; ++j) sum[j] += o[j];
                     }
-#pragma unroll
-                    for (int j = 0; j < G; ++j) sum[j] = A(0);
-                    first_run = false;
+                    store_row<FORM>(grad + static_cast<long long>(w.row_at(i)) * width, sum, at, width);
                 }
+#pragma unroll
+                for (int j = 0; j < G; ++j) sum[j] = A(0);
+                first_run = false;
             }
+            load(k, i + kBatch);
         }
-    };
-    load(0, from);
-    for (int i0 = from; i0 < until; i0 += 2 * kBatch) {
-        load(1, i0 + kBatch);
-        take(0, i0);
-        load(0, i0 + 2 * kBatch);
-        take(1, i0 + kBatch);
     }
 }
 
-template <int R, typename D, typename T, bool ADD>
+template <int R, typename D, typename T, RowForm FORM, bool ADD>
 __global__ void __launch_bounds__(256)
 sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, int* __restrict__ totals, const int* __restrict__ place,
            const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad, typename Traits<D>::acc_t* __restrict__ parts,
@@ -598,10 +613,8 @@ sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, int* __rest
     const long long units = min(n_chunks, (static_cast<long long>(total) + R - 1) / R) * slices;
     for (long long unit = static_cast<long long>(blockIdx.x) * 4 + (threadIdx.x >> 6); unit < units; unit += 4ll * gridDim.x) {
         const int slice = static_cast<int>(unit % slices);
-        if ((slice + 1) * 64 * Traits<D>::VEC <= width)
-            sum_chunk<R, D, T, true, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
-        else
-            sum_chunk<R, D, T, false, ADD>(unit / slices, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
+        const long long chunk = unit / slices;
+        sum_chunk<R, D, T, FORM, ADD>(chunk, slice, lane, dy, dy_stride, width, total, place, row, scale, grad, parts, totals + 1, listed);
     }
 }
 
@@ -699,9 +712,12 @@ int launch_lookup(int dtype, int out_dtype, const void* table, int64_t rows, int
         const int64_t per_block = large ? 1024 : 256;
         const int64_t tokens = granules >= per_block ? 1 : per_block / granules;
         const int64_t blocks = (ids.n + tokens - 1) / tokens;
-        const auto kernel = large ? lookup_kernel<T, U, 4> : lookup_kernel<T, U, 1>;
-        return launch(kernel, at_most_groups(blocks), 1, 256, 0, stream, static_cast<const T*>(table), rows, width, ids, scale,
-                      static_cast<U*>(out), out_stride, tokens, make_divider(static_cast<unsigned>(granules)));
+        return with_form(row_form(width, G), [&](auto form) -> int {
+            constexpr RowForm F = decltype(form)::value;
+            return launch(large ? lookup_kernel<T, U, F, 4> : lookup_kernel<T, U, F, 1>, at_most_groups(blocks), 1, 256, 0, stream,
+                          static_cast<const T*>(table), rows, width, ids, scale, static_cast<U*>(out), out_stride, tokens,
+                          make_divider(static_cast<unsigned>(granules)));
+        });
     });
 }
 
@@ -722,15 +738,20 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
         int* const part_row = reinterpret_cast<int*>(g.ws + g.lay.off_part_row);
         // each launch clears half of the table
         const int64_t half = clear_bytes / 2 / kClearBytes * kClearBytes;
-        rc = launch(part_kernel, n_parts + at_most_groups((half + kClearBytes - 1) / kClearBytes), 1, kPartThreads, 0, stream, g.ids, g.rows,
-                    make_divider(static_cast<unsigned>(per_group)), n_parts, begins, part_place, part_row, clear, half);
+        rc = launch(part_kernel, n_parts + at_most_groups((half + kClearBytes - 1) / kClearBytes), 1, kPartThreads, 0, stream, g.ids, g.rows, n_parts, begins, part_place, part_row, clear, half);
         if (rc != 0) return rc;
-        const size_t lds = sizeof(int) * (kSortWaves + 1) * per_group;
-        rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(gather_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                  static_cast<int>(sizeof(int) * (kSortWaves + 1) * kGatherRows)));
-        if (rc != 0) return rc;
-        rc = launch(gather_kernel, kSortGroups + at_most_groups((clear_bytes - half + kClearBytes - 1) / kClearBytes), 1, kSortThreads, lds, stream,
-                    g.rows, per_group, row_bits, n_parts, begins, part_place, part_row, totals, place, row, clear + half, clear_bytes - half);
+        const int64_t clearing = at_most_groups((clear_bytes - half + kClearBytes - 1) / kClearBytes);
+        if (per_group == 1) {
+            const int64_t pieces = (n_parts + kPieceParts - 1) / kPieceParts, groups = g.rows * pieces;
+            rc = launch(move_kernel, groups + clearing, 1, 256, 0, stream, n_parts, pieces, begins, part_place, totals, place, row, groups,
+                        clear + half, clear_bytes - half);
+        } else {
+            rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(gather_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                      static_cast<int>(sizeof(int) * (kSortWaves + 1) * kGatherRows)));
+            if (rc != 0) return rc;
+            rc = launch(gather_kernel, kSortGroups + clearing, 1, kSortThreads, sizeof(int) * (kSortWaves + 1) * per_group, stream, per_group,
+                        row_bits, n_parts, begins, part_place, part_row, totals, place, row, clear + half, clear_bytes - half);
+        }
     } else {
         const int64_t per_group = sort_rows(g.rows);
         const int64_t groups = g.ids.n == 0 ? 0 : (g.rows + per_group - 1) / per_group;
@@ -750,9 +771,12 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
         A* const parts = reinterpret_cast<A*>(g.ws + g.lay.off_parts);
         auto go = [&](auto run) -> int {
             constexpr int R = decltype(run)::value;
-            const int rc2 = launch(g.accumulate ? sum_kernel<R, D, T, true> : sum_kernel<R, D, T, false>, at_most_groups((units + 3) / 4), 1, 256, 0,
-                                   stream, static_cast<const D*>(g.dy), g.dy_stride, g.width, totals, place, row, g.scale,
-                                   static_cast<T*>(g.grad), parts, listed, slices, g.lay.chunks);
+            const int rc2 = with_form(row_form(g.width, Traits<D>::VEC), [&](auto form) -> int {
+                constexpr RowForm F = decltype(form)::value;
+                return launch(g.accumulate ? sum_kernel<R, D, T, F, true> : sum_kernel<R, D, T, F, false>, at_most_groups((units + 3) / 4), 1, 256,
+                              0, stream, static_cast<const D*>(g.dy), g.dy_stride, g.width, totals, place, row, g.scale,
+                              static_cast<T*>(g.grad), parts, listed, slices, g.lay.chunks);
+            });
             if (rc2 != 0 || g.ids.n <= R) return rc2;   // (so few tokens make no long run)
             const int64_t most = (g.ids.n / (R + 1)) * ((g.width + 63) / 64);
             // few rows that all tokens share make few and very long runs (two rows, 16384 tokens: 9.0 us with 1024 lanes, 11.6 with 256),

@@ -94,6 +94,7 @@ int adasum_embedding(const void* params, int dtype, int64_t offset, int64_t rows
     ADASUM_CHECK(check_ids(ids, id_type, n_ids));
     ADASUM_CHECK(check_rows(out, n_ids, width, out_stride, true));
     if (n_ids == 0 || width == 0) return ADASUM_OK;
+    if (rows == 0) return ADASUM_ERR_INVALID_ARG;
     const void* const table = static_cast<const char*>(params) + offset * elem_bytes(dtype);
     const Range result = rows_range(out, n_ids, width, out_stride, out_dtype);
     if (result.meets(rows_range(table, rows, width, width, dtype)) ||

@@ -69,8 +69,16 @@ __device__ __forceinline__ void store_words_any(void* p, const unsigned int (&w)
     }
 }
 
-__device__ __forceinline__ unsigned int bits_of(bf16_t, float v) { return f32_to_bf16_rne(v); }
-__device__ __forceinline__ unsigned int bits_of(f16_t, float v) { return f32_to_f16_bits(v); }
+// Two values rounded to a 16-bit type (to nearest even, by the conversion instructions).
+__device__ __forceinline__ unsigned int rounded_pair(bf16_t, float a, float b) {
+    bf16x2_t p;
+    p.x = static_cast<__bf16>(a);
+    p.y = static_cast<__bf16>(b);
+    return __builtin_bit_cast(unsigned int, p);
+}
+__device__ __forceinline__ unsigned int rounded_pair(f16_t, float a, float b) {
+    return f32_to_f16_bits(a) | f32_to_f16_bits(b) << 16;
+}
 
 // G values to consecutive elements of T.
 template <int G, typename T, typename A>
@@ -78,7 +86,7 @@ __device__ __forceinline__ void store_any(T* p, const A (&v)[G]) {
     unsigned int w[Granule<T, G>::NW];
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < G / 2; ++i) w[i] = bits_of(T{}, v[2 * i]) | (bits_of(T{}, v[2 * i + 1]) << 16);
+        for (int i = 0; i < G / 2; ++i) w[i] = rounded_pair(T{}, v[2 * i], v[2 * i + 1]);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < G; ++i) w[i] = __float_as_uint(v[i]);
@@ -93,7 +101,8 @@ __device__ __forceinline__ void store_any(T* p, const A (&v)[G]) {
     store_words_any(p, w);
 }
 
-// `there` (1 .. G) elements of T as values, zeros behind them.
+// `there` (1 .. G) elements of T as values, zeros behind them.  (What is loaded in a branch is waited for at its end: for kernels that keep
+// many loads in flight see load_row.)
 template <int G, typename T, typename A>
 __device__ __forceinline__ void load_some(A (&v)[G], const T* p, int there) {
     if (there >= G) {
@@ -116,33 +125,69 @@ __device__ __forceinline__ void store_some(T* p, const A (&v)[G], int there) {
     }
 }
 
-// The same where FULL says that all are there, and as raw words: the values are taken out where they are used.
-template <bool FULL, typename T, int G>
-__device__ __forceinline__ void load_part(Granule<T, G>& r, const T* p, int there) {
-    if (FULL || there >= G) {
-        load_any(r, p);
+// How rows of `width` elements fall into granules of G: whole ones; a last one that is shorter, which is loaded as the row's last G elements
+// and moved down, without a branch; rows shorter than a granule, element by element.
+enum RowForm { kWhole, kRagged, kShort };
+inline RowForm row_form(int64_t width, int G) { return width % G == 0 ? kWhole : width >= G ? kRagged : kShort; }
+
+// Moves a granule's elements `by` places down.
+template <typename T, int G>
+__device__ __forceinline__ void move_down(Granule<T, G>& r, int by) {
+    constexpr int NW = Granule<T, G>::NW;
+    const int halves = by * static_cast<int>(sizeof(T) / 2);
+#pragma unroll
+    for (int step = NW / 2; step >= 1; step /= 2) {
+        const bool yes = (halves / 2) & step;
+#pragma unroll
+        for (int i = 0; i + step < NW; ++i) {
+            const unsigned here = r.w[i], there = r.w[i + step];   // (values: a choice between places would put the granule in memory)
+            r.w[i] = yes ? there : here;
+        }
+    }
+    if constexpr (sizeof(T) == 2) {
+        const bool yes = halves & 1;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const unsigned here = r.w[i], moved = here >> 16 | (i + 1 < NW ? r.w[i + 1] << 16 : 0u);
+            r.w[i] = yes ? moved : here;
+        }
+    }
+}
+
+// The granule at element `at` of a row; what lies behind the row's end is not defined (`at` may lie there too).
+template <RowForm FORM, typename T, int G>
+__device__ __forceinline__ void load_row(Granule<T, G>& r, const T* row, int at, int width) {
+    if constexpr (FORM == kWhole) {
+        load_any(r, row + (at < width ? at : 0));
+    } else if constexpr (FORM == kRagged) {
+        const int from = min(at, width - G);
+        load_any(r, row + from);
+        move_down(r, at - from);
     } else {
 #pragma unroll
         for (int w = 0; w < Granule<T, G>::NW; ++w) r.w[w] = 0;
 #pragma unroll
-        for (int i = 0; i < G; ++i)
-            if (i < there) {
-                if constexpr (sizeof(T) == 2) {
-                    r.w[i / 2] |= static_cast<unsigned>(p[i].v) << (16 * (i & 1));
-                } else if constexpr (sizeof(T) == 4) {
-                    r.w[i] = __float_as_uint(p[i]);
-                } else {
-                    const long long b = __double_as_longlong(p[i]);
-                    r.w[2 * i] = static_cast<unsigned>(b);
-                    r.w[2 * i + 1] = static_cast<unsigned>(b >> 32);
-                }
+        for (int i = 0; i < G; ++i) {
+            const T* const p = row + min(at + i, width - 1);
+            if constexpr (sizeof(T) == 2) {
+                r.w[i / 2] |= static_cast<unsigned>(p->v) << (16 * (i & 1));
+            } else if constexpr (sizeof(T) == 4) {
+                r.w[i] = __float_as_uint(*p);
+            } else {
+                const long long b = __double_as_longlong(*p);
+                r.w[2 * i] = static_cast<unsigned>(b);
+                r.w[2 * i + 1] = static_cast<unsigned>(b >> 32);
             }
+        }
     }
 }
-template <bool FULL, int G, typename T, typename A>
-__device__ __forceinline__ void store_part(T* p, const A (&v)[G], int there) {
-    if constexpr (FULL) store_any<G>(p, v);
-    else store_some<G>(p, v, there);
+template <RowForm FORM, int G, typename T, typename A>
+__device__ __forceinline__ void store_row(T* row, const A (&v)[G], int at, int width) {
+    if constexpr (FORM == kWhole) {
+        if (at < width) store_any<G>(row + at, v);
+    } else {
+        store_some<G>(row + at, v, width - at);
+    }
 }
 
 // Division of numbers below 2^31 by a fixed one, by a multiplication: q = (n * m) >> (32 + s) with
@@ -161,6 +206,15 @@ __device__ __forceinline__ unsigned divide(unsigned n, const Divider& v) {
     return static_cast<unsigned>((static_cast<unsigned long long>(__umulhi(n, v.m)) + n) >> v.s);
 }
 
+// f(form) as a constant.
+template <typename F>
+int with_form(RowForm form, F&& f) {
+    switch (form) {
+        case kWhole: return f(std::integral_constant<RowForm, kWhole>{});
+        case kRagged: return f(std::integral_constant<RowForm, kRagged>{});
+        default: return f(std::integral_constant<RowForm, kShort>{});
+    }
+}
 // f(type of a, type of b) for storage types that go together.
 template <typename F>
 int with_type(int dtype, F&& f) {

@@ -38,7 +38,7 @@ def weight_grad(lib, kept=FAR, rows=4, width=40, dy=2 * FAR, dtype=B.F32, stride
 
 
 @pytest.mark.parametrize("call, wrong", [
-    (embedding, [dict(params=None), dict(ids=None), dict(out=None), dict(offset=-1), dict(rows=-1), dict(width=-1), dict(n=-1), dict(stride=7),
+    (embedding, [dict(params=None), dict(ids=None), dict(out=None), dict(offset=-1), dict(rows=-1), dict(rows=0), dict(width=-1), dict(n=-1), dict(stride=7),
                  dict(stride=-8), dict(rows=1 << 31), dict(width=(1 << 24) + 1), dict(n=1 << 31), dict(offset=1 << 50)]),
     (embedding_grad, [dict(dy=None), dict(ids=None), dict(grad=None), dict(offset=-1), dict(rows=-1), dict(width=-1), dict(n=-1),
                       dict(stride=-1), dict(accumulate=2), dict(rows=1 << 31), dict(rows=(1 << 31) - 65536, width=1 << 24)]),
