@@ -404,20 +404,48 @@ def adasum_group_combine(xs: Sequence, layer_offsets: Sequence[int], weights, *,
 
 # ---- the gradients that fill a worker's buffer ----------------------------------------
 
+# (A call over a few rows is bound by what happens here: every look at a tensor counts.)
+_types, _ids = {}, {}    # torch.float32 .. -> F32 ..; torch.int32 .. -> ID_I32 ..; filled by the first call that needs them
+
+
+def _learn_types() -> None:
+    import torch
+    _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16, torch.float64: F64})
+    _ids.update({torch.int32: ID_I32, torch.int64: ID_I64})
+
+
+def _type_of(t) -> int:
+    if not _types:
+        _learn_types()
+    code = _types.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
+
+
+def _id_type(ids) -> int:
+    if not _ids:
+        _learn_types()
+    code = _ids.get(ids.dtype)
+    if code is None or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous int32 or int64 device tensor")
+    return code
+
+
 def _rows_of(t, width=None, what="tensor"):
-    """(rows, width, distance of two rows) of a device tensor whose last dimension is contiguous: a matrix, or any
-    contiguous tensor with its leading dimensions taken together."""
-    if not t.is_cuda:
-        raise ValueError("libadasum works on device memory only (no CPU path)")
-    if t.dim() < 2:
+    """(rows, width, distance of two rows) of a tensor whose last dimension is contiguous: a matrix, or any contiguous
+    tensor with its leading dimensions taken together."""
+    shape = t.shape
+    if len(shape) < 2:
         raise ValueError(f"{what} must have rows: at least two dimensions")
-    w = t.shape[-1]
+    w = shape[-1]
     if width is not None and w != width:
         raise ValueError(f"{what} must have rows of {width} elements")
-    if t.dim() == 2:
-        if w > 1 and t.stride(1) != 1:
+    if len(shape) == 2:
+        stride = t.stride()
+        if w > 1 and stride[1] != 1:
             raise ValueError(f"the rows of {what} must be contiguous")
-        return t.shape[0], w, t.stride(0)
+        return shape[0], w, stride[0]
     if not t.is_contiguous():
         raise ValueError(f"{what} must be a matrix or contiguous")
     return (t.numel() // w if w else 0), w, w
@@ -425,41 +453,41 @@ def _rows_of(t, width=None, what="tensor"):
 
 def _flat(t, offset, elems, what):
     """A flat buffer that holds `elems` elements at `offset`."""
-    if not t.is_cuda:
-        raise ValueError("libadasum works on device memory only (no CPU path)")
-    if t.dim() != 1 or not t.is_contiguous() or offset < 0 or offset + elems > t.numel():
+    shape = t.shape
+    if len(shape) != 1 or offset < 0 or offset + elems > shape[0] or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous 1-D buffer that holds the layer at its offset")
 
 
-def _id_type(ids) -> int:
-    import torch
-    if not ids.is_cuda or not ids.is_contiguous() or ids.dtype not in (torch.int32, torch.int64):
-        raise ValueError("ids must be a contiguous int32 or int64 device tensor")
-    return ID_I64 if ids.dtype == torch.int64 else ID_I32
-
-
-def _same_device(first, *others):
+def _device_of(first, *others) -> int:
     dev = first.get_device()
+    if dev < 0:
+        raise ValueError("libadasum works on device memory only (no CPU path)")
     for t in others:
-        if t is not None and t.get_device() != dev:
+        if t.get_device() != dev:
             raise ValueError("all tensors must be on one device")
     return dev
 
 
 def _call(fn, dev, stream, *args):
     """The library launches on the current device: make that the tensors'."""
-    import torch
-    if dev == torch.cuda.current_device():
-        check(fn(*args, _stream(stream)))
+    from torch import _C
+    raw = getattr(_C, "_cuda_getCurrentRawStream", None)
+    if raw is not None and stream is None and _C._cuda_getDevice() == dev:
+        code = fn(*args, raw(dev))
     else:
+        import torch
         with torch.cuda.device(dev):
-            check(fn(*args, _stream(stream)))
+            code = fn(*args, _stream(stream))
+    if code != OK:
+        check(code)
 
 
 def _empty(shape, dtype, dev, stream):
     """A new tensor for work on `stream` (None: the device's current one): memory of that stream, so that nothing that still
     runs on another has it."""
     import torch
+    if dev < 0:
+        raise ValueError("libadasum works on device memory only (no CPU path)")
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=dev)
     with torch.cuda.stream(stream):
@@ -467,22 +495,23 @@ def _empty(shape, dtype, dev, stream):
 
 
 def _scratch(workspace, need, dev, stream):
+    """(address, bytes) of the workspace, which is made here when None, and what keeps it alive."""
     import torch
     if workspace is None:
-        return _empty(need, torch.uint8, dev, stream) if need else None
+        n = need()
+        if n == 0:
+            return None, 0, None
+        workspace = _empty(n, torch.uint8, dev, stream)
+        return workspace.data_ptr(), n, workspace
     if workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the device of the operands")
-    return workspace
-
-
-def _address(t):
-    return None if t is None else t.data_ptr()
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def adasum_embedding(params, offset: int, rows: int, width: int, ids, *, scale: float = 1.0, out=None, out_dtype=None, stream=None):
     """``scale * table[ids]`` for the table of ``rows`` x ``width`` that lies at ``offset`` of the flat buffer ``params``; rows of
     zeros where an id names no row.  Returns ``out``, [*ids.shape, width] (made here when None)."""
-    lib = load()
+    lib = _lib or load()
     _flat(params, offset, rows * width, "params")
     id_type = _id_type(ids)
     n = ids.numel()
@@ -495,9 +524,9 @@ def adasum_embedding(params, offset: int, rows: int, width: int, ids, *, scale: 
         have, _, stride = _rows_of(out, width, "out")
         if have != n and width:
             raise ValueError("out must have a row for every id")
-    dev = _same_device(params, ids, out)
-    _call(lib.adasum_embedding, dev, stream, params.data_ptr(), _dtype_code(params), offset, rows, width, ids.data_ptr(), id_type, n, scale,
-          out.data_ptr(), _dtype_code(out), stride)
+    dev = _device_of(params, ids, out)
+    _call(lib.adasum_embedding, dev, stream, params.data_ptr(), _type_of(params), offset, rows, width, ids.data_ptr(), id_type, n, scale,
+          out.data_ptr(), _type_of(out), stride)
     return out
 
 
@@ -511,21 +540,17 @@ def adasum_embedding_grad(dy, ids, grad, offset: int, rows: int, *, scale: float
                           stream=None):
     """Writes (or, with ``accumulate``, adds) the gradient of a table of ``rows`` rows, ``scale`` times the sums of the rows of ``dy``
     ([*ids.shape, width]) with one id, at ``offset`` of the flat buffer ``grad``.  Returns ``grad``."""
-    lib = load()
+    lib = _lib or load()
     n, width, stride = _rows_of(dy, None, "dy")
     id_type = _id_type(ids)
     if ids.numel() != n and width:
         raise ValueError("dy must have a row for every id")
     _flat(grad, offset, rows * width, "grad")
-    dev = _same_device(grad, dy, ids)
-    code = _dtype_code(dy)
-    if workspace is None:
-        workspace = _scratch(None, adasum_embedding_grad_workspace_bytes(rows, width, n, dy.dtype), dev, stream)
-    else:
-        workspace = _scratch(workspace, 0, dev, stream)
+    dev = _device_of(grad, dy, ids)
+    code = _type_of(dy)
+    ws, ws_bytes, _keep = _scratch(workspace, lambda: adasum_embedding_grad_workspace_bytes(rows, width, n, dy.dtype), dev, stream)
     _call(lib.adasum_embedding_grad, dev, stream, dy.data_ptr(), code, stride, ids.data_ptr(), id_type, n, scale, grad.data_ptr(),
-          _dtype_code(grad), offset, rows, width, 1 if accumulate else 0, _address(workspace),
-          0 if workspace is None else workspace.numel() * workspace.element_size())
+          _type_of(grad), offset, rows, width, 1 if accumulate else 0, ws, ws_bytes)
     return grad
 
 
@@ -539,6 +564,7 @@ class Checkpoint:
         check(load().adasum_checkpoint_bytes(rows, width, C.byref(n)))
         if dtype not in (torch.float32, torch.bfloat16, torch.float16):
             raise ValueError("checkpoints hold float32, bfloat16 or float16 activations")
+        self.code = _code_of(dtype)
         if data is None:
             data = torch.empty(n.value, dtype=torch.int8, device="cuda" if device is None else device)
         elif data.dim() != 1 or data.element_size() != 1 or data.numel() != n.value or not data.is_contiguous():
@@ -548,17 +574,17 @@ class Checkpoint:
 
 def adasum_checkpoint_store(x, *, out: Optional[Checkpoint] = None, stream=None) -> Checkpoint:
     """Keeps ``x`` ([..., width]) in 8 bits.  Returns the checkpoint (made here when None)."""
-    lib = load()
+    lib = _lib or load()
     n, width, stride = _rows_of(x, None, "x")
     if out is None:
         size = C.c_size_t(0)
         check(lib.adasum_checkpoint_bytes(n, width, C.byref(size)))
         import torch
         out = Checkpoint(n, width, x.dtype, data=_empty(size.value, torch.int8, x.get_device(), stream))
-    elif (out.rows, out.width, out.dtype) != (n, width, x.dtype):
+    elif out.rows != n or out.width != width or out.dtype != x.dtype:
         raise ValueError("the checkpoint was made for another shape or dtype")
-    dev = _same_device(x, out.data)
-    _call(lib.adasum_checkpoint_store, dev, stream, x.data_ptr(), _dtype_code(x), stride, n, width, out.data.data_ptr())
+    dev = _device_of(x, out.data)
+    _call(lib.adasum_checkpoint_store, dev, stream, x.data_ptr(), _type_of(x), stride, n, width, out.data.data_ptr())
     return out
 
 
@@ -569,9 +595,9 @@ def adasum_checkpoint_load(checkpoint: Checkpoint, *, out=None, stream=None):
     n, width, stride = _rows_of(out, checkpoint.width, "out")
     if n != checkpoint.rows and width:
         raise ValueError("out must have a row for every one of the checkpoint")
-    dev = _same_device(checkpoint.data, out)
-    _call(load().adasum_checkpoint_load, dev, stream, checkpoint.data.data_ptr(), checkpoint.rows, checkpoint.width, out.data_ptr(),
-          _dtype_code(out), stride)
+    dev = _device_of(checkpoint.data, out)
+    _call((_lib or load()).adasum_checkpoint_load, dev, stream, checkpoint.data.data_ptr(), checkpoint.rows, checkpoint.width, out.data_ptr(),
+          _type_of(out), stride)
     return out
 
 
@@ -588,8 +614,8 @@ def adasum_checkpoint_act_grad(checkpoint: Checkpoint, dy, act: str, *, out=None
     m, _, out_stride = _rows_of(out, width, "out")
     if (m != n and width) or out.dtype != dy.dtype:
         raise ValueError("out must have the rows and dtype of dy")
-    dev = _same_device(checkpoint.data, dy, out)
-    _call(load().adasum_checkpoint_act_grad, dev, stream, checkpoint.data.data_ptr(), n, width, ACTS[act], dy.data_ptr(), _dtype_code(dy),
+    dev = _device_of(checkpoint.data, dy, out)
+    _call((_lib or load()).adasum_checkpoint_act_grad, dev, stream, checkpoint.data.data_ptr(), n, width, ACTS[act], dy.data_ptr(), _type_of(dy),
           stride, out.data_ptr(), out_stride)
     return out
 
@@ -604,26 +630,23 @@ def adasum_checkpoint_weight_grad(checkpoint: Checkpoint, dy, grad, offset: int,
                                   accumulate: bool = False, workspace=None, stream=None):
     """Writes (or adds) the gradient of a linear layer's weight, [outputs, width], at ``offset`` of the flat buffer ``grad``, and that
     of its bias at ``bias_offset`` (None: it has none), from the kept input and ``dy`` ([..., outputs]).  Returns ``grad``."""
-    import torch
-    lib = load()
+    lib = _lib or load()
     n, outputs, stride = _rows_of(dy, None, "dy")
     width = checkpoint.width
     if n != checkpoint.rows and outputs:
         raise ValueError("dy must have a row for every one of the checkpoint")
-    if dy.dtype == torch.float16 and checkpoint.dtype != torch.float16:
+    code = _type_of(dy)
+    if code == F16 and checkpoint.code != F16:
         raise ValueError("a float16 dy needs a checkpoint of float16 activations")
     _flat(grad, offset, outputs * width, "grad")
     if bias_offset is not None:
         _flat(grad, bias_offset, outputs, "grad")
-    dev = _same_device(grad, checkpoint.data, dy)
-    code = _dtype_code(dy)
-    if workspace is None:
-        workspace = _scratch(None, adasum_checkpoint_weight_grad_workspace_bytes(checkpoint.rows, width, outputs, dy.dtype), dev, stream)
-    else:
-        workspace = _scratch(workspace, 0, dev, stream)
+    dev = _device_of(grad, checkpoint.data, dy)
+    ws, ws_bytes, _keep = _scratch(
+        workspace, lambda: adasum_checkpoint_weight_grad_workspace_bytes(checkpoint.rows, width, outputs, dy.dtype), dev, stream)
     _call(lib.adasum_checkpoint_weight_grad, dev, stream, checkpoint.data.data_ptr(), checkpoint.rows, width, dy.data_ptr(), code, stride,
-          outputs, grad.data_ptr(), _dtype_code(grad), offset, -1 if bias_offset is None else bias_offset, 1 if accumulate else 0,
-          _address(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size())
+          outputs, grad.data_ptr(), _type_of(grad), offset, -1 if bias_offset is None else bias_offset, 1 if accumulate else 0,
+          ws, ws_bytes)
     return grad
 
 
