@@ -104,13 +104,15 @@ template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 store_kernel(const T* __restrict__ x, long long stride, int width, long long pitch, signed char* __restrict__ q, signed char* __restrict__ e,
              RowWork work) {
+    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
+    constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
             Granule<T, kG> raw[ITEMS];
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
                 const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
-                load_row<FORM>(raw[k], x + p.row * stride, p.at, width);
+                load_row<FORM, NT>(raw[k], x + p.row * stride, p.at, width);
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
@@ -149,6 +151,8 @@ template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 load_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, T* __restrict__ out,
             long long stride, RowWork work) {
+    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
+    constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
             u32x2 kept[ITEMS];
@@ -166,7 +170,7 @@ load_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e
                     const Place p = place_of(work, first, g);
                     float v[kG];
                     kept_values(v, kept[k], step_of(exponent[k]));
-                    store_row<FORM>(out + p.row * stride, v, p.at, width);
+                    store_row<FORM, NT>(out + p.row * stride, v, p.at, width);
                 }
             }
         }
@@ -178,6 +182,8 @@ template <typename T, int ACT, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, const T* dy,
                 long long dy_stride, T* dx, long long dx_stride, RowWork work) {
+    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
+    constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
             u32x2 kept[ITEMS];
@@ -188,7 +194,7 @@ act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict
                 const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
                 kept[k] = *reinterpret_cast<const u32x2*>(q + p.row * pitch + p.at);
                 exponent[k] = e[p.row * (pitch / kBlock) + p.at / kBlock];
-                load_row<FORM>(raw[k], dy + p.row * dy_stride, p.at, width);
+                load_row<FORM, NT>(raw[k], dy + p.row * dy_stride, p.at, width);
             }
 #pragma unroll
             for (int k = 0; k < ITEMS; ++k) {
@@ -200,7 +206,7 @@ act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict
                     unpack(raw[k], d);
 #pragma unroll
                     for (int i = 0; i < kG; ++i) v[i] = d[i] * slope<ACT>(v[i]);
-                    store_row<FORM>(dx + p.row * dx_stride, v, p.at, width);
+                    store_row<FORM, NT>(dx + p.row * dx_stride, v, p.at, width);
                 }
             }
         }

@@ -49,7 +49,7 @@ lookup_kernel(const T* __restrict__ table, unsigned rows, int width, Ids ids, ty
                 unpack(raw[k], v);
 #pragma unroll
                 for (int i = 0; i < G; ++i) v[i] = id[k] < rows ? v[i] * scale : A(0);
-                if (base + 256 * k < work) store_row<FORM>(out + (first + t[k]) * out_stride, v, at[k], width);
+                if (base + 256 * k < work) store_row<FORM, (ITEMS > 1)>(out + (first + t[k]) * out_stride, v, at[k], width);
             }
         }
     }
@@ -76,7 +76,7 @@ __device__ __forceinline__ void clear_table(long long block, long long blocks, c
         for (int k = threadIdx.x; k < kClearBytes / 16; k += static_cast<int>(blockDim.x)) {
             const long long at = from + 16ll * k;
             if (at + 16 <= clear_bytes) {
-                store_words_any(clear + at, zero);
+                store_words_any<true>(clear + at, zero);
             } else {
                 for (long long b = at; b < clear_bytes; b += 2) *reinterpret_cast<unsigned short*>(clear + b) = 0;
             }
@@ -431,10 +431,10 @@ gather_kernel(unsigned per_group, int row_bits, int n_parts, const int* __restri
 }
 
 // Where every range has one row only, its tokens are sorted as they are: workgroup (range, piece) moves those of the parts of its piece, a
-// wave a part.
-constexpr int kPieceParts = 4;
+// wave a part, and at most kPieces pieces.
+constexpr int kPieces = 1024;
 __global__ void __launch_bounds__(256)
-move_kernel(int n_parts, int pieces, const int* __restrict__ begins, const int* __restrict__ part_place, int* __restrict__ totals,
+move_kernel(int n_parts, int pieces, int piece_parts, const int* __restrict__ begins, const int* __restrict__ part_place, int* __restrict__ totals,
             int* __restrict__ place, int* __restrict__ row, int groups, char* __restrict__ clear, long long clear_bytes) {
     if (static_cast<int>(blockIdx.x) >= groups) {
         clear_table(blockIdx.x - groups, gridDim.x - groups, clear, clear_bytes);
@@ -442,7 +442,7 @@ move_kernel(int n_parts, int pieces, const int* __restrict__ begins, const int* 
     }
     __shared__ int shared[3][4];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int range = static_cast<int>(blockIdx.x) / pieces, first = static_cast<int>(blockIdx.x) % pieces * kPieceParts;
+    const int range = static_cast<int>(blockIdx.x) / pieces, first = static_cast<int>(blockIdx.x) % pieces * piece_parts;
     const int* const begin_here = begins + static_cast<int64_t>(range) * n_parts;
     const int* const begin_next = begin_here + n_parts;
     // tokens of the ranges before this one, of this one in the parts before, and of all ranges
@@ -465,7 +465,7 @@ move_kernel(int n_parts, int pieces, const int* __restrict__ begins, const int* 
     }
     int to = 0;
     for (int w = 0; w < 4; ++w) to += shared[0][w] + shared[1][w];
-    for (int p = first; p < min(first + kPieceParts, n_parts); ++p) {
+    for (int p = first; p < min(first + piece_parts, n_parts); ++p) {
         const int b = begin_here[p], n = begin_next[p] - b;
         if ((p & 3) == wave)
 #pragma unroll 8
@@ -592,7 +592,7 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
 #pragma unroll
                         for (int j = 0; j < G; ++j) sum[j] += o[j];
                     }
-                    store_row<FORM>(grad + static_cast<long long>(w.row_at(i)) * width, sum, at, width);
+                    store_row<FORM, true>(grad + static_cast<long long>(w.row_at(i)) * width, sum, at, width);
                 }
 #pragma unroll
                 for (int j = 0; j < G; ++j) sum[j] = A(0);
@@ -742,8 +742,9 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
         if (rc != 0) return rc;
         const int64_t clearing = at_most_groups((clear_bytes - half + kClearBytes - 1) / kClearBytes);
         if (per_group == 1) {
-            const int64_t pieces = (n_parts + kPieceParts - 1) / kPieceParts, groups = g.rows * pieces;
-            rc = launch(move_kernel, groups + clearing, 1, 256, 0, stream, n_parts, pieces, begins, part_place, totals, place, row, groups,
+            const int64_t piece_parts = n_parts <= 4 * kPieces ? 4 : (n_parts + kPieces - 1) / kPieces;
+            const int64_t pieces = (n_parts + piece_parts - 1) / piece_parts, groups = g.rows * pieces;
+            rc = launch(move_kernel, groups + clearing, 1, 256, 0, stream, n_parts, pieces, piece_parts, begins, part_place, totals, place, row, groups,
                         clear + half, clear_bytes - half);
         } else {
             rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(gather_kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
@@ -782,7 +783,10 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
             // few rows that all tokens share make few and very long runs (two rows, 16384 tokens: 9.0 us with 1024 lanes, 11.6 with 256),
             // otherwise most of those that are long are so by little (30522 rows, 65501 tokens: 17.3 us and 7.4)
             const bool few = g.ids.n > 256 * g.rows;
-            return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < 1024 ? most : 1024, 1, few ? 1024 : 256, 0, stream,
+            // and where rows have sixteen tokens on average, many are long (512 rows, 65536 tokens: @@ us with up to 8192 workgroups, 70.6
+            // with 1024); else workgroups that find nothing would only cost time
+            const int64_t at_most = g.ids.n >= 16 * g.rows ? 8192 : 1024;
+            return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < at_most ? most : at_most, 1, few ? 1024 : 256, 0, stream,
                           g.width, totals, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, listed);
         };
         return g.lay.run == 16 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 32>{});

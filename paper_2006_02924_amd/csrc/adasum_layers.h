@@ -33,7 +33,7 @@ constexpr int64_t kFewTokens = 32768;
 // Workgroups that sort: each takes an equal range of rows, at most kSortRows where it reads all tokens itself and at most kGatherRows
 // where the tokens have been sorted by range before, in parts of kPartTokens.
 constexpr int kSortGroups = 256;
-constexpr int kSortRows = 512;
+constexpr int kSortRows = 1008;   // (their counts take just under 64 KB)
 constexpr int kGatherRows = 1024;
 constexpr int kPartTokens = 2048;
 inline int64_t sort_rows(int64_t rows) {

@@ -30,17 +30,24 @@ inline int64_t at_most_groups(int64_t groups) { return groups < kMostGroups ? gr
 typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
-template <typename T, int G>
+template <bool NT, typename V>
+__device__ __forceinline__ V through(const V* p) {
+    if constexpr (NT) return stream_load(p);
+    else return *p;
+}
+
+// NT: what is used once passes the caches by (streams of many megabytes; see the kernels for what that gave).
+template <bool NT = false, typename T, int G>
 __device__ __forceinline__ void load_any(Granule<T, G>& r, const T* p) {
     constexpr int NW = Granule<T, G>::NW;
     if constexpr (NW == 2) {
-        const u32x2_any q = *reinterpret_cast<const u32x2_any*>(p);
+        const u32x2_any q = through<NT>(reinterpret_cast<const u32x2_any*>(p));
         r.w[0] = q.x;
         r.w[1] = q.y;
     } else {
 #pragma unroll
         for (int i = 0; i < NW / 4; ++i) {
-            const u32x4_any q = *(reinterpret_cast<const u32x4_any*>(p) + i);
+            const u32x4_any q = through<NT>(reinterpret_cast<const u32x4_any*>(p) + i);
             r.w[4 * i + 0] = q.x;
             r.w[4 * i + 1] = q.y;
             r.w[4 * i + 2] = q.z;
@@ -49,13 +56,13 @@ __device__ __forceinline__ void load_any(Granule<T, G>& r, const T* p) {
     }
 }
 
-template <int NW>
+template <bool NT = false, int NW>
 __device__ __forceinline__ void store_words_any(void* p, const unsigned int (&w)[NW]) {
     if constexpr (NW == 2) {
         u32x2_any q;
         q.x = w[0];
         q.y = w[1];
-        *reinterpret_cast<u32x2_any*>(p) = q;
+        stream_store<NT>(q, reinterpret_cast<u32x2_any*>(p));
     } else {
 #pragma unroll
         for (int i = 0; i < NW / 4; ++i) {
@@ -64,7 +71,7 @@ __device__ __forceinline__ void store_words_any(void* p, const unsigned int (&w)
             q.y = w[4 * i + 1];
             q.z = w[4 * i + 2];
             q.w = w[4 * i + 3];
-            *(reinterpret_cast<u32x4_any*>(p) + i) = q;
+            stream_store<NT>(q, reinterpret_cast<u32x4_any*>(p) + i);
         }
     }
 }
@@ -81,7 +88,7 @@ __device__ __forceinline__ unsigned int rounded_pair(f16_t, float a, float b) {
 }
 
 // G values to consecutive elements of T.
-template <int G, typename T, typename A>
+template <int G, bool NT = false, typename T, typename A>
 __device__ __forceinline__ void store_any(T* p, const A (&v)[G]) {
     unsigned int w[Granule<T, G>::NW];
     if constexpr (sizeof(T) == 2) {
@@ -98,7 +105,7 @@ __device__ __forceinline__ void store_any(T* p, const A (&v)[G]) {
             w[2 * i + 1] = static_cast<unsigned int>(b >> 32);
         }
     }
-    store_words_any(p, w);
+    store_words_any<NT>(p, w);
 }
 
 // `there` (1 .. G) elements of T as values, zeros behind them.  (What is loaded in a branch is waited for at its end: for kernels that keep
@@ -114,10 +121,10 @@ __device__ __forceinline__ void load_some(A (&v)[G], const T* p, int there) {
         for (int i = 0; i < G; ++i) v[i] = i < there ? load_elem(p + i) : A(0);
     }
 }
-template <int G, typename T, typename A>
+template <int G, bool NT = false, typename T, typename A>
 __device__ __forceinline__ void store_some(T* p, const A (&v)[G], int there) {
     if (there >= G) {
-        store_any<G>(p, v);
+        store_any<G, NT>(p, v);
     } else {
 #pragma unroll
         for (int i = 0; i < G; ++i)
@@ -155,13 +162,13 @@ __device__ __forceinline__ void move_down(Granule<T, G>& r, int by) {
 }
 
 // The granule at element `at` of a row; what lies behind the row's end is not defined (`at` may lie there too).
-template <RowForm FORM, typename T, int G>
+template <RowForm FORM, bool NT = false, typename T, int G>
 __device__ __forceinline__ void load_row(Granule<T, G>& r, const T* row, int at, int width) {
     if constexpr (FORM == kWhole) {
-        load_any(r, row + (at < width ? at : 0));
+        load_any<NT>(r, row + (at < width ? at : 0));
     } else if constexpr (FORM == kRagged) {
         const int from = min(at, width - G);
-        load_any(r, row + from);
+        load_any<NT>(r, row + from);
         move_down(r, at - from);
     } else {
 #pragma unroll
@@ -181,12 +188,12 @@ __device__ __forceinline__ void load_row(Granule<T, G>& r, const T* row, int at,
         }
     }
 }
-template <RowForm FORM, int G, typename T, typename A>
+template <RowForm FORM, bool NT = false, int G, typename T, typename A>
 __device__ __forceinline__ void store_row(T* row, const A (&v)[G], int at, int width) {
     if constexpr (FORM == kWhole) {
-        if (at < width) store_any<G>(row + at, v);
+        if (at < width) store_any<G, NT>(row + at, v);
     } else {
-        store_some<G>(row + at, v, width - at);
+        store_some<G, NT>(row + at, v, width - at);
     }
 }
 

@@ -166,7 +166,7 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("n, rows, width", [(50000, 30522, 256), (70001, 2, 1024), (20000, 140001, 8), (9000, 262144, 8), (20000, 300001, 8),
-                                            (4096, 5000, 40), (4097, 5000, 40), (2200000, 300, 8), (30000, 1, 72)])
+                                            (4096, 5000, 40), (4097, 5000, 40), (2200000, 300, 8), (30000, 1, 72), (8500000, 3, 1), (3000, 300001, 9)])
 def test_larger_sums_are_right_and_the_same_every_time(n, rows, width):
     """More tokens than the sort takes at once, in every row or in a few, and tables on both sides of its limits."""
     g = torch.Generator().manual_seed(n)
