@@ -302,10 +302,15 @@ gather_kernel(unsigned per_group, int row_bits, int n_parts, const int* __restri
     int* const next = counts + kSortWaves * per_group;
     const lds_counts mine = (lds_counts)(counts + wave * per_group);
     // tokens of the ranges before this one, and of those up to it
-    int below = 0, upto = 0;
+    int below = 0, upto = 0, first_here = 0, first_next = 0;
     for (int p = threadIdx.x; p < n_parts; p += kSortThreads) {
-        below += begin_here[p];
-        upto += begin_next[p];
+        const int b = begin_here[p], e = begin_next[p];
+        if (p < kSortThreads) {
+            first_here = b;
+            first_next = e;
+        }
+        below += b;
+        upto += e;
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) {
@@ -332,13 +337,16 @@ gather_kernel(unsigned per_group, int row_bits, int n_parts, const int* __restri
     }
     if (all_here == 0) return;
     for (unsigned r = threadIdx.x; r < per_group; r += kSortThreads) next[r] = 0;
+    // the search for a token's part begins with half of a power of two that is no less than the parts in hand
+    const int half_parts = n_parts >= kSortThreads ? kSortThreads / 2 : n_parts > 1 ? 1 << (31 - __builtin_clz(n_parts - 1)) : 0;
     int token[kGatherBatch], rank[kGatherBatch];
     unsigned key[kGatherBatch];
     // f() for every `at_once` tokens of the range, in order: then a wave has consecutive ones, 64 at a time
     auto every = [&](auto&& f) {
         for (int p0 = 0; p0 < n_parts; p0 += kSortThreads) {
             const int p = p0 + static_cast<int>(threadIdx.x);
-            const int b = p < n_parts ? begin_here[p] : 0, n = p < n_parts ? begin_next[p] - b : 0;
+            const bool later = p0 > 0 && p < n_parts;
+            const int b = later ? begin_here[p] : p0 > 0 ? 0 : first_here, n = (later ? begin_next[p] : p0 > 0 ? 0 : first_next) - b;
             int all = 0;
             const int before = scan_before<kSortWaves>(n, scan, all);
             length[threadIdx.x] = before;
@@ -353,8 +361,7 @@ gather_kernel(unsigned per_group, int row_bits, int n_parts, const int* __restri
                     if (k < rounds && e < all) {
                         // the part that has it: the last one that begins at or before it
                         int q = 0;
-#pragma unroll
-                        for (int step = kSortThreads / 2; step > 0; step >>= 1)
+                        for (int step = half_parts; step > 0; step >>= 1)
                             if (length[q + step] <= e) q += step;
                         const int64_t from = static_cast<int64_t>(p0 + q) * kPartTokens + source[q] + (e - length[q]);
                         token[k] = part_place[from];
@@ -783,7 +790,7 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
             // few rows that all tokens share make few and very long runs (two rows, 16384 tokens: 9.0 us with 1024 lanes, 11.6 with 256),
             // otherwise most of those that are long are so by little (30522 rows, 65501 tokens: 17.3 us and 7.4)
             const bool few = g.ids.n > 256 * g.rows;
-            // and where rows have sixteen tokens on average, many are long (512 rows, 65536 tokens: @@ us with up to 8192 workgroups, 70.6
+            // and where rows have sixteen tokens on average, many are long (512 rows, 65536 tokens: 67.4 us with up to 8192 workgroups, 70.6
             // with 1024); else workgroups that find nothing would only cost time
             const int64_t at_most = g.ids.n >= 16 * g.rows ? 8192 : 1024;
             return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < at_most ? most : at_most, 1, few ? 1024 : 256, 0, stream,
