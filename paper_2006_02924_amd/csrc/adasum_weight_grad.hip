@@ -4,6 +4,7 @@
 #include "adasum_layers.h"
 #include "adasum_rows.h"
 
+
 namespace adasum {
 namespace {
 
@@ -122,10 +123,10 @@ __device__ __forceinline__ void to_lds(char* at, int plane_bytes, const Granule<
 }
 template <typename E>
 __device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) {
-    const float step = !there ? 0.f : __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
     unsigned word[4] = {q.x, q.y, q.z, q.w};
     // (here and not before: the compiler would take the bytes apart where they are loaded, and wait for the load there)
-    asm volatile("" : "+v"(word[0]), "+v"(word[1]), "+v"(word[2]), "+v"(word[3]));
+    asm volatile("" : "+v"(word[0]), "+v"(word[1]), "+v"(word[2]), "+v"(word[3]), "+v"(e));
+    const float step = !there ? 0.f : __uint_as_float(e == -128 ? 0x7fc00000u : static_cast<unsigned>(e + 127) << 23);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         u32x4 w;
@@ -298,6 +299,15 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
                            write_b(k, buffer ^ 1, true);
                            load_b(k);
                        });
+                // what there is to do on the vector units, six instructions at a time, between the matrix cores': left to itself the
+                // compiler puts much of it before or behind them (32768 x 4096 x 4096 bf16 1038 -> 1017 us)
+                if constexpr (P == 1) {
+#pragma unroll
+                    for (int k = 0; k < FO * FI; ++k) {
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
+                    }
+                }
             }
             end_run();
             if constexpr (SETS == 1) __syncthreads();
@@ -359,32 +369,65 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             }
         }
     }
-    // a lane holds four consecutive channels of one output
+    // four consecutive channels of one output
+    auto put = [&](int to, int ti, float (&v)[4]) {
+        if (to >= outputs || ti >= width) return;
+        const long long at = static_cast<long long>(to) * width + ti;
+        if (parts != nullptr) {
+            store_some<4>(parts + static_cast<long long>(part) * outputs * width + at, v, width - ti);
+        } else {
+            if (accumulate) {
+                float old[4];
+                load_some<4>(old, grad + at, width - ti);
 #pragma unroll
-    for (int m = 0; m < FO; ++m)
+                for (int j = 0; j < 4; ++j) v[j] += old[j];
+            }
+            store_some<4>(grad + at, v, width - ti);
+        }
+    };
+    // A lane has such fours of 32 outputs apart.  Through LDS, a wave's 32 outputs at a time, consecutive lanes get consecutive channels
+    // to store: 16384 x 4096 x 1024 bf16 175 -> 168 us.  The smaller square, whose workgroups come and
+    // go beside another's products, is faster without (1024 x 4096 x 1024: 20.6 us and 22.1).
+    if constexpr (TILE == 256) {
+        constexpr int kRow = 32 * FI + 4, kLanes = 8 * FI;   // floats a row takes; lanes that store one
+        static_assert(S::threads / 64 * 32 * kRow * 4 <= S::lds_bytes, "the waves' rows fit");
+        float* const rows_of_wave = reinterpret_cast<float*>(lds) + wave * (32 * kRow);
 #pragma unroll
-        for (int k = 0; k < FI; ++k)
+        for (int m = 0; m < FO; ++m) {
+            __syncthreads();
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int to = o0 + wo + 32 * m + (lane & 31), ti = i0 + wi + 32 * k + 8 * r + 4 * (lane >> 5);
-                if (to < outputs && ti < width) {
+            for (int k = 0; k < FI; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    u32x4 w;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(acc[m][k][4 * r + j]);
+                    *reinterpret_cast<u32x4*>(rows_of_wave + (lane & 31) * kRow + 32 * k + 8 * r + 4 * (lane >> 5)) = w;
+                }
+            __syncthreads();
+#pragma unroll 4
+            for (int n = lane; n < 32 * kLanes; n += 64) {
+                const int row = n / kLanes, col = 4 * (n % kLanes);
+                const u32x4 w = *reinterpret_cast<const u32x4*>(rows_of_wave + row * kRow + col);
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
+                put(o0 + wo + 32 * m + row, i0 + wi + col, v);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < FO; ++m)
+#pragma unroll
+            for (int k = 0; k < FI; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
                     float v[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) v[j] = acc[m][k][4 * r + j];
-                    const long long at = static_cast<long long>(to) * width + ti;
-                    if (parts != nullptr) {
-                        store_some<4>(parts + static_cast<long long>(part) * outputs * width + at, v, width - ti);
-                    } else {
-                        if (accumulate) {
-                            float old[4];
-                            load_some<4>(old, grad + at, width - ti);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) v[j] += old[j];
-                        }
-                        store_some<4>(grad + at, v, width - ti);
-                    }
+                    put(o0 + wo + 32 * m + (lane & 31), i0 + wi + 32 * k + 8 * r + 4 * (lane >> 5), v);
                 }
-            }
+    }
 }
 
 // out (+)= the sum of the parts, in a fixed order: the weight's in the first `groups` workgroups, the bias's in the others.  WAYS waves
