@@ -599,7 +599,7 @@ sum_chunk(long long chunk, int slice, int lane, const D* __restrict__ dy, long l
 #pragma unroll
                         for (int j = 0; j < G; ++j) sum[j] += o[j];
                     }
-                    store_row<FORM, true>(grad + static_cast<long long>(w.row_at(i)) * width, sum, at, width);
+                    store_row<FORM>(grad + static_cast<long long>(w.row_at(i)) * width, sum, at, width);
                 }
 #pragma unroll
                 for (int j = 0; j < G; ++j) sum[j] = A(0);
