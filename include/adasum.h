@@ -40,6 +40,9 @@
  * workers; squares that overflow make it NaN.  Other layers are unaffected.  Gradients, with
  * or without loss scaling, are many orders of magnitude inside the range.
  *
+ * Beside the reduction: operators that fill a worker's gradient buffer (embedding tables, linear layers from activations kept in
+ * 8 bits), see "the gradients that fill a worker's buffer" below.
+ *
  * Conventions for every entry point
  *   - returns ADASUM_OK (0) or a negative ADASUM_ERR_* code; never throws,
  *     aborts or prints.  All argument validation happens before any device

@@ -141,12 +141,20 @@ __device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) 
     }
 }
 
-// A workgroup of four waves: TILE x TILE of dW over one part of the tokens, each wave a quarter.
+// TILE x TILE of dW over one part of the tokens: eight waves of 64 x 128 or four of 64 x 64.
 //
 // Both operands lie with the tokens in rows, and the matrix cores want eight tokens of a channel in a lane: a step of both is staged in
 // LDS as it lies in memory (x as the values it stands for), and read with the transposing LDS read.  While a step is multiplied out of
 // one buffer, the next one, which is in registers by then, is written into the other and the loads of the one after are issued, a
 // part of them beside every sixteen tokens' products.  One barrier a step.
+//
+// What bounds it: the products.  65536 x 4096 x 4096 in bf16 takes 1.80 - 2.03 ms (1.08 - 1.22 PFLOP/s; a library product of 8192^3 reaches
+// 1.19 on this card, and 0.83 on the 16384 x 4096 x 1024 that this kernel does at 0.92 - 0.98 with the join), fp32, three products for one,
+// 4096 x 1024 x 4096 113 - 118 us (0.9 PFLOP/s of bf16 products).  The matrix cores are busy 60 % of the cycles, of which there are 1.6e9 a
+// second then: the card lowers its clock, so what is taken off the other units pays little.  Four waves of 128 x 128 read a third less LDS
+// but leave the vector unit's 280 instructions a step beside 64 of the matrix core to one wave, which cannot issue both (44 % of the
+// cycles).  With parts, what they store and the join reads is 16 bytes per weight for four parts: some 25 us of 16384 x 4096 x 1024's
+// 141 - 168.  Products of the two 16-bit types are exact in fp32; the cores' sums were not found to drift (40000 terms of one sign).
 template <typename D, typename T, int TILE>
 __global__ void __launch_bounds__((GradShape<D, TILE>::threads), 2)
 weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
@@ -214,7 +222,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         f.w = h.y;
         return f;
     };
-        // two sets of operands: the next sixteen tokens' are read beside this one's products.  (With fp32's three parts there is enough to
+    // two sets of operands: the next sixteen tokens' are read beside this one's products.  (With fp32's three parts there is enough to
     // do beside one set's reads: 117 us for 122, 4096 x 1024 x 4096.)
     constexpr int SETS = P == 3 ? 1 : 2;
     u32x4 fa[SETS][FO], fb[SETS][FI];
