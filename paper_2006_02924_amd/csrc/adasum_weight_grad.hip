@@ -100,18 +100,18 @@ struct GradShape {
     static constexpr int lds_bytes = 2 * buffer_bytes;
 };
 
-// Eight elements of dy, and sixteen of x, to LDS (zeros where there is no such token).
+// Eight elements of dy, and sixteen of x (zeros where there is no such token), to LDS.
 template <typename D>
-__device__ __forceinline__ void to_lds(char* at, int plane_bytes, const Granule<D, 8>& g, bool there) {
+__device__ __forceinline__ void to_lds(char* at, int plane_bytes, const Granule<D, 8>& g) {
     if constexpr (sizeof(D) == 2) {
         u32x4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = there ? g.w[i] : 0u;
+        for (int i = 0; i < 4; ++i) w[i] = g.w[i];
         *reinterpret_cast<u32x4*>(at) = w;
     } else {
         Parts3 s[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = parts_of(there ? g.w[i] : 0u);
+        for (int i = 0; i < 8; ++i) s[i] = parts_of(g.w[i]);
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
             u32x4 w;
@@ -155,7 +155,9 @@ __device__ __forceinline__ void to_lds(E, char* at, u32x4 q, int e, bool there) 
 // but leave the vector unit's 280 instructions a step beside 64 of the matrix core to one wave, which cannot issue both (44 % of the
 // cycles).  With parts, what they store and the join reads is 16 bytes per weight for four parts: some 25 us of 16384 x 4096 x 1024's
 // 141 - 168.  Products of the two 16-bit types are exact in fp32; the cores' sums were not found to drift (40000 terms of one sign).
-template <typename D, typename T, int TILE>
+// RAGGED: outputs that are no multiple of eight; the last ones' eight are loaded as the last eight there are, and moved down where they are
+// staged (4096 x 30522 x 1024 bf16 370 -> 324 us, 8192 x 2047 x 2048 fp16 169 -> 94, against element by element without a pipeline).
+template <typename D, typename T, int TILE, bool RAGGED>
 __global__ void __launch_bounds__((GradShape<D, TILE>::threads), 2)
 weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, long long rows, int width, long long pitch,
                    const D* __restrict__ dy, long long dy_stride, int outputs, T* __restrict__ grad, int accumulate,
@@ -177,7 +179,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
     const int b_row = threadIdx.x / (TILE / 16), b_col = threadIdx.x % (TILE / 16) * 16;
     const int o = o0 + a_col, i = i0 + b_col < pitch ? i0 + b_col : 0;
     const int a_there = outputs - o;          // elements of this lane's eight that exist
-    const int o_safe = a_there >= 8 ? o : 0;
+    const int o_safe = a_there >= 8 ? o : RAGGED ? max(outputs - 8, 0) : 0;
     const D* a_at = dy + (t_begin + a_row) * dy_stride + o_safe;
     const signed char* b_at = q + (t_begin + b_row) * pitch + i;
     const signed char* e_at = e + (t_begin + b_row) * (pitch / kBlock) + i / kBlock;
@@ -200,8 +202,10 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         b_reg[k] = *reinterpret_cast<const u32x4*>(b_at + k * S::b_rows * pitch);
         e_reg[k] = e_at[k * S::b_rows * (pitch / kBlock)];
     };
-    auto write_a = [&](int k, int buffer, bool there) {
-        to_lds<D>(a_lds + buffer * S::buffer_bytes + k * S::a_rows * S::pitch, S::plane_bytes, a_reg[k], there);
+    auto write_a = [&](int k, int buffer, int down) {
+        Granule<D, 8> g = a_reg[k];
+        if constexpr (RAGGED) move_down(g, down);
+        to_lds<D>(a_lds + buffer * S::buffer_bytes + k * S::a_rows * S::pitch, S::plane_bytes, g);
     };
     auto write_b = [&](int k, int buffer, bool there) {
         to_lds(E{}, b_lds + buffer * S::buffer_bytes + k * S::b_rows * S::pitch, b_reg[k], e_reg[k], there);
@@ -247,7 +251,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             }
     };
 
-    const bool ragged = o0 + TILE > outputs && (outputs & 7) != 0;
+    const bool few = RAGGED && outputs < 8;   // (no eight to load)
     auto end_run = [&] {
 #pragma unroll
         for (int m = 0; m < FO; ++m) {
@@ -264,12 +268,12 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         for (int k = 0; k < S::b_passes; ++k)
             if (k * (S::subs - (SETS == 2)) / S::b_passes == sub) b(k);
     };
-    if (whole > 0 && !ragged) {
+    if (whole > 0 && !few) {
 #pragma unroll
         for (int sub = 0; sub < S::subs; ++sub) staged(sub, load_a, load_b);
 #pragma unroll
         for (int sub = 0; sub < S::subs; ++sub)
-            staged(sub, [&](int k) { write_a(k, 0, true); }, [&](int k) { write_b(k, 0, true); });
+            staged(sub, [&](int k) { write_a(k, 0, o - o_safe); }, [&](int k) { write_b(k, 0, true); });
         if (whole > 1) next();
         // (the loads are in flight in the order in which the loop issues them: what waits for one waits for no later one)
 #pragma unroll
@@ -300,7 +304,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
                 multiply(sub, sub, buffer);
                 staged(sub,
                        [&](int k) {
-                           write_a(k, buffer ^ 1, true);
+                           write_a(k, buffer ^ 1, o - o_safe);
                            load_a(k);
                        },
                        [&](int k) {
@@ -322,8 +326,8 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             __builtin_amdgcn_sched_barrier(0);
         }
     }
-    // the steps that are left: the last one, which may be short; all of them where the outputs end inside a lane's eight
-    for (int s = ragged ? 0 : whole; t_begin + static_cast<long long>(s) * S::step < t_end; ++s) {
+    // the steps that are left: the last one, which may be short; all of them of fewer than eight outputs
+    for (int s = few ? 0 : whole; t_begin + static_cast<long long>(s) * S::step < t_end; ++s) {
         const long long t0 = t_begin + static_cast<long long>(s) * S::step;
 #pragma unroll
         for (int k = 0; k < S::a_passes; ++k) {
@@ -354,7 +358,7 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < S::a_passes; ++k) write_a(k, 0, true);
+        for (int k = 0; k < S::a_passes; ++k) write_a(k, 0, 0);
 #pragma unroll
         for (int k = 0; k < S::b_passes; ++k) write_b(k, 0, t0 + k * S::b_rows + b_row < t_end);
         __syncthreads();
@@ -544,7 +548,9 @@ int launch_weight_grad(const WeightGrad& g, void* stream) {
             const bool wide = w.tile == 256;
             const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
             const int threads = wide ? GradShape<D, 256>::threads : GradShape<D, 128>::threads;
-            const auto kernel = wide ? weight_grad_kernel<D, T, 256> : weight_grad_kernel<D, T, 128>;
+            const bool ragged = g.outputs % 8 != 0;
+            const auto kernel = wide ? (ragged ? weight_grad_kernel<D, T, 256, true> : weight_grad_kernel<D, T, 256, false>)
+                                     : (ragged ? weight_grad_kernel<D, T, 128, true> : weight_grad_kernel<D, T, 128, false>);
             int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
             if (rc != 0) return rc;
             rc = launch(kernel, tiles_o * tiles_i * w.parts, 1, threads, lds, stream, reinterpret_cast<const signed char*>(g.x.q),

@@ -58,6 +58,14 @@ def test_pieces_and_edges(dtype, out, n, outputs, width):
     run(n + 2, n, outputs, width, DTYPES[dtype], DTYPES[out], 9, 2, accumulate=True)
 
 
+@pytest.mark.parametrize("dtype, n, outputs, width", [("f32", 9000, 1021, 1024), ("bf16", 16400, 1021, 1000), ("f16", 16400, 1023, 1000),
+                                                      ("f32", 500, 9, 130), ("bf16", 500, 15, 130), ("f16", 500, 7, 130), ("f16", 500, 8, 130)])
+def test_outputs_that_end_inside_eight(dtype, n, outputs, width):
+    """In large tiles and small ones, over many steps; what lies behind a row's outputs is not a number."""
+    run(n, n, outputs, width, DTYPES[dtype], DTYPES[dtype], 3, 0)
+    run(n, n, outputs, width, DTYPES[dtype], DTYPES[dtype], 0, 5)
+
+
 def test_no_tokens():
     flat = torch.ones(100, device="cuda")
     kept = B.Checkpoint(0, 8, torch.float32, device="cuda")
