@@ -543,8 +543,7 @@ int launch_weight_grad(const WeightGrad& g, void* stream) {
             float* const bias_parts = w.parts > 1 ? reinterpret_cast<float*>(g.ws + w.off_bias) : nullptr;
             T* const grad = static_cast<T*>(g.grad);
             T* const bias = static_cast<T*>(g.bias);
-            // (a layer without inputs has a bias all the same)
-            const int64_t tiles_o = (g.outputs + w.tile - 1) / w.tile, tiles_i = g.x.width > 0 ? (g.x.width + w.tile - 1) / w.tile : 1;
+            const int64_t tiles_o = (g.outputs + w.tile - 1) / w.tile, tiles_i = (g.x.width + w.tile - 1) / w.tile;
             const bool wide = w.tile == 256;
             const int lds = wide ? GradShape<D, 256>::lds_bytes : GradShape<D, 128>::lds_bytes;
             const int threads = wide ? GradShape<D, 256>::threads : GradShape<D, 128>::threads;
