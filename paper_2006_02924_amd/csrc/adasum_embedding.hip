@@ -634,6 +634,20 @@ sum_kernel(const D* __restrict__ dy, long long dy_stride, int width, int* __rest
     }
 }
 
+// A sum in fp64 to the result's type, with one rounding: on the way to 16 bits fp32 takes what is cut off into its last bit (rounding to
+// odd; it has more than two bits more than either type, at all magnitudes), so that the second rounding sees on which side of half a
+// step the sum lies.
+__device__ __forceinline__ float to_odd(double s) {
+    const float f = static_cast<float>(s);
+    if (!(static_cast<double>(f) != s) || s != s) return f;
+    const unsigned bits = __float_as_uint(f);
+    return __uint_as_float((fabs(static_cast<double>(f)) > fabs(s) ? bits - 1 : bits) | 1u);
+}
+__device__ __forceinline__ void store_sum(double* p, double s) { *p = s; }
+__device__ __forceinline__ void store_sum(float* p, double s) { *p = static_cast<float>(s); }
+template <typename T>
+__device__ __forceinline__ void store_sum(T* p, double s) { store_elem(p, to_odd(s)); }
+
 // The parts of long runs.  A compute unit alone reads little, so a workgroup takes 64 elements only: groups of sixteen lanes share a
 // run's chunks, four elements a lane.
 template <int R, int THREADS, typename D, typename T>
@@ -684,7 +698,7 @@ join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ r
                 for (int g = 0; g < kJoinGroups; ++g) s += shared[g][lane];
                 s *= scale;
                 T* const to = grad + static_cast<long long>(key) * width + e;
-                store_elem(to, static_cast<A>(accumulate ? s + load_elem(to) : s));
+                store_sum(to, accumulate ? s + load_elem(to) : s);
             }
         }
     }
