@@ -30,10 +30,26 @@ inline int64_t at_most_groups(int64_t groups) { return groups < kMostGroups ? gr
 typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 
-template <bool NT, typename V>
-__device__ __forceinline__ V through(const V* p) {
-    if constexpr (NT) return stream_load(p);
+// (Not through templates of any type: as a template's argument a type loses the alignment that it was declared with.)
+template <bool NT>
+__device__ __forceinline__ u32x4 load_at(const u32x4_any* p) {
+    if constexpr (NT && ADASUM_NT_LOAD) return __builtin_nontemporal_load(p);
     else return *p;
+}
+template <bool NT>
+__device__ __forceinline__ u32x2 load_at(const u32x2_any* p) {
+    if constexpr (NT && ADASUM_NT_LOAD) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool NT>
+__device__ __forceinline__ void store_at(u32x4 v, u32x4_any* p) {
+    if constexpr (NT && ADASUM_NT_STORE) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool NT>
+__device__ __forceinline__ void store_at(u32x2 v, u32x2_any* p) {
+    if constexpr (NT && ADASUM_NT_STORE) __builtin_nontemporal_store(v, p);
+    else *p = v;
 }
 
 // NT: what is used once passes the caches by (streams of many megabytes; see the kernels for what that gave).
@@ -41,13 +57,13 @@ template <bool NT = false, typename T, int G>
 __device__ __forceinline__ void load_any(Granule<T, G>& r, const T* p) {
     constexpr int NW = Granule<T, G>::NW;
     if constexpr (NW == 2) {
-        const u32x2_any q = through<NT>(reinterpret_cast<const u32x2_any*>(p));
+        const u32x2 q = load_at<NT>(reinterpret_cast<const u32x2_any*>(p));
         r.w[0] = q.x;
         r.w[1] = q.y;
     } else {
 #pragma unroll
         for (int i = 0; i < NW / 4; ++i) {
-            const u32x4_any q = through<NT>(reinterpret_cast<const u32x4_any*>(p) + i);
+            const u32x4 q = load_at<NT>(reinterpret_cast<const u32x4_any*>(p) + i);
             r.w[4 * i + 0] = q.x;
             r.w[4 * i + 1] = q.y;
             r.w[4 * i + 2] = q.z;
@@ -59,19 +75,19 @@ __device__ __forceinline__ void load_any(Granule<T, G>& r, const T* p) {
 template <bool NT = false, int NW>
 __device__ __forceinline__ void store_words_any(void* p, const unsigned int (&w)[NW]) {
     if constexpr (NW == 2) {
-        u32x2_any q;
+        u32x2 q;
         q.x = w[0];
         q.y = w[1];
-        stream_store<NT>(q, reinterpret_cast<u32x2_any*>(p));
+        store_at<NT>(q, reinterpret_cast<u32x2_any*>(p));
     } else {
 #pragma unroll
         for (int i = 0; i < NW / 4; ++i) {
-            u32x4_any q;
+            u32x4 q;
             q.x = w[4 * i + 0];
             q.y = w[4 * i + 1];
             q.z = w[4 * i + 2];
             q.w = w[4 * i + 3];
-            stream_store<NT>(q, reinterpret_cast<u32x4_any*>(p) + i);
+            store_at<NT>(q, reinterpret_cast<u32x4_any*>(p) + i);
         }
     }
 }
