@@ -406,7 +406,7 @@ ADASUM_API int adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows, 
  * Gradients of a linear layer y = W x + b (W: outputs x width, row-major) whose input x was kept:
  *   grad[offset + o * width + i]  (+)= sum_t dy[t][o] * x[t][i]
  *   grad[bias_offset + o]         (+)= sum_t dy[t][o]           (bias_offset < 0: no bias)
- * The products are exact (matrix cores; fp32 dy as three bf16 parts) and summed in fp32.  With `dtype`
+ * The products are exact (matrix cores; fp32 dy as three bf16 parts, without what lies below 2^-133) and summed in fp32.  With `dtype`
  * ADASUM_F16 the kept values must be fp16's own: a checkpoint of fp16 activations (others are cut to
  * fp16).  rows and width as above; outputs at most 2^24.  A layer without inputs (width 0) has no bias here
  * (ADASUM_ERR_INVALID_ARG).
