@@ -43,7 +43,11 @@ __device__ __forceinline__ void kept_values(float (&x)[kG], u32x2 q, float step)
 // gelu: with the normal density f and its upper tail Q, the slope at -a is Q(a) - a f(a) = f(a) (M(a) - a), M = Q / f, and that at
 // a is 1 minus it.  M falls smoothly from 1.25 to 1 / a: a polynomial in t = 1 / (1 + a / 4), fitted here for the least largest
 // error relative to what fp32's own roundings leave (M + a) at 0 <= a <= 16; 1.7 % of that.  What is evaluated is M / sqrt(2 pi).
-// Against fp64 the slope is off by 2.3e-7 at most, and by little more relative to f(a) (M(a) + a) on the negative side.
+// Against fp64 the slope is off by 1.1e-7 at most.  Relative to f(a) (M(a) + a) on the negative side, the rounding of the exponential's
+// argument and that of its constant show: 4.4e-7 below 4, 1.4e-6 at 9, 7.6e-6 at 12, which is far below the rounding of a result of
+// 16 bits.  For results in fp32 (FINE) a^2 is exact, as kept values have seven bits, and what its product with the constant loses,
+// and the constant itself, multiplies the exponential: 4.5e-7 down to -12.5, where the terms leave fp32's range.  (32768 x 4096:
+// 217 - 218 us in fp32 with and without that, where memory bounds it; for 16 bits it would cost 158 us instead of 142.)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // s(z) + f s(z) s(-z) for s(z) = 1 / (1 + exp(-z)), from e = exp(-|z|): s is 1 / (1 + e), or e / (1 + e) below zero, and the product
 // e / (1 + e)^2 on both sides.  (e is held times 2^16: its product with f may be a normal number where e is none.)
@@ -52,7 +56,7 @@ __device__ __forceinline__ float logistic_slope(float z, float f) {
     const float r = __builtin_amdgcn_rcpf(1.f + less);
     return __builtin_fmaf(f * 0x1p-16f, e * r * r, z < 0.f ? less * r : r);
 }
-template <int ACT>
+template <int ACT, bool FINE>
 __device__ __forceinline__ float slope(float x) {
     if constexpr (ACT == ADASUM_ACT_RELU) {
         return x != x ? x : x > 0.f ? 1.f : 0.f;
@@ -65,7 +69,12 @@ __device__ __forceinline__ float slope(float x) {
         m = __builtin_fmaf(m, t, 0.01876537874341011f);
         m = __builtin_fmaf(m, t, 0.11390205472707748f);
         m = __builtin_fmaf(m, t, 0.09862539917230606f);
-        const float s = exp2_fast(x * x * -0.7213475204444817f) * __builtin_fmaf(a, -0.3989422804014327f, m * t);
+        constexpr double kPower = -0.72134752044448170;   // - log2(e) / 2
+        constexpr float kHigh = static_cast<float>(kPower), kLow = static_cast<float>(kPower - static_cast<double>(kHigh));
+        const float b = FINE ? fminf(a, 64.f) : a, bb = b * b, power = bb * kHigh;   // (beyond, nothing is left; NaN comes in with m)
+        float e = exp2_fast(power);
+        if constexpr (FINE) e = __builtin_fmaf(e, __builtin_fmaf(bb, kLow, __builtin_fmaf(bb, kHigh, -power)) * 0.6931471805599453f, e);
+        const float s = e * __builtin_fmaf(a, -0.3989422804014327f, m * t);
         return x < 0.f ? s : 1.f - s;
     } else if constexpr (ACT == ADASUM_ACT_GELU_TANH) {
         // beyond 30 the slope is 0 or 1 to the last bit, and the cube may overflow
@@ -206,7 +215,7 @@ act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict
                     kept_values(v, kept[k], step_of(exponent[k]));
                     unpack(raw[k], d);
 #pragma unroll
-                    for (int i = 0; i < kG; ++i) v[i] = d[i] * slope<ACT>(v[i]);
+                    for (int i = 0; i < kG; ++i) v[i] = d[i] * slope<ACT, sizeof(T) == 4>(v[i]);
                     store_row<FORM, NT>(dx + p.row * dx_stride, v, p.at, width);
                 }
             }
