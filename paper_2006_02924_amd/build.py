@@ -24,7 +24,7 @@ CEILING_PATH = os.path.join(HERE, "pattern_ceiling")
 SOURCES = [("adasum_resident.hip", [f"-DADASUM_LEAF_TYPE={t}", f"-DADASUM_WIDE_GROUPS={w}"])
            for t, w in ((0, 0), (1, 0), (2, 0), (3, 0), (0, 1), (1, 1), (2, 1))] + [
     ("adasum_kernels.hip", []), ("adasum_weight_grad.hip", []), ("adasum_embedding.hip", []), ("adasum_checkpoint.hip", []),
-    ("adasum_api.cpp", []), ("adasum_layers.cpp", []), ("adasum_plan.cpp", [])]
+    ("adasum_api.cpp", []), ("adasum_layers.cpp", []), ("adasum_weight_split.cpp", []), ("adasum_plan.cpp", [])]
 
 # -packed-fp32-ops off: the compiler must not form packed fp32 instructions.
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

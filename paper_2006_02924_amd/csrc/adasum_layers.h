@@ -100,10 +100,10 @@ int launch_load(const Kept& k, void* out, int dtype, int64_t out_stride, void* s
 int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t dy_stride, void* dx, int64_t dx_stride,
                     void* stream);
 
-// ---- weight gradients (adasum_weight_grad.hip) ----------------------------------
+// ---- weight gradients (adasum_weight_grad.hip, adasum_weight_split.cpp) -----------
 
-// A workgroup computes a square of the weight, `tile` wide, over one of `parts` parts of the tokens, each `steps` steps of the kernel,
-// `tokens` in all.
+// A workgroup computes a square of the weight, `tile` wide, over one of `parts` parts of the tokens, each `steps` steps of the kernel (of
+// 64 tokens, 32 in fp32).
 struct WeightSplit {
     int tile = 0;
     int64_t parts = 1, steps = 0;
