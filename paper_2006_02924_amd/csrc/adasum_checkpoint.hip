@@ -3,8 +3,9 @@
 //
 // All three stream: a lane takes eight channels of a row, four lanes a block of 32 that shares an exponent.  The exponent comes
 // from the bits of the block's largest magnitude, scaling by a power of two is exact, and the sum with 3 * 2^22 rounds to nearest
-// even and leaves the whole number in the low byte.  Memory bounds them: 32768 x 4096 bf16 stored (406 MB) and loaded again take 70 - 77 and
-// 60 us, the gradient through gelu (675 MB) 119 - 123 us, 5.3 - 6.7 TB/s.
+// even and leaves the whole number in the low byte.  Memory bounds them: 32768 x 4096 bf16 stored and loaded again (406 MB each) take 80 and
+// 67 us, the gradient (675 MB) through relu and silu 109 - 112 us, through gelu 117 and its other form 122, where the vector units are
+// as busy: 5.1 - 6.2 TB/s.  In fp32 116 us each (675 MB) and 207 us for every gradient (1.21 GB), 5.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "adasum_layers.h"
@@ -47,7 +48,7 @@ __device__ __forceinline__ void kept_values(float (&x)[kG], u32x2 q, float step)
 // argument and that of its constant show: 4.4e-7 below 4, 1.4e-6 at 9, 7.6e-6 at 12, which is far below the rounding of a result of
 // 16 bits.  For results in fp32 (FINE) a^2 is exact, as kept values have seven bits, and what its product with the constant loses,
 // and the constant itself, multiplies the exponential: 4.5e-7 down to -12.5, where the terms leave fp32's range.  (32768 x 4096:
-// 217 - 218 us in fp32 with and without that, where memory bounds it; for 16 bits it would cost 158 us instead of 142.)
+// 207 us in fp32 with and without that, where memory bounds it; for 16 bits it would cost 123 us instead of 117.)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 // s(z) + f s(z) s(-z) for s(z) = 1 / (1 + exp(-z)), from e = exp(-|z|): s is 1 / (1 + e), or e / (1 + e) below zero, and the product
 // e / (1 + e)^2 on both sides.  (e is held times 2^16: its product with f may be a normal number where e is none.)
@@ -114,7 +115,7 @@ template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 store_kernel(const T* __restrict__ x, long long stride, int width, long long pitch, signed char* __restrict__ q, signed char* __restrict__ e,
              RowWork work) {
-    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
+    // (of large tensors only x: eight bytes a lane are slower so)
     constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
@@ -161,7 +162,6 @@ template <typename T, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 load_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, T* __restrict__ out,
             long long stride, RowWork work) {
-    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
     constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
@@ -192,7 +192,6 @@ template <typename T, int ACT, RowForm FORM, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict__ e, int width, long long pitch, const T* dy,
                 long long dy_stride, T* dx, long long dx_stride, RowWork work) {
-    // (activations and gradients of large tensors; what is small is in the caches for the next kernel, and eight bytes a lane are slower so)
     constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
@@ -223,15 +222,22 @@ act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict
     });
 }
 
+// Four granules of a lane in flight, past the caches, or one through them.  Rows of 1024 (in thousands of granules: microseconds with one and
+// with four of them), operands that no cache holds: loads of bf16 524: 4.7 and 4.3; 4194: 21.2 and 19.7; 16777: 73 and 67.  Stores 524: 5.0 and
+// 5.5; 2097: 13.6 and 12.3; 16777: 77 and 79.  In fp32, where a granule is 32 bytes, four are slower: loads 4194: 35 and 40; 16777: 116
+// and 137, stores 116 and 124.  Gradients of relu in bf16 524: 6.0 and 6.3; 1049: 10.5 and 9.7; 16777: 114 and 109, of silu 4194: 31.7 and
+// 32.1; 16777: 115 and 110; gelu, whose vector instructions take as long as its memory, 4194: 32 and 34; 16777: 118 and 122, and its
+// other form 34 and 37, 124 and 129.  fp16 is like bf16.  Operands that were just used are faster with one (4194, bf16: stores 18.5 and 21).
+constexpr int64_t kMany = 1 << 19, kManyOfSilu = 1 << 21;
 struct RowGrid {
     RowWork work;
     int64_t groups;
     bool large;
 };
-RowGrid row_grid(int64_t rows, int64_t pitch) {
+RowGrid row_grid(int64_t rows, int64_t pitch, int dtype, int64_t many) {
     RowGrid r;
     const int64_t granules = pitch / kG;
-    r.large = rows * granules > (1 << 18);
+    r.large = dtype != ADASUM_F32 && rows * granules > many;
     const int64_t per_group = r.large ? 4 * kThreadsRow : kThreadsRow;
     const int64_t tokens = granules >= per_group ? 1 : per_group / granules;
     r.work.rows = rows;
@@ -241,30 +247,43 @@ RowGrid row_grid(int64_t rows, int64_t pitch) {
     return r;
 }
 
+// f(granules of a lane in flight) as a constant.
+template <typename T, typename F>
+int with_items(const RowGrid& g, F&& f) {
+    if constexpr (sizeof(T) == 2) {
+        if (g.large) return f(std::integral_constant<int, 4>{});
+    }
+    return f(std::integral_constant<int, 1>{});
+}
+
 }  // namespace
 
 int launch_store(const void* x, int dtype, int64_t x_stride, const Kept& to, void* stream) {
-    const RowGrid g = row_grid(to.rows, to.pitch);
+    const RowGrid g = row_grid(to.rows, to.pitch, dtype, kMany);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
         return with_form(row_form(to.width, kG), [&](auto form) -> int {
             constexpr RowForm F = decltype(form)::value;
-            return launch(g.large ? store_kernel<T, F, 4> : store_kernel<T, F, 1>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x),
-                          x_stride, to.width, to.pitch, reinterpret_cast<signed char*>(const_cast<int8_t*>(to.q)),
-                          reinterpret_cast<signed char*>(const_cast<int8_t*>(to.e)), g.work);
+            return with_items<T>(g, [&](auto items) -> int {
+                return launch(store_kernel<T, F, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x), x_stride,
+                              to.width, to.pitch, reinterpret_cast<signed char*>(const_cast<int8_t*>(to.q)),
+                              reinterpret_cast<signed char*>(const_cast<int8_t*>(to.e)), g.work);
+            });
         });
     });
 }
 
 int launch_load(const Kept& k, void* out, int dtype, int64_t out_stride, void* stream) {
-    const RowGrid g = row_grid(k.rows, k.pitch);
+    const RowGrid g = row_grid(k.rows, k.pitch, dtype, kMany);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
         auto go = [&](auto form) -> int {
             constexpr RowForm F = decltype(form)::value;
-            return launch(g.large ? load_kernel<T, F, 4> : load_kernel<T, F, 1>, g.groups, 1, kThreadsRow, 0, stream,
-                          reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
-                          static_cast<T*>(out), out_stride, g.work);
+            return with_items<T>(g, [&](auto items) -> int {
+                return launch(load_kernel<T, F, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream,
+                              reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+                              static_cast<T*>(out), out_stride, g.work);
+            });
         };
         // (short rows are stored like ragged ones)
         return k.width % kG == 0 ? go(std::integral_constant<RowForm, kWhole>{}) : go(std::integral_constant<RowForm, kRagged>{});
@@ -272,16 +291,20 @@ int launch_load(const Kept& k, void* out, int dtype, int64_t out_stride, void* s
 }
 
 int launch_act_grad(const Kept& k, int act, const void* dy, int dtype, int64_t dy_stride, void* dx, int64_t dx_stride, void* stream) {
-    const RowGrid g = row_grid(k.rows, k.pitch);
+    const RowGrid g = row_grid(k.rows, k.pitch, dtype, act == ADASUM_ACT_RELU ? kMany : act == ADASUM_ACT_SILU ? kManyOfSilu : INT64_MAX);
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
         return with_form(row_form(k.width, kG), [&](auto form) -> int {
             constexpr RowForm F = decltype(form)::value;
             auto go = [&](auto chosen) -> int {
                 constexpr int ACT = decltype(chosen)::value;
-                return launch(g.large ? act_grad_kernel<T, ACT, F, 4> : act_grad_kernel<T, ACT, F, 1>, g.groups, 1, kThreadsRow, 0, stream,
-                              reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
-                              static_cast<const T*>(dy), dy_stride, static_cast<T*>(dx), dx_stride, g.work);
+                auto run = [&](auto items) -> int {
+                    return launch(act_grad_kernel<T, ACT, F, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream,
+                                  reinterpret_cast<const signed char*>(k.q), reinterpret_cast<const signed char*>(k.e), k.width, k.pitch,
+                                  static_cast<const T*>(dy), dy_stride, static_cast<T*>(dx), dx_stride, g.work);
+                };
+                if constexpr (ACT == ADASUM_ACT_GELU || ACT == ADASUM_ACT_GELU_TANH) return run(std::integral_constant<int, 1>{});
+                else return with_items<T>(g, run);
             };
             switch (act) {
                 case ADASUM_ACT_RELU: return go(std::integral_constant<int, ADASUM_ACT_RELU>{});

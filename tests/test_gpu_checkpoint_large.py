@@ -7,7 +7,7 @@ from layer_grads_util import DTYPES, f64, half_step, keep, least, slope, split, 
 from paper_2006_02924_amd import binding as B
 
 pytestmark = pytest.mark.gpu
-SHAPES = [(3000, 1000, 8), (2500, 1001, 3), (70001, 5, 1), (9000, 256, 0)]
+SHAPES = [(17000, 1000, 8), (16500, 1001, 3), (530001, 5, 1), (66000, 256, 0)]
 
 
 def some_activations(n, width, dtype):
@@ -21,8 +21,10 @@ def some_activations(n, width, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("n, width, gap", SHAPES)
 def test_store_load_and_every_activation(n, width, gap, dtype):
+    # eight channels a lane: so many of them that every form for 16 bits that takes four at a time is reached; fp32 has no such form
+    n = n // 8 if dtype == "f32" else n
+    assert dtype == "f32" or n * (-(-width // 32) * 4) > 1 << 21
     dtype = DTYPES[dtype]
-    assert n * (-(-width // 32) * 4) > 1 << 18           # eight channels a lane: many of them
     x = torch.full((n, width + gap), float("nan"), dtype=dtype, device="cuda")
     given = some_activations(n, width, dtype)
     x[:, :width] = given.cuda()
