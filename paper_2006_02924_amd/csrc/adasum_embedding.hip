@@ -650,6 +650,7 @@ __device__ __forceinline__ void store_sum(T* p, double s) { store_elem(p, to_odd
 
 // The parts of long runs.  A compute unit alone reads little, so a workgroup takes 64 elements only: groups of sixteen lanes share a
 // run's chunks, four elements a lane.
+constexpr int64_t kMostJoins = 8192;   // workgroups
 template <int R, int THREADS, typename D, typename T>
 __global__ void __launch_bounds__(THREADS)
 join_kernel(int width, const int* __restrict__ totals, const int* __restrict__ row, typename Traits<D>::acc_t scale, T* __restrict__ grad,
@@ -738,6 +739,8 @@ int launch_lookup(int dtype, int out_dtype, const void* table, int64_t rows, int
         typedef decltype(u) U;
         constexpr int G = 16 / (sizeof(T) < sizeof(U) ? sizeof(T) : sizeof(U));
         const int64_t granules = (width + G - 1) / G;
+        // one granule of a lane in flight, or four, stored past the caches (rows of 1024, in thousands of granules): 131: 2.6 and 3.4 us; 262: 3.6
+        // and 3.8, in fp32 4.8 and 4.5; 4194: 25.4 and 21.7; 16777: 93 and 77, in fp32 192 and 153
         const bool large = ids.n * granules > (1 << 18);
         const int64_t per_block = large ? 1024 : 256;
         const int64_t tokens = granules >= per_block ? 1 : per_block / granules;
@@ -809,15 +812,16 @@ int launch_embedding_grad(const EmbeddingGrad& g, void* stream) {
                               static_cast<T*>(g.grad), parts, listed, slices, g.lay.chunks);
             });
             if (rc2 != 0 || g.ids.n <= R) return rc2;   // (so few tokens make no long run)
-            const int64_t most = (g.ids.n / (R + 1)) * ((g.width + 63) / 64);
-            // few rows that all tokens share make few and very long runs (two rows, 16384 tokens: 9.0 us with 1024 lanes, 11.6 with 256),
-            // otherwise most of those that are long are so by little (30522 rows, 65501 tokens: 17.3 us and 7.4)
-            const bool few = g.ids.n > 256 * g.rows;
-            // and where rows have sixteen tokens on average, many are long (512 rows, 65536 tokens: 67.4 us with up to 8192 workgroups, 70.6
-            // with 1024); else workgroups that find nothing would only cost time
-            const int64_t at_most = g.ids.n >= 16 * g.rows ? 8192 : 1024;
-            return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < at_most ? most : at_most, 1, few ? 1024 : 256, 0, stream,
-                          g.width, totals, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, listed);
+            // Runs times slices, at most; workgroups that find nothing cost less than workgroups that take turns (512 rows x 1024, 65536 tokens: 66.0 us
+            // with up to 8192 of them, 70.4 with 1024; 32768 rows 63.7 and 64.3; 4096 tokens of 30522 rows 29.0 both).
+            const int64_t slices64 = (g.width + 63) / 64, most = (g.ids.n / (R + 1)) * slices64;
+            // Workgroups of 1024 lanes shorten the way through a run's parts, but need the room of four: they are better where few runs share
+            // many tokens (whole calls, bf16, 256 and 1024 lanes: 16384 tokens, two rows x 1024 35.7 and 30.0 us; 131072, 8 rows x 1024 75.6 and
+            // 70.6; 131072, 16 rows x 64 33.5 and 29.5) and worse elsewhere (16384 tokens, 16 rows x 1024 25.2 and 31.2; 65536, 32 rows x 256
+            // 27.5 and 30.6; 131072, 16 rows x 1024 69 and 72.5; 65536, 64 rows x 64 24.7 and 24.9).
+            const bool few = static_cast<double>(g.ids.n) >= 64.0 * static_cast<double>(g.rows) * static_cast<double>(g.rows * slices64);
+            return launch(few ? join_kernel<R, 1024, D, T> : join_kernel<R, 256, D, T>, most < kMostJoins ? most : kMostJoins, 1, few ? 1024 : 256, 0,
+                          stream, g.width, totals, row, g.scale, static_cast<T*>(g.grad), g.accumulate, parts, listed);
         };
         return g.lay.run == 16 ? go(std::integral_constant<int, 16>{}) : go(std::integral_constant<int, 32>{});
     });
