@@ -339,7 +339,8 @@ ADASUM_API int adasum_group_combine(const void* const* x, int R,
  * lie closer, or all be the same one (stride 0).  n = 0 and width 0 are allowed.
  * Storage types: any of ADASUM_F32, ADASUM_BF16 and ADASUM_F16 goes with any other of the three, ADASUM_F64
  * only with itself and not with checkpoints (else ADASUM_ERR_UNSUPPORTED).  Sums are formed in fp32 or more
- * (fp64 for fp64) and rounded once to the result's type, with `accumulate` after what the layer held is added.
+ * (fp64 for fp64; a factor is taken in that type too) and rounded once to the result's type, with `accumulate`
+ * after what the layer held is added.
  * `accumulate` = 0 overwrites the layer, 1 adds to what it holds (micro-batches, or a table that is also an
  * output layer).
  */
@@ -392,7 +393,8 @@ ADASUM_API int adasum_checkpoint_load(const void* checkpoint, int64_t rows, int6
 
 /*
  * Gradient through an activation function whose input x was kept:  dx = dy * act'(x), both of `dtype`.
- * `dx` may be `dy` itself (same stride); any other overlap is ADASUM_ERR_ALIAS.  relu'(0) = 0.
+ * `dx` may be `dy` itself (same stride); any other overlap is ADASUM_ERR_ALIAS.  relu'(0) = 0.  Where NaN is
+ * kept the result is NaN, for every function.
  */
 #define ADASUM_ACT_RELU      0
 #define ADASUM_ACT_GELU      1   /* x Phi(x) */
@@ -406,9 +408,9 @@ ADASUM_API int adasum_checkpoint_act_grad(const void* checkpoint, int64_t rows, 
  * Gradients of a linear layer y = W x + b (W: outputs x width, row-major) whose input x was kept:
  *   grad[offset + o * width + i]  (+)= sum_t dy[t][o] * x[t][i]
  *   grad[bias_offset + o]         (+)= sum_t dy[t][o]           (bias_offset < 0: no bias)
- * The products are exact (matrix cores; fp32 dy as three bf16 parts, without what lies below 2^-133) and summed in fp32.  With `dtype`
- * ADASUM_F16 the kept values must be fp16's own: a checkpoint of fp16 activations (others are cut to
- * fp16).  rows and width as above; outputs at most 2^24.  A layer without inputs (width 0) has no bias here
+ * The products are exact (matrix cores; fp32 dy as three bf16 parts, without what lies below 2^-133) and summed in
+ * fp32 (dy's own sums, within 64 tokens, with additions that cut off rather than round).  With `dtype` ADASUM_F16 the
+ * kept values must be fp16's own: a checkpoint of fp16 activations (others are cut to fp16).  rows and width as above; outputs at most 2^24.  A layer without inputs (width 0) has no bias here
  * (ADASUM_ERR_INVALID_ARG).
  */
 ADASUM_API int adasum_checkpoint_weight_grad_workspace_bytes(int64_t rows, int64_t width, int64_t outputs,

@@ -510,7 +510,8 @@ def _scratch(workspace, need, dev, stream):
 
 def adasum_embedding(params, offset: int, rows: int, width: int, ids, *, scale: float = 1.0, out=None, out_dtype=None, stream=None):
     """``scale * table[ids]`` for the table of ``rows`` x ``width`` that lies at ``offset`` of the flat buffer ``params``; rows of
-    zeros where an id names no row.  Returns ``out``, [*ids.shape, width] (made here when None)."""
+    zeros where an id names no row.  Returns ``out``, [*ids.shape, width] (made here when None).  As every operand ``ids`` must
+    begin at a multiple of 16 bytes, which a slice of a longer tensor may not (``ids.clone()`` does)."""
     lib = _lib or load()
     _flat(params, offset, rows * width, "params")
     id_type = _id_type(ids)

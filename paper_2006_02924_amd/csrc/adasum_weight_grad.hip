@@ -4,7 +4,6 @@
 #include "adasum_layers.h"
 #include "adasum_rows.h"
 
-
 namespace adasum {
 namespace {
 
@@ -48,7 +47,8 @@ __device__ __forceinline__ unsigned exact_pair(f16_t, float a, float b) {
 }
 
 // c and the sum of eight values.  The instruction multiplies with one, exactly, and adds with truncation: a step's run of them is then
-// added to the rest with rounding.
+// added to the rest with rounding.  (40000 positive tokens come out within 3 steps of fp32, 0.1 on average.  Additions on the vector
+// unit would take four instructions for one.)
 __device__ __forceinline__ float plus_eight(bf16_t, u32x4 a, float c) {
     typedef __bf16 pair __attribute__((ext_vector_type(2)));
     const pair one = {static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
@@ -251,7 +251,9 @@ weight_grad_kernel(const signed char* __restrict__ q, const signed char* __restr
             }
     };
 
-    const bool few = RAGGED && outputs < 8;   // (no eight to load)
+    // (no eight to load: such layers go without the pipeline, bf16 16384 x 1024 with 1, 2, 7 and 8 outputs 17, 18, 20 and 16 us, 65536 x 256
+    // 25, 27, 31 and 20.5; fp32, 27 and 37 us, does not feel it)
+    const bool few = RAGGED && outputs < 8;
     auto end_run = [&] {
 #pragma unroll
         for (int m = 0; m < FO; ++m) {
