@@ -19,23 +19,22 @@ __device__ __forceinline__ f32x16 mfma(f16_t, u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // What the matrix cores multiply: the 16-bit types as they are; fp32 as three bf16 parts, each what the parts before it leave, rounded to
-// nearest.  The three add up to the value (9 + 9 + 6 bits; of values below 2^-109 what lies below 2^-133 is lost).  Rounded rather than
+// nearest.  The three add up to the value (9 + 9 + 6 bits; of values below 2^-110 what lies below 2^-133 is lost).  Rounded rather than
 // cut off, so that the smaller parts of values of one sign have either sign: a sum of some thousand tokens is too large for a run of
 // third parts to change it, and what is lost must not add up (8192 positive tokens came out 46 steps of fp32 too small on average
 // with parts cut off, 0.7 with parts rounded).
 template <typename T> struct Products { typedef T type; static constexpr int planes = 1; };
 template <> struct Products<float> { typedef bf16_t type; static constexpr int planes = 3; };
 
-// The parts of two values.  (Values that would round to an infinity take bf16's largest number first.  Infinities and NaN are in the second
-// part.)
+// The parts of two values.  (Near the end of the range the first two are limited, so that no part and no sum of them is an infinity that the
+// value is not.  Infinities and NaN leave the limits as they are and are in the third part.)
 __device__ __forceinline__ void parts_of(unsigned (&p)[3], unsigned a, unsigned b) {
-    constexpr float kMost = 0x1.fep127f;
+    constexpr float kMost = 0x1.fep127f, kRest = 0x1.fep119f;   // bf16's largest number, and its largest below what fp32 has beyond that
     const float x = __uint_as_float(a), y = __uint_as_float(b);
     p[0] = rounded_pair(bf16_t{}, __builtin_amdgcn_fmed3f(x, -kMost, kMost), __builtin_amdgcn_fmed3f(y, -kMost, kMost));
     const float rx = x - __uint_as_float(p[0] << 16), ry = y - __uint_as_float(p[0] & 0xffff0000u);
-    p[1] = rounded_pair(bf16_t{}, rx, ry);
-    const float sx = rx - __uint_as_float(p[1] << 16), sy = ry - __uint_as_float(p[1] & 0xffff0000u);
-    p[2] = rounded_pair(bf16_t{}, __builtin_isfinite(rx) ? sx : 0.f, __builtin_isfinite(ry) ? sy : 0.f);
+    p[1] = rounded_pair(bf16_t{}, __builtin_amdgcn_fmed3f(rx, -kRest, kRest), __builtin_amdgcn_fmed3f(ry, -kRest, kRest));
+    p[2] = rounded_pair(bf16_t{}, rx - __uint_as_float(p[1] << 16), ry - __uint_as_float(p[1] & 0xffff0000u));
 }
 
 // Two values that their type holds exactly.
