@@ -203,8 +203,8 @@ def prepare(case, seed):
             from paper_2006_02924_amd import binding
             s["weight8"] = binding.Weight8(case["outputs"], width, device="cuda")
             if kind == "linear":
-                binding.adasum_linear8_store(s["params"], places["weight"][0], case["outputs"], width, out=s["weight8"])
-            need = binding.adasum_linear8_workspace_bytes(n, width, case["outputs"], dtype)
+                binding.adasum_linear_store(s["params"], places["weight"][0], case["outputs"], width, out=s["weight8"])
+            need = binding.adasum_linear_workspace_bytes(n, width, case["outputs"], dtype)
             s["workspace"] = torch.empty(need, dtype=torch.uint8, device="cuda")
         return s
     stream = DTYPES[case["stream"]]
@@ -407,11 +407,11 @@ def _run_own(s):
         return out + [s["grad"]]
     w = s["weight8"]
     if kind == "step":
-        binding.adasum_linear8_store(s["params"], _offset(case, "weight"), case["outputs"], case["width"], out=w)
-    y = binding.adasum_linear8(w, s["x"], params=s["params"], bias_offset=_offset(case, "bias"), out=s["y"], workspace=s["workspace"])
+        binding.adasum_linear_store(s["params"], _offset(case, "weight"), case["outputs"], case["width"], out=w)
+    y = binding.adasum_linear(w, s["x"], params=s["params"], bias_offset=_offset(case, "bias"), out=s["y"], workspace=s["workspace"])
     if kind == "linear":
         return [y]
-    return [y, binding.adasum_linear8_grad(w, s["dy"], out=s["dx"], workspace=s["workspace"])]
+    return [y, binding.adasum_linear_grad(w, s["dy"], out=s["dx"], workspace=s["workspace"])]
 
 
 def run(s):
