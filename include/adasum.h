@@ -41,7 +41,8 @@
  * or without loss scaling, are many orders of magnitude inside the range.
  *
  * Beside the reduction: operators that fill a worker's gradient buffer (embedding tables, linear layers from activations kept in
- * 8 bits), see "the gradients that fill a worker's buffer" below.
+ * 8 bits), see "the gradients that fill a worker's buffer" below, and those between the layers (dropout, norms with the residual
+ * stream, products in 8-bit floating point), see "between the layers".
  *
  * Conventions for every entry point
  *   - returns ADASUM_OK (0) or a negative ADASUM_ERR_* code; never throws,
@@ -419,6 +420,118 @@ ADASUM_API int adasum_checkpoint_weight_grad(const void* checkpoint, int64_t row
                                              const void* dy, int dtype, int64_t dy_stride, int64_t outputs,
                                              void* grad, int grad_dtype, int64_t offset, int64_t bias_offset,
                                              int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- between the layers ----
+ *
+ * What carries activations and their gradients from one of those layers to the next.  The same conventions: matrices of rows,
+ * parameters in a flat buffer at offsets, the gradients of parameters written into a worker's flat buffer at the same offsets,
+ * a workspace of the caller, no allocation, capturable.  Storage types are ADASUM_F32, ADASUM_BF16 and ADASUM_F16 (else
+ * ADASUM_ERR_UNSUPPORTED); sums, statistics and products are held in fp32 or more and rounded once.
+ */
+
+/*
+ * Dropout, with a mask that is never stored: element j of row t is kept where u(t, j) >= T and multiplied by 65536 / (65536 - T), else it
+ * is 0 (also if x is an infinity or NaN there).  T = floor(65536 p + 1/2), for 0 <= p <= 1.
+ *   u(t, j): of the four 32-bit words that Philox4x32-10 makes of the counter (j / 8, t, low half of step, high half of step) and
+ *            the key (low half of seed, high half of seed), the 16-bit half number j % 8, lower halves first
+ *   step     DEVICE, one 64-bit number, 8-byte aligned, that the kernel reads when it runs; NULL: 0.  A captured program draws new masks
+ *            by counting it up between replays; layers of one program have seeds of their own.
+ * The same call on the gradient of the result gives that of x.  `out` may be x itself (same stride); any other overlap is
+ * ADASUM_ERR_ALIAS.  rows at most 2^31 - 65536, width at most 2^24.
+ */
+ADASUM_API int adasum_dropout(const void* x, int dtype, int64_t x_stride, int64_t rows, int64_t width,
+                              double p, uint64_t seed, const uint64_t* step, void* out, int64_t out_stride, void* stream);
+
+/*
+ * Where a block's output x joins the residual stream and the next block's input leaves it:
+ *   v = N(x) * after_weight + after_bias      (`after`; else v = x)
+ *   h = residual_scale * residual + gate * dropout(v)
+ *   y = N(h) * before_weight + before_bias    (`before`; else no y)
+ * N of a row t: (t - mean t) / sqrt(mean (t - mean t)^2 + eps) (ADASUM_NORM_LAYER) or t / sqrt(mean t^2 + eps) (ADASUM_NORM_RMS).
+ * Weights, biases and the gate are vectors of `width` elements at offsets of the flat buffer `params`; a negative offset means that
+ * there is none (1 for a weight and the gate, 0 for a bias), and those of a norm that is not there are not looked at.
+ * y is that of h before h's rounding.  Rows whose squares leave the range of fp32 give no numbers.
+ */
+#define ADASUM_NORM_LAYER 0
+#define ADASUM_NORM_RMS   1
+typedef struct adasum_join_form {
+    uint32_t struct_bytes;     /* sizeof(adasum_join_form) as the caller compiled it */
+    int32_t  dtype;            /* of x, y and their gradients */
+    int32_t  stream_dtype;     /* of residual, h and their gradients: dtype or ADASUM_F32 */
+    int32_t  norm;             /* ADASUM_NORM_... */
+    int32_t  after, before;    /* 1: with that norm, 0: without */
+    int64_t  width;            /* channels, at most 8192 (else ADASUM_ERR_UNSUPPORTED) */
+    double   eps;              /* above 0, also in fp32 */
+    double   residual_scale;
+    double   dropout;          /* p of adasum_dropout, 0: none */
+    uint64_t seed;             /* and its seed */
+    int64_t  after_weight, after_bias, gate, before_weight, before_bias;   /* offsets in elements, or negative */
+} adasum_join_form;
+/*
+ *   params    may be NULL where the form names no vector
+ *   step      as for adasum_dropout
+ *   residual  NULL: none (h = gate * dropout(v), and y = N(x) with neither)
+ *   h         NULL: not wanted (only with a y); may be `residual` itself (same stride)
+ *   y         NULL exactly if the form has no `before`
+ * The results must not overlap anything else (ADASUM_ERR_ALIAS).
+ */
+ADASUM_API int adasum_join(const adasum_join_form* form, const void* params, int param_dtype, const uint64_t* step,
+                           const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, int64_t rows,
+                           void* h, int64_t h_stride, void* y, int64_t y_stride, void* stream);
+/*
+ * The gradients, from those of y (`dy`) and of h (`dh`):
+ *   D = dh + (gradient of N(h) * before_weight + before_bias at h, of dy);     dresidual = residual_scale * D
+ *   dx = gradient of gate * dropout(v) at x, of D
+ *   grad[before_weight + j] (+)= sum_t dy N(h),  [before_bias + j] (+)= sum_t dy,  [gate + j] (+)= sum_t D dropout(v),
+ *   grad[after_weight + j] (+)= sum_t dv N(x),   [after_bias + j] (+)= sum_t dv,   with dv = the gradient that reaches v
+ * The statistics are those of the rows that are given here.
+ *   x          read with `after` or a gate, else not looked at
+ *   h, dy      read with `before`, else not looked at
+ *   dh         NULL: none (only with `before`)
+ *   dresidual  NULL: not wanted; may be `dh` itself (same stride)
+ *   grad       may be NULL where the form names no vector.  Every result's layer (offset, width) has its place: two that overlap
+ *              are ADASUM_ERR_ALIAS, as is any other overlap of a result.
+ * rows = 0 sets the parameters' gradients to 0 (or leaves them, with `accumulate`).  A lane sums up to rows / 512 of its rows (rounded up) in
+ * fp32, what is above that is summed in fp64: bit-identical from run to run.
+ */
+ADASUM_API int adasum_join_grad_workspace_bytes(const adasum_join_form* form, int64_t rows, size_t* bytes);
+ADASUM_API int adasum_join_grad(const adasum_join_form* form, const void* params, int param_dtype, const uint64_t* step,
+                                const void* x, int64_t x_stride, const void* h, int64_t h_stride,
+                                const void* dy, int64_t dy_stride, const void* dh, int64_t dh_stride, int64_t rows,
+                                void* dx, int64_t dx_stride, void* dresidual, int64_t dresidual_stride,
+                                void* grad, int grad_dtype, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Linear layers whose products are taken in 8-bit floating point (e4m3: 1 sign, 4 exponent and 3 fraction bits, at most 448).
+ * Blocks of ADASUM_LINEAR_BLOCK channels of a row of activations (or gradients), and of 128 outputs x 128 inputs of a weight, share
+ * an exponent e: the least with max |x| <= 448 * 2^e, but at least -120, where the largest finite value counts.  x / 2^e is
+ * rounded to nearest even; infinities and NaN become NaN.  Products of the rounded operands are exact.  For fp32 results they are summed in
+ * fp32 (operands as bf16 numbers: from 1.9375 * 2^127 on they are infinities); for 16-bit results by the 8-bit matrix cores, which cut off
+ * what lies 2^-13 below the largest (its power of two) of the products of eight consecutive channels, and add the rest in fp32.
+ *
+ * adasum_linear_store puts the weight of a layer (outputs x width, row-major, at `offset` of the flat buffer `params`) into 8 bits, once
+ * as it is and once transposed, with the same blocks: adasum_linear_bytes, 16-byte aligned.  Layout: outputs rows of
+ * width rounded up to a whole block, width rows of outputs rounded up, zeros behind the last channel; then a byte e + 127 for each
+ * block, [blocks of outputs][blocks of width].  outputs and width at most 2^24.
+ */
+#define ADASUM_LINEAR_BLOCK 128
+ADASUM_API int adasum_linear_bytes(int64_t outputs, int64_t width, size_t* bytes);
+ADASUM_API int adasum_linear_store(const void* params, int dtype, int64_t offset, int64_t outputs, int64_t width,
+                                    void* weight, void* stream);
+/*
+ *   y[t][o]  = bias[o] + sum_i x8[t][i] * w8[o][i]           (bias: at bias_offset of params; negative: none, params may be NULL)
+ *   dx[t][i] = sum_o dy8[t][o] * w8[o][i]
+ * x, dy: any of the three types, put into 8 bits by the call; results in any of them, rounded once, and not overlapping any
+ * operand (ADASUM_ERR_ALIAS).  The workspace's size goes by the results' type, and does for both.  rows at most
+ * 2^31 - 65536.
+ */
+ADASUM_API int adasum_linear_workspace_bytes(int64_t rows, int64_t width, int64_t outputs, int out_dtype, size_t* bytes);
+ADASUM_API int adasum_linear(const void* weight, int64_t outputs, int64_t width, const void* x, int dtype, int64_t x_stride,
+                              int64_t rows, const void* params, int param_dtype, int64_t bias_offset,
+                              void* out, int out_dtype, int64_t out_stride, void* workspace, size_t workspace_bytes, void* stream);
+ADASUM_API int adasum_linear_grad(const void* weight, int64_t outputs, int64_t width, const void* dy, int dtype, int64_t dy_stride,
+                                   int64_t rows, void* dx, int dx_dtype, int64_t dx_stride,
+                                   void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- host-side planning, exposed for inspection and tests (no GPU needed) ---- */
 

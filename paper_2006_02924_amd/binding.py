@@ -27,6 +27,8 @@ NOALLOC_SCRATCH_BYTES = 64 << 20
 ID_I32, ID_I64 = 0, 1
 ACTS = {"relu": 0, "gelu": 1, "gelu_tanh": 2, "silu": 3}
 CHECKPOINT_BLOCK = 32
+NORMS = {"layer": 0, "rms": 1}
+LINEAR_BLOCK = 128
 
 EXPORTS = [
     "adasum_reduce", "adasum_reduce_ex", "adasum_reduce_noalloc", "adasum_workspace_bytes",
@@ -35,6 +37,8 @@ EXPORTS = [
     "adasum_embedding", "adasum_embedding_grad_workspace_bytes", "adasum_embedding_grad",
     "adasum_checkpoint_bytes", "adasum_checkpoint_store", "adasum_checkpoint_load", "adasum_checkpoint_act_grad",
     "adasum_checkpoint_weight_grad_workspace_bytes", "adasum_checkpoint_weight_grad",
+    "adasum_dropout", "adasum_join", "adasum_join_grad_workspace_bytes", "adasum_join_grad",
+    "adasum_linear_bytes", "adasum_linear_store", "adasum_linear_workspace_bytes", "adasum_linear", "adasum_linear_grad",
     "adasum_tile_capacity", "adasum_plan_tiles", "adasum_plan_levels", "adasum_plan_groups",
     "adasum_profile_enable", "adasum_profile_collect",
     "adasum_strerror", "adasum_last_hip_error", "adasum_version", "adasum_shutdown",
@@ -63,6 +67,27 @@ class Options(C.Structure):
         ("reserved1", C.c_int32),
         ("resident_wait_us", C.c_int32),
         ("reserved2", C.c_int32),
+    ]
+
+
+class JoinForm(C.Structure):
+    _fields_ = [
+        ("struct_bytes", C.c_uint32),
+        ("dtype", C.c_int32),
+        ("stream_dtype", C.c_int32),
+        ("norm", C.c_int32),
+        ("after", C.c_int32),
+        ("before", C.c_int32),
+        ("width", C.c_int64),
+        ("eps", C.c_double),
+        ("residual_scale", C.c_double),
+        ("dropout", C.c_double),
+        ("seed", C.c_uint64),
+        ("after_weight", C.c_int64),
+        ("after_bias", C.c_int64),
+        ("gate", C.c_int64),
+        ("before_weight", C.c_int64),
+        ("before_bias", C.c_int64),
     ]
 
 
@@ -110,6 +135,16 @@ def load() -> C.CDLL:
     lib.adasum_checkpoint_act_grad.argtypes = [vp, i64, i64, i32, vp, i32, i64, vp, i64, vp]
     lib.adasum_checkpoint_weight_grad_workspace_bytes.argtypes = [i64, i64, i64, i32, szp]
     lib.adasum_checkpoint_weight_grad.argtypes = [vp, i64, i64, vp, i32, i64, i64, vp, i32, i64, i64, i32, vp, C.c_size_t, vp]
+    u64, formp = C.c_uint64, C.POINTER(JoinForm)
+    lib.adasum_dropout.argtypes = [vp, i32, i64, i64, i64, C.c_double, u64, vp, vp, i64, vp]
+    lib.adasum_join.argtypes = [formp, vp, i32, vp, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp]
+    lib.adasum_join_grad_workspace_bytes.argtypes = [formp, i64, szp]
+    lib.adasum_join_grad.argtypes = [formp, vp, i32, vp, vp, i64, vp, i64, vp, i64, vp, i64, i64, vp, i64, vp, i64, vp, i32, i32, vp, C.c_size_t, vp]
+    lib.adasum_linear_bytes.argtypes = [i64, i64, szp]
+    lib.adasum_linear_store.argtypes = [vp, i32, i64, i64, i64, vp, vp]
+    lib.adasum_linear_workspace_bytes.argtypes = [i64, i64, i64, i32, szp]
+    lib.adasum_linear.argtypes = [vp, i64, i64, vp, i32, i64, i64, vp, i32, i64, vp, i32, i64, vp, C.c_size_t, vp]
+    lib.adasum_linear_grad.argtypes = [vp, i64, i64, vp, i32, i64, i64, vp, i32, i64, vp, C.c_size_t, vp]
     lib.adasum_tile_capacity.argtypes = []
     lib.adasum_plan_tiles.argtypes = [i64p, C.c_int, C.c_int64, C.POINTER(Tile), C.c_int64, i64p]
     lib.adasum_plan_levels.argtypes = [C.c_int, C.c_int, C.POINTER(C.c_int), C.c_int, C.POINTER(C.c_int)]
@@ -649,6 +684,229 @@ def adasum_checkpoint_weight_grad(checkpoint: Checkpoint, dy, grad, offset: int,
           outputs, grad.data_ptr(), _type_of(grad), offset, -1 if bias_offset is None else bias_offset, 1 if accumulate else 0,
           ws, ws_bytes)
     return grad
+
+
+# ---- between the layers -----------------------------------------------------------------
+
+def _step_of(step, dev):
+    """The address of a mask's step: one 64-bit number on the device."""
+    if step is None:
+        return None
+    if step.numel() != 1 or step.element_size() != 8 or step.get_device() != dev:
+        raise ValueError("step must be one 64-bit number on the device of the operands")
+    return step.data_ptr()
+
+
+def _same_rows(t, n, width, dtype, what):
+    """The distance of two rows of a tensor that must have n rows of `width` elements of `dtype`."""
+    have, _, stride = _rows_of(t, width, what)
+    if (have != n and width) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what} must have {n} rows of {dtype}")
+    return stride
+
+
+def adasum_dropout(x, p: float, seed: int, *, step=None, out=None, stream=None):
+    """Dropout of ``x`` ([..., width]) with the mask of ``seed`` (64 bits) and ``step`` (None, or a tensor of one int64 on the device); on
+    a gradient of the result, with the same two, the gradient of ``x``.  Returns ``out`` (made here when None; may be ``x``)."""
+    n, width, stride = _rows_of(x, None, "x")
+    if out is None:
+        out = _empty(tuple(x.shape), x.dtype, x.get_device(), stream)
+    out_stride = stride if out is x else _same_rows(out, n, width, x.dtype, "out")
+    dev = _device_of(x, out)
+    _call((_lib or load()).adasum_dropout, dev, stream, x.data_ptr(), _type_of(x), stride, n, width, p, seed, _step_of(step, dev), out.data_ptr(),
+          out_stride)
+    return out
+
+
+class Join:
+    """What happens between a block's output and the next block's input (see ``include/adasum.h``): which norms there are (``after`` the
+    block, ``before`` the next), of which kind, the residual stream's type and scale, dropout with its seed, and where in the
+    flat parameter (and gradient) buffer the vectors of ``width`` elements lie, None for those that are not there."""
+
+    def __init__(self, width: int, dtype, *, stream_dtype=None, norm: str = "layer", eps: float = 1e-5, after: bool = False, before: bool = True,
+                 residual_scale: float = 1.0, dropout: float = 0.0, seed: int = 0, after_weight: Optional[int] = None,
+                 after_bias: Optional[int] = None, gate: Optional[int] = None, before_weight: Optional[int] = None,
+                 before_bias: Optional[int] = None):
+        if norm not in NORMS:
+            raise ValueError(f"norm must be one of {', '.join(NORMS)}")
+        offsets = {"gate": gate}
+        if after:
+            offsets.update(after_weight=after_weight, after_bias=after_bias)
+        if before:
+            offsets.update(before_weight=before_weight, before_bias=before_bias)
+        if any(o is not None and o < 0 for o in offsets.values()):
+            raise ValueError("offsets must not be negative (None: no such vector)")
+        self.width, self.dtype, self.stream_dtype = width, dtype, stream_dtype or dtype
+        self.after, self.before, self.reads_x = bool(after), bool(before), bool(after) or gate is not None
+        f = JoinForm()
+        f.struct_bytes = C.sizeof(JoinForm)
+        f.dtype, f.stream_dtype, f.norm = _code_of(dtype), _code_of(self.stream_dtype), NORMS[norm]
+        f.after, f.before, f.width = int(self.after), int(self.before), width
+        f.eps, f.residual_scale, f.dropout, f.seed = eps, residual_scale, dropout, seed
+        for name in ("after_weight", "after_bias", "gate", "before_weight", "before_bias"):
+            offset = offsets.get(name)
+            setattr(f, name, -1 if offset is None else offset)
+        ends = [o + width for o in offsets.values() if o is not None]
+        self.elems = max(ends) if ends else 0      # the flat buffers hold at least these
+        self.form, self._ref = f, C.byref(f)
+
+    def _flat(self, t, what):
+        """(address, type) of a flat buffer that holds the vectors; t may be None where there are none."""
+        if t is None:
+            if self.elems:
+                raise ValueError(f"{what} must hold the form's vectors")
+            return None, F32
+        _flat(t, 0, self.elems, what)
+        return t.data_ptr(), _type_of(t)
+
+
+def adasum_join(join: Join, params, x, residual=None, *, step=None, h=None, y=None, keep_h: bool = True, stream=None):
+    """The new residual stream ``h`` and the next block's input ``y`` (None without the norm ``before``) of a block's output ``x`` and the
+    stream ``residual`` (None: none).  Returns (h, y), made here when None; without ``keep_h`` no h is made where none is given.
+    ``h`` may be ``residual``.  The gradient wants h where the form has ``before``."""
+    lib = _lib or load()
+    n, width, stride = _rows_of(x, join.width, "x")
+    if x.dtype != join.dtype:
+        raise ValueError("x must have the form's dtype")
+    dev = x.get_device()
+    if h is None and (keep_h or not join.before):
+        h = _empty(tuple(x.shape), join.stream_dtype, dev, stream)
+    if y is None:
+        if join.before:
+            y = _empty(tuple(x.shape), join.dtype, dev, stream)
+    elif not join.before:
+        raise ValueError("a form without the norm before the next block has no y")
+    there = [t for t in (params, residual, h, y) if t is not None]
+    _device_of(x, *there)
+    flat, flat_type = join._flat(params, "params")
+    h_stride = 0 if h is None else _same_rows(h, n, width, join.stream_dtype, "h")
+    y_stride = 0 if y is None else _same_rows(y, n, width, join.dtype, "y")
+    residual_stride = 0 if residual is None else _same_rows(residual, n, width, join.stream_dtype, "residual")
+    _call(lib.adasum_join, dev, stream, join._ref, flat, flat_type, _step_of(step, dev), x.data_ptr(), stride,
+          None if residual is None else residual.data_ptr(), residual_stride, n, None if h is None else h.data_ptr(), h_stride,
+          None if y is None else y.data_ptr(), y_stride)
+    return h, y
+
+
+def adasum_join_grad_workspace_bytes(join: Join, rows: int) -> int:
+    n = C.c_size_t(0)
+    check(load().adasum_join_grad_workspace_bytes(join._ref, rows, C.byref(n)))
+    return int(n.value)
+
+
+def adasum_join_grad(join: Join, params, grad, *, x=None, h=None, dy=None, dh=None, step=None, dx=None, dresidual=None,
+                     accumulate: bool = False, workspace=None, stream=None):
+    """The gradients of a join from those of y (``dy``) and h (``dh``): returns (dx, dresidual), made here when None, and writes (or adds)
+    those of the form's vectors at their offsets of the flat buffer ``grad``.  ``x`` (with ``after`` or a gate) and ``h`` (with
+    ``before``) are what the forward pass had and gave.  ``dresidual`` may be ``dh``, or False where it is not wanted."""
+    lib = _lib or load()
+    if join.before != (h is not None and dy is not None) or (not join.before and (h is not None or dy is not None)):
+        raise ValueError("h and dy are given exactly if the form has the norm before the next block")
+    if join.reads_x and x is None:
+        raise ValueError("x must be given with a norm after the block or a gate")
+    if dy is None and dh is None:
+        raise ValueError("no gradient comes in")
+    first, dtype = (dy, join.dtype) if dy is not None else (dh, join.stream_dtype)
+    n, width, _ = _rows_of(first, join.width, "the gradient")
+    dev = first.get_device()
+    if dx is None:
+        dx = _empty(tuple(first.shape), join.dtype, dev, stream)
+    if dresidual is None:
+        dresidual = _empty(tuple(first.shape), join.stream_dtype, dev, stream)
+    elif dresidual is False:
+        dresidual = None
+    rows = []
+    for t, dtype, what in ((x if join.reads_x else None, join.dtype, "x"), (h, join.stream_dtype, "h"), (dy, join.dtype, "dy"),
+                           (dh, join.stream_dtype, "dh")):
+        rows += (None, 0) if t is None else (t.data_ptr(), _same_rows(t, n, width, dtype, what))
+    to = []
+    for t, dtype, what in ((dx, join.dtype, "dx"), (dresidual, join.stream_dtype, "dresidual")):
+        to += (None, 0) if t is None else (t.data_ptr(), _same_rows(t, n, width, dtype, what))
+    _device_of(first, *[t for t in (params, grad, x, h, dy, dh, dx, dresidual) if t is not None])
+    flat, flat_type = join._flat(params, "params")
+    grads, grad_type = join._flat(grad, "grad")
+    ws, ws_bytes, _keep = _scratch(workspace, lambda: adasum_join_grad_workspace_bytes(join, n), dev, stream)
+    _call(lib.adasum_join_grad, dev, stream, join._ref, flat, flat_type, _step_of(step, dev), *rows, n, *to, grads, grad_type,
+          1 if accumulate else 0, ws, ws_bytes)
+    return dx, dresidual
+
+
+class Weight8:
+    """The weight of a linear layer, [outputs, width], in 8-bit floating point, as it is and transposed (see ``include/adasum.h`` for the
+    layout of ``data``, a 1-D tensor of bytes, made here when None)."""
+
+    def __init__(self, outputs: int, width: int, *, device=None, data=None):
+        import torch
+        n = C.c_size_t(0)
+        check(load().adasum_linear_bytes(outputs, width, C.byref(n)))
+        if data is None:
+            data = torch.empty(n.value, dtype=torch.uint8, device="cuda" if device is None else device)
+        elif data.dim() != 1 or data.element_size() != 1 or data.numel() != n.value or not data.is_contiguous():
+            raise ValueError(f"data must be a contiguous 1-D tensor of {n.value} bytes")
+        self.outputs, self.width, self.data = outputs, width, data
+
+
+def adasum_linear_store(params, offset: int, outputs: int, width: int, *, out: Optional[Weight8] = None, stream=None) -> Weight8:
+    """Puts the weight of ``outputs`` x ``width`` that lies at ``offset`` of the flat buffer ``params`` into 8 bits.  Returns the weight (made
+    here when None)."""
+    lib = _lib or load()
+    _flat(params, offset, outputs * width, "params")
+    if out is None:
+        size = C.c_size_t(0)
+        check(lib.adasum_linear_bytes(outputs, width, C.byref(size)))
+        import torch
+        out = Weight8(outputs, width, data=_empty(size.value, torch.uint8, params.get_device(), stream))
+    elif out.outputs != outputs or out.width != width:
+        raise ValueError("the weight was made for another shape")
+    dev = _device_of(params, out.data)
+    _call(lib.adasum_linear_store, dev, stream, params.data_ptr(), _type_of(params), offset, outputs, width, out.data.data_ptr())
+    return out
+
+
+def adasum_linear_workspace_bytes(rows: int, width: int, outputs: int, out_dtype) -> int:
+    n = C.c_size_t(0)
+    check(load().adasum_linear_workspace_bytes(rows, width, outputs, _code_of(out_dtype), C.byref(n)))
+    return int(n.value)
+
+
+def adasum_linear(weight: Weight8, x, *, params=None, bias_offset: Optional[int] = None, out=None, out_dtype=None, workspace=None, stream=None):
+    """``x`` ([..., width], put into 8 bits here) times the transpose of a weight in 8 bits, plus the bias at ``bias_offset`` of the flat
+    buffer ``params`` (None: no bias).  Returns ``out``, [..., outputs] (made here when None)."""
+    n, width, stride = _rows_of(x, weight.width, "x")
+    outputs = weight.outputs
+    if out is None:
+        out = _empty((*x.shape[:-1], outputs), out_dtype or x.dtype, x.get_device(), stream)
+        out_stride = outputs
+    else:
+        out_stride = _same_rows(out, n, outputs, out_dtype, "out")
+    bias, bias_type = None, F32
+    if bias_offset is not None:
+        _flat(params, bias_offset, outputs, "params")
+        bias, bias_type = params.data_ptr(), _type_of(params)
+        dev = _device_of(x, weight.data, out, params)
+    else:
+        dev = _device_of(x, weight.data, out)
+    ws, ws_bytes, _keep = _scratch(workspace, lambda: adasum_linear_workspace_bytes(n, width, outputs, out.dtype), dev, stream)
+    _call((_lib or load()).adasum_linear, dev, stream, weight.data.data_ptr(), outputs, width, x.data_ptr(), _type_of(x), stride, n, bias, bias_type,
+          -1 if bias_offset is None else bias_offset, out.data_ptr(), _type_of(out), out_stride, ws, ws_bytes)
+    return out
+
+
+def adasum_linear_grad(weight: Weight8, dy, *, out=None, out_dtype=None, workspace=None, stream=None):
+    """The gradient of a layer's input: ``dy`` ([..., outputs], put into 8 bits here) times its weight in 8 bits.  Returns ``out``,
+    [..., width] (made here when None)."""
+    n, outputs, stride = _rows_of(dy, weight.outputs, "dy")
+    width = weight.width
+    if out is None:
+        out = _empty((*dy.shape[:-1], width), out_dtype or dy.dtype, dy.get_device(), stream)
+        out_stride = width
+    else:
+        out_stride = _same_rows(out, n, width, out_dtype, "out")
+    dev = _device_of(dy, weight.data, out)
+    ws, ws_bytes, _keep = _scratch(workspace, lambda: adasum_linear_workspace_bytes(n, width, outputs, out.dtype), dev, stream)
+    _call((_lib or load()).adasum_linear_grad, dev, stream, weight.data.data_ptr(), outputs, width, dy.data_ptr(), _type_of(dy), stride, n,
+          out.data_ptr(), _type_of(out), out_stride, ws, ws_bytes)
+    return out
 
 
 # ---- planning (host only) ---------------------------------------------------------

@@ -20,10 +20,12 @@ LIB_PATH = os.path.join(HERE, "libadasum.so")
 # a measuring tool (the memory system's ceiling for the combine pass's access pattern)
 CEILING_PATH = os.path.join(HERE, "pattern_ceiling")
 
-# (source, defines): the resident kernels are compiled once per storage type of the gradients and range of worker counts
+# (source, defines): the resident kernels are compiled once per storage type of the gradients and range of worker counts, the join's once per
+# pair of storage types
 SOURCES = [("adasum_resident.hip", [f"-DADASUM_LEAF_TYPE={t}", f"-DADASUM_WIDE_GROUPS={w}"])
            for t, w in ((0, 0), (1, 0), (2, 0), (3, 0), (0, 1), (1, 1), (2, 1))] + [
     ("adasum_kernels.hip", []), ("adasum_weight_grad.hip", []), ("adasum_embedding.hip", []), ("adasum_checkpoint.hip", []),
+    *[("adasum_join.hip", [f"-DADASUM_JOIN_TYPES={k}"]) for k in range(5)], ("adasum_linear.hip", []), ("adasum_dropout.hip", []),
     ("adasum_api.cpp", []), ("adasum_layers.cpp", []), ("adasum_weight_split.cpp", []), ("adasum_plan.cpp", [])]
 
 # -packed-fp32-ops off: the compiler must not form packed fp32 instructions.

@@ -14,9 +14,6 @@
 namespace adasum {
 namespace {
 
-constexpr int kG = 8;            // channels of a lane
-constexpr int kThreadsRow = 256;
-
 __device__ __forceinline__ unsigned quad_max(unsigned v) {
     v = max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0xb1, 0xf, 0xf, true)));   // lanes 1 0 3 2
     return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x4e, 0xf, 0xf, true)));   // 2 3 0 1
@@ -86,29 +83,6 @@ __device__ __forceinline__ float slope(float x) {
     } else {
         return logistic_slope(x, x);
     }
-}
-
-// What a launch works on: eight channels of a row up to the pitch are a granule, ITEMS of a lane's are in flight.
-struct RowWork {
-    long long rows;
-    int tokens;          // rows of a workgroup at a time
-    Divider granules;    // of a row
-};
-// The place of a lane's granule number g of n among rows `first` and on.
-struct Place {
-    long long row;
-    int at;
-};
-__device__ __forceinline__ Place place_of(const RowWork& work, long long first, unsigned g) {
-    const unsigned t = divide(g, work.granules);
-    return {first + t, static_cast<int>((g - t * work.granules.d) * kG)};
-}
-// f(first row, granules) for every run of rows that this workgroup has.
-template <typename F>
-__device__ __forceinline__ void every_rows(const RowWork& work, F&& f) {
-    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
-         first += static_cast<long long>(gridDim.x) * work.tokens)
-        f(first, static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d);
 }
 
 template <typename T, RowForm FORM, int ITEMS>
@@ -229,32 +203,6 @@ act_grad_kernel(const signed char* __restrict__ q, const signed char* __restrict
 // 32.1; 16777: 115 and 110; gelu, whose vector instructions take as long as its memory, 4194: 32 and 34; 16777: 118 and 122, and its
 // other form 34 and 37, 124 and 129.  fp16 is like bf16.  Operands that were just used are faster with one (4194, bf16: stores 18.5 and 21).
 constexpr int64_t kMany = 1 << 19, kManyOfSilu = 1 << 21;
-struct RowGrid {
-    RowWork work;
-    int64_t groups;
-    bool large;
-};
-RowGrid row_grid(int64_t rows, int64_t pitch, int dtype, int64_t many) {
-    RowGrid r;
-    const int64_t granules = pitch / kG;
-    r.large = dtype != ADASUM_F32 && rows * granules > many;
-    const int64_t per_group = r.large ? 4 * kThreadsRow : kThreadsRow;
-    const int64_t tokens = granules >= per_group ? 1 : per_group / granules;
-    r.work.rows = rows;
-    r.work.tokens = static_cast<int>(tokens);
-    r.work.granules = make_divider(static_cast<unsigned>(granules));
-    r.groups = at_most_groups((rows + tokens - 1) / tokens);
-    return r;
-}
-
-// f(granules of a lane in flight) as a constant.
-template <typename T, typename F>
-int with_items(const RowGrid& g, F&& f) {
-    if constexpr (sizeof(T) == 2) {
-        if (g.large) return f(std::integral_constant<int, 4>{});
-    }
-    return f(std::integral_constant<int, 1>{});
-}
 
 }  // namespace
 

@@ -1,0 +1,61 @@
+// gfx950 kernel of dropout whose mask is never stored: a stream like those of the checkpoints, eight channels a lane.
+#include <hip/hip_runtime.h>
+
+#include "adasum_layers.h"
+#include "adasum_mask.h"
+
+namespace adasum {
+namespace {
+
+// (x and out may be the same rows: a lane loads what it stores before it does)
+template <typename T, RowForm FORM, int ITEMS>
+__global__ void __launch_bounds__(kThreadsRow)
+dropout_kernel(const T* x, long long x_stride, int width, T* out, long long out_stride, Mask mask, RowWork work) {
+    constexpr bool NT = ITEMS > 1;
+    const Step step = step_of(mask);
+    every_rows(work, [&](long long first, unsigned n) {
+        for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
+            Granule<T, kG> raw[ITEMS];
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const Place p = place_of(work, first, min(base + kThreadsRow * k, n - 1));
+                load_row<FORM, NT>(raw[k], x + p.row * x_stride, p.at, width);
+            }
+#pragma unroll
+            for (int k = 0; k < ITEMS; ++k) {
+                const unsigned g = base + kThreadsRow * k;
+                if (g < n) {
+                    const Place p = place_of(work, first, g);
+                    unsigned w[4];
+                    mask_words(w, mask, step, static_cast<unsigned>(p.at) / kG, static_cast<unsigned>(p.row));
+                    float v[kG];
+                    unpack(raw[k], v);
+                    drop(v, w, mask);
+                    store_row<FORM, NT>(out + p.row * out_stride, v, p.at, width);
+                }
+            }
+        }
+    });
+}
+
+constexpr int64_t kMany = 1 << 19;
+
+}  // namespace
+
+int launch_dropout(const void* x, int dtype, int64_t x_stride, int64_t rows, int64_t width, double p, uint64_t seed, const void* step, void* out,
+                   int64_t out_stride, void* stream) {
+    const RowGrid g = row_grid(rows, (width + kG - 1) / kG * kG, dtype, kMany);
+    const Mask mask = make_mask(p, seed, step);
+    return with_type(dtype, [&](auto t) -> int {
+        typedef decltype(t) T;
+        return with_form(row_form(width, kG), [&](auto form) -> int {
+            constexpr RowForm F = decltype(form)::value;
+            return with_items<T>(g, [&](auto items) -> int {
+                return launch(dropout_kernel<T, F, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const T*>(x), x_stride,
+                              width, static_cast<T*>(out), out_stride, mask, g.work);
+            });
+        });
+    });
+}
+
+}  // namespace adasum

@@ -1,5 +1,6 @@
-// Internal declarations of the operators that fill a worker's gradient buffer: embedding tables, activation
-// checkpoints in 8 bits and the gradients made from them.  Nothing here is exported.
+// Internal declarations of the operators that fill a worker's gradient buffer (embedding tables, activation
+// checkpoints in 8 bits and the gradients made from them) and of those between the layers (dropout, the join of a
+// block with its residual stream, products in 8-bit floating point).  Nothing here is exported.
 #pragma once
 
 #include <cstddef>
@@ -127,5 +128,110 @@ struct WeightGrad {
     WeightSplit split;
 };
 int launch_weight_grad(const WeightGrad& g, void* stream);
+
+// ---- dropout (adasum_dropout.hip) ---------------------------------------------
+
+int launch_dropout(const void* x, int dtype, int64_t x_stride, int64_t rows, int64_t width, double p, uint64_t seed, const void* step,
+                   void* out, int64_t out_stride, void* stream);
+
+// ---- the join of a block with its residual stream (adasum_join.hip) -------------
+
+constexpr int64_t kMostJoined = 8192;   // channels of a row: what the lanes of a workgroup hold
+struct Matrix {
+    const void* p;
+    int64_t stride;
+};
+struct JoinCall {
+    const adasum_join_form* form;
+    const void* params;
+    int param_dtype;
+    const void* step;
+    int64_t rows;
+};
+struct JoinRows {
+    Matrix x, residual, h, y;
+};
+struct JoinGradRows {
+    Matrix x, h, dy, dh, dx, dresidual;
+};
+// The sums of the parameters' gradients: fp32 [group][kind][width].
+struct JoinLayout {
+    int groups = 0, kinds = 0;
+    size_t total = 0;
+};
+// Rows that a workgroup has in its lanes at once.
+inline int joined_at_once(int64_t width) { return width <= 128 ? 16 : width <= 1024 ? 4 : 1; }
+inline JoinLayout join_layout(const adasum_join_form& f, int64_t rows) {
+    JoinLayout lay;
+    const bool full = f.after || f.gate >= 0;
+    const bool any = f.gate >= 0 || (f.after && (f.after_weight >= 0 || f.after_bias >= 0)) ||
+                     (f.before && (f.before_weight >= 0 || f.before_bias >= 0));
+    const int64_t needed = (rows + joined_at_once(f.width) - 1) / joined_at_once(f.width);
+    lay.groups = static_cast<int>(needed < 512 ? needed : 512);
+    lay.kinds = !any ? 0 : full ? 5 : 2;
+    lay.total = static_cast<size_t>(lay.groups) * lay.kinds * f.width * 4;
+    return lay;
+}
+struct JoinSums {
+    JoinLayout layout;
+    void* ws;
+    void* grads[5];          // after weight and bias, gate, before weight and bias; null: none
+    int dtype, accumulate;
+};
+// By the storage types of activations and stream: 0 fp32, 1 bf16, 2 fp16, and 3 bf16, 4 fp16 with a stream of fp32.
+template <int TYPES> int launch_join(const JoinCall& c, const JoinRows& m, void* stream);
+template <int TYPES> int launch_join_grad(const JoinCall& c, const JoinGradRows& m, const JoinSums& to, void* stream);
+template <> int launch_join<0>(const JoinCall&, const JoinRows&, void*);
+template <> int launch_join<1>(const JoinCall&, const JoinRows&, void*);
+template <> int launch_join<2>(const JoinCall&, const JoinRows&, void*);
+template <> int launch_join<3>(const JoinCall&, const JoinRows&, void*);
+template <> int launch_join<4>(const JoinCall&, const JoinRows&, void*);
+template <> int launch_join_grad<0>(const JoinCall&, const JoinGradRows&, const JoinSums&, void*);
+template <> int launch_join_grad<1>(const JoinCall&, const JoinGradRows&, const JoinSums&, void*);
+template <> int launch_join_grad<2>(const JoinCall&, const JoinGradRows&, const JoinSums&, void*);
+template <> int launch_join_grad<3>(const JoinCall&, const JoinGradRows&, const JoinSums&, void*);
+template <> int launch_join_grad<4>(const JoinCall&, const JoinGradRows&, const JoinSums&, void*);
+
+// ---- linear layers in 8-bit floating point (adasum_linear.hip) ------------------
+
+constexpr int kBlock8 = ADASUM_LINEAR_BLOCK;
+inline int64_t blocks8(int64_t n) { return (n + kBlock8 - 1) / kBlock8; }
+// A weight: its rows, [outputs][blocks of width * 128] bytes, those of its transpose, [width][blocks of outputs * 128], and a byte for
+// each block, [blocks of outputs][blocks of width], e + 127.
+struct Weight8 {
+    unsigned char *q, *turned, *e;
+    int64_t outputs, width;
+};
+inline size_t weight8_bytes(int64_t outputs, int64_t width) {
+    return static_cast<size_t>(outputs) * blocks8(width) * kBlock8 + static_cast<size_t>(width) * blocks8(outputs) * kBlock8 +
+           align_up(static_cast<size_t>(blocks8(outputs)) * blocks8(width), 16);
+}
+inline Weight8 weight8_view(const void* weight, int64_t outputs, int64_t width) {
+    Weight8 w;
+    w.q = static_cast<unsigned char*>(const_cast<void*>(weight));
+    w.turned = w.q + outputs * blocks8(width) * kBlock8;
+    w.e = w.turned + width * blocks8(outputs) * kBlock8;
+    w.outputs = outputs;
+    w.width = width;
+    return w;
+}
+int launch_weight8_store(const void* w, int dtype, const Weight8& to, void* stream);
+
+// out [rows][outputs] = x [rows][depth] times the transpose of w [outputs][depth] in 8 bits, and a bias.
+struct Product8 {
+    const unsigned char *w, *e;          // rows of whole blocks; the exponent of block (output, depth) is e[output * e_output + depth * e_depth]
+    int64_t outputs, depth, e_output, e_depth;
+    const void* x;
+    int dtype;
+    int64_t x_stride, rows;
+    const void* bias;                    // or null
+    int bias_dtype;
+    void* out;
+    int out_dtype;
+    int64_t out_stride;
+    char* ws;
+};
+size_t product8_workspace(int64_t rows, int64_t outputs, int64_t depth, int out_dtype);
+int launch_product8(const Product8& p, void* stream);
 
 }  // namespace adasum

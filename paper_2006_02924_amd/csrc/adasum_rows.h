@@ -229,6 +229,12 @@ __device__ __forceinline__ unsigned divide(unsigned n, const Divider& v) {
     return static_cast<unsigned>((static_cast<unsigned long long>(__umulhi(n, v.m)) + n) >> v.s);
 }
 
+// Workgroup `b` of n as the eight dies see it: consecutive workgroups go to dies in turn, and those of one die should share operands.
+__device__ __forceinline__ unsigned die_order(unsigned b, unsigned n) {
+    const unsigned die = b & 7, at = b >> 3, each = n >> 3, more = n & 7;
+    return die * each + (die < more ? die : more) + at;
+}
+
 // f(form) as a constant.
 template <typename F>
 int with_form(RowForm form, F&& f) {
@@ -251,6 +257,59 @@ template <typename F>
 int with_types(int a, int b, F&& f) {
     if (a == ADASUM_F64) return f(double{}, double{});
     return with_type(a, [&](auto ta) { return with_type(b, [&](auto tb) { return f(ta, tb); }); });
+}
+
+constexpr int kG = 8;            // channels of a lane
+constexpr int kThreadsRow = 256;
+
+// What a launch works on: eight channels of a row up to the pitch are a granule, ITEMS of a lane's are in flight.
+struct RowWork {
+    long long rows;
+    int tokens;          // rows of a workgroup at a time
+    Divider granules;    // of a row
+};
+// The place of a lane's granule number g of n among rows `first` and on.
+struct Place {
+    long long row;
+    int at;
+};
+__device__ __forceinline__ Place place_of(const RowWork& work, long long first, unsigned g) {
+    const unsigned t = divide(g, work.granules);
+    return {first + t, static_cast<int>((g - t * work.granules.d) * kG)};
+}
+// f(first row, granules) for every run of rows that this workgroup has.
+template <typename F>
+__device__ __forceinline__ void every_rows(const RowWork& work, F&& f) {
+    for (long long first = static_cast<long long>(blockIdx.x) * work.tokens; first < work.rows;
+         first += static_cast<long long>(gridDim.x) * work.tokens)
+        f(first, static_cast<unsigned>(min(static_cast<long long>(work.tokens), work.rows - first)) * work.granules.d);
+}
+
+struct RowGrid {
+    RowWork work;
+    int64_t groups;
+    bool large;
+};
+inline RowGrid row_grid(int64_t rows, int64_t pitch, int dtype, int64_t many) {
+    RowGrid r;
+    const int64_t granules = pitch / kG;
+    r.large = dtype != ADASUM_F32 && rows * granules > many;
+    const int64_t per_group = r.large ? 4 * kThreadsRow : kThreadsRow;
+    const int64_t tokens = granules >= per_group ? 1 : per_group / granules;
+    r.work.rows = rows;
+    r.work.tokens = static_cast<int>(tokens);
+    r.work.granules = make_divider(static_cast<unsigned>(granules));
+    r.groups = at_most_groups((rows + tokens - 1) / tokens);
+    return r;
+}
+
+// f(granules of a lane in flight) as a constant.
+template <typename T, typename F>
+int with_items(const RowGrid& g, F&& f) {
+    if constexpr (sizeof(T) == 2) {
+        if (g.large) return f(std::integral_constant<int, 4>{});
+    }
+    return f(std::integral_constant<int, 1>{});
 }
 
 }  // namespace

@@ -72,12 +72,6 @@ __device__ __forceinline__ float plus_eight(f16_t, u32x4 a, float c) {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 
-// Workgroup `b` of n as the eight dies see it: consecutive workgroups go to dies in turn, and those of one die should share operands.
-__device__ __forceinline__ unsigned die_order(unsigned b, unsigned n) {
-    const unsigned die = b & 7, at = b >> 3, each = n >> 3, more = n & 7;
-    return die * each + (die < more ? die : more) + at;
-}
-
 // What a workgroup does, by the edge of its square of dW (TILE) and the storage type of dy.
 template <typename D, int TILE>
 struct GradShape {
