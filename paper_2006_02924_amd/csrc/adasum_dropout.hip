@@ -26,11 +26,15 @@ dropout_kernel(const T* x, long long x_stride, int width, T* out, long long out_
                 const unsigned g = base + kThreadsRow * k;
                 if (g < n) {
                     const Place p = place_of(work, first, g);
-                    unsigned w[4];
-                    mask_words(w, mask, step, static_cast<unsigned>(p.at) / kG, static_cast<unsigned>(p.row));
                     float v[kG];
                     unpack(raw[k], v);
-                    drop(v, w, mask);
+                    if (mask.drops) {
+                        unsigned w[4];
+                        bool keep[kG];
+                        mask_words(w, mask, step, static_cast<unsigned>(p.at) / kG, static_cast<unsigned>(p.row));
+                        kept(keep, w, mask.below);
+                        drop(v, keep, mask.factor);
+                    }
                     store_row<FORM, NT>(out + p.row * out_stride, v, p.at, width);
                 }
             }

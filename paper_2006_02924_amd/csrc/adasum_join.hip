@@ -29,20 +29,28 @@ typedef f16_t T; typedef float S;
 
 // ---- sums over the lanes of a row ---------------------------------------------
 
-template <int N>
-__device__ __forceinline__ float turned(float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+template <int ORDER>
+__device__ __forceinline__ float moved(float x) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ORDER, 0xf, 0xf, true));
 }
-// Over each run of 16 or 64 lanes, in every lane of it.
+// Over each run of 8, 16, 32 or 64 lanes, in every lane of it.
 template <int LANES>
 __device__ __forceinline__ float lanes_sum(float v) {
-    v += turned<8>(v);
-    v += turned<4>(v);
-    v += turned<2>(v);
-    v += turned<1>(v);
+    if constexpr (LANES == 8) {
+        v += moved<0xb1>(v);       // 1 0 3 2 of every four lanes
+        v += moved<0x4e>(v);       // 2 3 0 1
+        v += moved<0x141>(v);      // the eight lanes from the last to the first
+    } else {
+        v += moved<0x128>(v);      // eight, four, two and one on, round the sixteen
+        v += moved<0x124>(v);
+        v += moved<0x122>(v);
+        v += moved<0x121>(v);
+    }
     if constexpr (LANES > 16) {
         const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    if constexpr (LANES > 32) {
         const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
     }
@@ -52,27 +60,27 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // next but one sum has passed the barrier behind which all have read this one.
 template <int LANES>
 struct RowSums {
-    static constexpr int kWaves = LANES > 64 ? LANES / 64 : 1;
-    float (*shared)[2][kWaves];   // [2]
+    static constexpr int kWaves = LANES > 64 ? LANES / 64 : 1, kRows = LANES > 64 && LANES < 256 ? 256 / LANES : 1;
+    float (*shared)[2][kRows][kWaves];   // [2]
     int turn = 0;
     template <int N>
     __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] = lanes_sum<LANES>(v[i]);
         if constexpr (LANES > 64) {
-            float(&at)[2][kWaves] = shared[turn];
+            float(&at)[2][kRows][kWaves] = shared[turn];
             turn ^= 1;
-            const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+            const int lane = threadIdx.x & 63, row = threadIdx.x / LANES, wave = threadIdx.x % LANES / 64;
             if (lane == 0) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) at[i][wave] = v[i];
+                for (int i = 0; i < N; ++i) at[i][row][wave] = v[i];
             }
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[i] = 0.f;
 #pragma unroll
-                for (int w = 0; w < kWaves; ++w) v[i] += at[i][w];
+                for (int w = 0; w < kWaves; ++w) v[i] += at[i][row][w];
             }
         }
     }
@@ -85,25 +93,37 @@ struct RowSums {
 
 // ---- a row's part in a lane ---------------------------------------------------
 
-template <int LANES, int V, RowForm FORM>
+// (FILLED: whole granules, as many as there are lanes for: no lane has to ask whether its channels are there)
+template <int LANES, int V, RowForm FORM, bool FILLED>
 struct Row {
     typedef float Part[V][kG];
-    static constexpr int threads = LANES > 256 ? LANES : 256;
+    static constexpr int lanes = LANES, threads = LANES > 256 ? LANES : 256;
     static constexpr int rows_at_once = threads / LANES;
     int width, lane;
     __device__ __forceinline__ int at(int k) const { return (k * LANES + lane) * kG; }
-    __device__ __forceinline__ bool there(int k, int i) const { return FORM == kWhole ? at(k) < width : at(k) + i < width; }
+    __device__ __forceinline__ bool there(int k, int i) const { return FILLED || (FORM == kWhole ? at(k) < width : at(k) + i < width); }
+    // (a last granule that is shorter is loaded as the row's last eight channels, and moved down when it is needed: nothing waits here)
     template <typename E>
     __device__ __forceinline__ void load(Granule<E, kG> (&raw)[V], const E* row) const {
 #pragma unroll
-        for (int k = 0; k < V; ++k) load_row<FORM>(raw[k], row, at(k), width);
+        for (int k = 0; k < V; ++k) {
+            if constexpr (FILLED) load_any(raw[k], row + at(k));
+            else if constexpr (FORM == kRagged) load_any(raw[k], row + min(at(k), width - kG));
+            else load_row<FORM>(raw[k], row, at(k), width);
+        }
     }
     // zeros where there is no channel
     template <typename E>
     __device__ __forceinline__ void values(Part& v, const Granule<E, kG> (&raw)[V]) const {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            unpack(raw[k], v[k]);
+            if constexpr (FORM == kRagged) {
+                Granule<E, kG> g = raw[k];
+                if (__any(at(k) < width && at(k) > width - kG)) move_down(g, at(k) - min(at(k), width - kG));
+                unpack(g, v[k]);
+            } else {
+                unpack(raw[k], v[k]);
+            }
 #pragma unroll
             for (int i = 0; i < kG; ++i)
                 if (!there(k, i)) v[k][i] = 0.f;
@@ -112,8 +132,10 @@ struct Row {
     template <typename E>
     __device__ __forceinline__ void store(E* row, const Part& v) const {
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            if (at(k) < width) store_row<FORM>(row, v[k], at(k), width);
+        for (int k = 0; k < V; ++k) {
+            if (FILLED) store_any<kG>(row + at(k), v[k]);
+            else if (at(k) < width) store_row<FORM>(row, v[k], at(k), width);
+        }
     }
     // a vector of parameters, or `instead`
     __device__ __forceinline__ void param(Part& v, const void* p, int type, float instead) const {
@@ -170,11 +192,36 @@ struct Row {
 #pragma unroll
         for (int k = 0; k < V; ++k)
 #pragma unroll
-            for (int i = 0; i < kG; ++i) d[k][i] = r * (d[k][i] - __builtin_fmaf(hat[k][i], inner, mean));
+            for (int i = 0; i < kG; ++i) d[k][i] = there(k, i) ? r * (d[k][i] - __builtin_fmaf(hat[k][i], inner, mean)) : 0.f;
     }
-    __device__ __forceinline__ void mask(unsigned (&w)[V][4], const Mask& m, Step step, long long row) const {
+    // two vectors' product, in the first one's place
+    __device__ __forceinline__ void times(Part& v, const Part& w) const {
 #pragma unroll
-        for (int k = 0; k < V; ++k) mask_words(w[k], m, step, static_cast<unsigned>(at(k)) / kG, static_cast<unsigned>(row));
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int i = 0; i < kG; ++i) v[k][i] *= w[k][i];
+    }
+    __device__ __forceinline__ void mask(bool (&keep)[V][kG], const Mask& m, Step step, long long row) const {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            unsigned w[4];
+            mask_words(w, m, step, static_cast<unsigned>(at(k)) / kG, static_cast<unsigned>(row));
+            kept(keep[k], w, m.below);
+        }
+    }
+};
+
+// A workgroup's rows: those that it has at once, and the ones after them, whose loads are issued before they are worked on.  All lanes go round
+// together; where there are no rows left, lanes take the last one again and store nothing of it.
+template <typename R>
+struct Rounds {
+    long long row, rows;
+    bool there;
+    __device__ __forceinline__ explicit Rounds(long long n) : rows(n) { at(static_cast<long long>(blockIdx.x) * R::rows_at_once); }
+    __device__ __forceinline__ void at(long long first) {
+        const long long r = first + threadIdx.x / R::lanes;
+        there = r < rows;
+        row = there ? r : rows - 1;
     }
 };
 
@@ -190,7 +237,7 @@ struct Args {
     S* dresidual;
     long long x_stride, residual_stride, h_stride, dy_stride, dh_stride, to_h_stride, to_y_stride, dx_stride, dresidual_stride, rows;
     const void *after_weight, *after_bias, *gate, *before_weight, *before_bias;
-    int param_type, width, after, before, centred, drop;
+    int param_type, width, after, before, centred;
     float eps, scale, each;     // each: one over the width
     Mask mask;
     float* parts;               // sums of the parameters' gradients: [workgroup][kind][width]
@@ -198,64 +245,66 @@ struct Args {
 };
 
 // FULL: with a norm of x, or a gate.
-template <int LANES, int V, RowForm FORM, bool FULL>
-__global__ void __launch_bounds__((Row<LANES, V, FORM>::threads))
+template <int LANES, int V, RowForm FORM, bool FILLED, bool FULL>
+__global__ void __launch_bounds__((Row<LANES, V, FORM, FILLED>::threads))
 join_kernel(Args a) {
-    typedef Row<LANES, V, FORM> R;
+    typedef Row<LANES, V, FORM, FILLED> R;
     typedef typename R::Part Part;
-    __shared__ float shared[2][2][RowSums<LANES>::kWaves];
+    __shared__ float shared[2][2][RowSums<LANES>::kRows][RowSums<LANES>::kWaves];
     RowSums<LANES> sums{shared};
     R r;
     r.width = a.width;
     r.lane = threadIdx.x % LANES;
+    if (a.rows == 0) return;
     const Step step = step_of(a.mask);
-    Part aw, ab, gate, bw, bb;
+    // (gate * dropout(hat * weight + bias) is taken as dropout(hat * (gate * weight) + gate * bias))
+    Part aw, ab, bw, bb;
     if constexpr (FULL) {
         r.param(aw, a.after_weight, a.param_type, 1.f);
         r.param(ab, a.after_bias, a.param_type, 0.f);
-        r.param(gate, a.gate, a.param_type, 1.f);
+        r.param(bw, a.gate, a.param_type, 1.f);
+        r.times(aw, bw);
+        r.times(ab, bw);
     }
     r.param(bw, a.before_weight, a.param_type, 1.f);
     r.param(bb, a.before_bias, a.param_type, 0.f);
-    // (rows of several waves: the workgroup's lanes go round together)
-    for (long long row = static_cast<long long>(blockIdx.x) * R::rows_at_once + threadIdx.x / LANES; row < a.rows;
-         row += static_cast<long long>(gridDim.x) * R::rows_at_once) {
-        Granule<T, kG> raw_x[V];
-        Granule<S, kG> raw_r[V];
+    Granule<T, kG> raw_x[V];
+    Granule<S, kG> raw_r[V];
+    auto load = [&](long long row) {
         r.load(raw_x, a.x + row * a.x_stride);
         if (a.residual != nullptr) r.load(raw_r, a.residual + row * a.residual_stride);
-        Part v;
+    };
+    Rounds<R> now(a.rows);
+    load(now.row);
+    const long long each = static_cast<long long>(gridDim.x) * R::rows_at_once;
+    for (long long first = static_cast<long long>(blockIdx.x) * R::rows_at_once; first < a.rows; first += each) {
+        const long long row = now.row;
+        const bool there = now.there;
+        Part v, res;
         r.values(v, raw_x);
+        if (a.residual != nullptr) r.values(res, raw_r);
+        now.at(first + each);
+        load(now.row);
         if constexpr (FULL) {
-            if (a.after) {
-                r.normed(v, sums, a.centred, a.eps, a.each);
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-#pragma unroll
-                    for (int i = 0; i < kG; ++i) v[k][i] = __builtin_fmaf(v[k][i], aw[k][i], ab[k][i]);
-            }
-        }
-        if (a.drop) {
-            unsigned w[V][4];
-            r.mask(w, a.mask, step, row);
-#pragma unroll
-            for (int k = 0; k < V; ++k) drop(v[k], w[k], a.mask);
-        }
-        if constexpr (FULL) {
+            if (a.after) r.normed(v, sums, a.centred, a.eps, a.each);
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
-                for (int i = 0; i < kG; ++i) v[k][i] *= gate[k][i];
+                for (int i = 0; i < kG; ++i) v[k][i] = __builtin_fmaf(v[k][i], aw[k][i], ab[k][i]);
+        }
+        if (a.mask.drops) {
+            bool keep[V][kG];
+            r.mask(keep, a.mask, step, row);
+#pragma unroll
+            for (int k = 0; k < V; ++k) drop(v[k], keep[k], a.mask.factor);
         }
         if (a.residual != nullptr) {
-            Part res;
-            r.values(res, raw_r);
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < kG; ++i) v[k][i] = __builtin_fmaf(a.scale, res[k][i], v[k][i]);
         }
-        if (a.to_h != nullptr) r.store(a.to_h + row * a.to_h_stride, v);
+        if (a.to_h != nullptr && there) r.store(a.to_h + row * a.to_h_stride, v);
         if (a.before) {
             // (a bias of the norm of x is there behind the row's end too)
 #pragma unroll
@@ -268,49 +317,70 @@ join_kernel(Args a) {
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < kG; ++i) v[k][i] = __builtin_fmaf(v[k][i], bw[k][i], bb[k][i]);
-            r.store(a.to_y + row * a.to_y_stride, v);
+            if (there) r.store(a.to_y + row * a.to_y_stride, v);
         }
     }
 }
 
-// The kinds of parameters in the order of their sums.
-enum { kAfterWeight, kAfterBias, kGate, kBeforeWeight, kBeforeBias };
+// What is summed over the rows, with D the gradient that comes to dropout, as it leaves of it, and v what the gate and the norm of x get to
+// see: x, normed where there is a norm.  The gradients of the weight and bias of that norm are gate * (sum of D v) and gate * (sum of D),
+// the gate's is weight * (sum of D v) + bias * (sum of D).
+enum { kAfterProduct, kAfter, kBeforeWeight, kBeforeBias };
 
-template <int LANES, int V, RowForm FORM, bool FULL>
-__global__ void __launch_bounds__((Row<LANES, V, FORM>::threads))
+template <int LANES, int V, RowForm FORM, bool FILLED, bool FULL>
+__global__ void __launch_bounds__((Row<LANES, V, FORM, FILLED>::threads))
 join_grad_kernel(Args a) {
-    typedef Row<LANES, V, FORM> R;
+    typedef Row<LANES, V, FORM, FILLED> R;
     typedef typename R::Part Part;
     constexpr int kFirst = FULL ? 0 : kBeforeWeight, kSums = kBeforeBias + 1 - kFirst;
-    __shared__ float shared[2][2][RowSums<LANES>::kWaves];
+    __shared__ float shared[2][2][RowSums<LANES>::kRows][RowSums<LANES>::kWaves];
     RowSums<LANES> sums{shared};
     R r;
     r.width = a.width;
     r.lane = threadIdx.x % LANES;
+    if (a.rows == 0) return;
     const Step step = step_of(a.mask);
-    Part aw, ab, gate, bw;
+    Part aw, bw;
     if constexpr (FULL) {
         r.param(aw, a.after_weight, a.param_type, 1.f);
-        r.param(ab, a.after_bias, a.param_type, 0.f);
-        r.param(gate, a.gate, a.param_type, 1.f);
+        r.param(bw, a.gate, a.param_type, 1.f);
+        r.times(aw, bw);
     }
     r.param(bw, a.before_weight, a.param_type, 1.f);
     Part total[kSums] = {};
-    for (long long row = static_cast<long long>(blockIdx.x) * R::rows_at_once + threadIdx.x / LANES; row < a.rows;
-         row += static_cast<long long>(gridDim.x) * R::rows_at_once) {
-        Granule<T, kG> raw_x[V], raw_dy[V];
-        Granule<S, kG> raw_h[V], raw_dh[V];
+    Granule<T, kG> raw_x[V], raw_dy[V];
+    Granule<S, kG> raw_h[V], raw_dh[V];
+    auto load = [&](long long row) {
         if (a.before) {
             r.load(raw_dy, a.dy + row * a.dy_stride);
             r.load(raw_h, a.h + row * a.h_stride);
         }
         if (a.dh != nullptr) r.load(raw_dh, a.dh + row * a.dh_stride);
         if constexpr (FULL) r.load(raw_x, a.x + row * a.x_stride);
-        Part d = {};
+    };
+    Rounds<R> now(a.rows);
+    load(now.row);
+    const long long each = static_cast<long long>(gridDim.x) * R::rows_at_once;
+    for (long long first = static_cast<long long>(blockIdx.x) * R::rows_at_once; first < a.rows; first += each) {
+        const long long row = now.row;
+        const bool there = now.there;
+        Part d = {}, dh = {}, hat, v;
         if (a.before) {
-            Part hat;
             r.values(hat, raw_h);
             r.values(d, raw_dy);
+        }
+        if (a.dh != nullptr) r.values(dh, raw_dh);
+        if constexpr (FULL) r.values(v, raw_x);
+        now.at(first + each);
+        load(now.row);
+        // (a row that is not there adds zeros)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+#pragma unroll
+            for (int i = 0; i < kG; ++i) {
+                if (!there) d[k][i] = dh[k][i] = 0.f;
+            }
+        if (a.before) {
             const float spread = r.normed(hat, sums, a.centred, a.eps, a.each);
 #pragma unroll
             for (int k = 0; k < V; ++k)
@@ -322,14 +392,12 @@ join_grad_kernel(Args a) {
             r.norm_grad(d, bw, hat, spread, sums, a.centred, a.each);
         }
         if (a.dh != nullptr) {
-            Part dh;
-            r.values(dh, raw_dh);
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < kG; ++i) d[k][i] += dh[k][i];
         }
-        if (a.dresidual != nullptr) {
+        if (a.dresidual != nullptr && there) {
             Part scaled;
 #pragma unroll
             for (int k = 0; k < V; ++k)
@@ -337,41 +405,35 @@ join_grad_kernel(Args a) {
                 for (int i = 0; i < kG; ++i) scaled[k][i] = a.scale * d[k][i];
             r.store(a.dresidual + row * a.dresidual_stride, scaled);
         }
-        // (what dropout leaves of d; its gradient is taken through the gate)
-        unsigned w[V][4];
-        if (a.drop) {
-            r.mask(w, a.mask, step, row);
+        bool keep[V][kG];
+        if (a.mask.drops) {
+            r.mask(keep, a.mask, step, row);
 #pragma unroll
-            for (int k = 0; k < V; ++k) drop(d[k], w[k], a.mask);
+            for (int k = 0; k < V; ++k) drop(d[k], keep[k], a.mask.factor);
         }
         if constexpr (FULL) {
-            Part hat;
-            r.values(hat, raw_x);
             float spread = 1.f;
-            if (a.after) spread = r.normed(hat, sums, a.centred, a.eps, a.each);
+            if (a.after) {
+                spread = r.normed(v, sums, a.centred, a.eps, a.each);
+            } else {
+                // (what x holds in dropped places, or a row that is not there, adds nothing)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+#pragma unroll
+                    for (int i = 0; i < kG; ++i)
+                        if (!there || (a.mask.drops && !keep[k][i])) v[k][i] = 0.f;
+            }
 #pragma unroll
             for (int k = 0; k < V; ++k)
 #pragma unroll
                 for (int i = 0; i < kG; ++i) {
-                    const bool here = r.there(k, i);
-                    // (dropped places of x add nothing, whatever it holds there)
-                    const float v = a.after ? __builtin_fmaf(hat[k][i], aw[k][i], ab[k][i]) : hat[k][i];
-                    if (here && (!a.drop || keeps(w[k], i, a.mask.limit)))
-                        total[kGate - kFirst][k][i] = __builtin_fmaf(d[k][i], v, total[kGate - kFirst][k][i]);
-                    d[k][i] = here ? d[k][i] * gate[k][i] : 0.f;
+                    total[kAfterProduct - kFirst][k][i] = __builtin_fmaf(d[k][i], v[k][i], total[kAfterProduct - kFirst][k][i]);
+                    total[kAfter - kFirst][k][i] += d[k][i];
                 }
-            if (a.after) {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-#pragma unroll
-                    for (int i = 0; i < kG; ++i) {
-                        total[kAfterWeight - kFirst][k][i] = __builtin_fmaf(d[k][i], hat[k][i], total[kAfterWeight - kFirst][k][i]);
-                        total[kAfterBias - kFirst][k][i] += d[k][i];
-                    }
-                r.norm_grad(d, aw, hat, spread, sums, a.centred, a.each);
-            }
+            if (a.after) r.norm_grad(d, aw, v, spread, sums, a.centred, a.each);
+            else r.times(d, aw);
         }
-        r.store(a.dx + row * a.dx_stride, d);
+        if (there) r.store(a.dx + row * a.dx_stride, d);
     }
     if (a.parts == nullptr) return;
     // the workgroup's rows together, where it has several at once, then its sums to memory
@@ -403,49 +465,83 @@ join_grad_kernel(Args a) {
     }
 }
 
-// The parameters' gradients out of the workgroups' sums: a workgroup takes 64 channels of a kind, four waves a quarter of the sums each.
+// The parameters' gradients out of the workgroups' sums: a workgroup takes 16 channels, sixteen lanes of each share the sums; those of D v
+// and D together, as the gate's gradient is made of both.
 struct Finish {
     const float* parts;
-    int groups, kinds, width, accumulate;
-    void* to[5];                 // by place among the sums; null: not asked for
+    int groups, kinds, width, accumulate, param_type;
+    const void *after_weight, *after_bias, *gate;     // parameters
+    void* to[5];                                      // gradients of after weight and bias, gate, before weight and bias; null: not asked for
 };
+__device__ __forceinline__ double param_at(const void* p, int type, int j, double instead) {
+    if (p == nullptr) return instead;
+    if (type == ADASUM_F32) return load_elem(static_cast<const float*>(p) + j);
+    return type == ADASUM_BF16 ? load_elem(static_cast<const bf16_t*>(p) + j) : load_elem(static_cast<const f16_t*>(p) + j);
+}
 template <typename G>
 __global__ void __launch_bounds__(256) join_finish_kernel(Finish f) {
-    __shared__ double shared[4][64];
-    const int kind = blockIdx.y, lane = threadIdx.x & 63, way = threadIdx.x >> 6, j = blockIdx.x * 64 + lane;
-    G* const to = static_cast<G*>(f.to[kind]);
-    if (to == nullptr) return;
-    double sum = 0;
+    __shared__ double shared[2][16][17];
+    const int lane = threadIdx.x & 15, way = threadIdx.x >> 4, j = blockIdx.x * 16 + lane;
+    // (the sums of the norm before the next block are the last two)
+    const bool of_block = f.kinds == 4 && blockIdx.y == 0;
+    const float* const parts = f.parts + (of_block ? 0 : f.kinds - 2) * f.width;
+    double sum[2] = {};
     if (j < f.width) {
-#pragma unroll 4
-        for (int g = way; g < f.groups; g += 4) sum += f.parts[(static_cast<long long>(g) * f.kinds + kind) * f.width + j];
+#pragma unroll 8
+        for (int g = way; g < f.groups; g += 16) {
+            const float* const at = parts + static_cast<long long>(g) * f.kinds * f.width + j;
+            sum[0] += at[0];
+            sum[1] += at[f.width];
+        }
     }
-    shared[way][lane] = sum;
+    shared[0][way][lane] = sum[0];
+    shared[1][way][lane] = sum[1];
     __syncthreads();
-    if (way == 0 && j < f.width) {
-        sum = shared[0][lane] + shared[1][lane] + shared[2][lane] + shared[3][lane];
-        if (f.accumulate) sum += load_elem(to + j);
-        store_elem(to + j, static_cast<float>(sum));
+    if (way != 0 || j >= f.width) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) {
+        sum[0] += shared[0][w][lane];
+        sum[1] += shared[1][w][lane];
+    }
+    auto put = [&](void* grad, double v) {
+        if (grad == nullptr) return;
+        G* const to = static_cast<G*>(grad) + j;
+        store_elem(to, static_cast<float>(f.accumulate ? v + load_elem(to) : v));
+    };
+    if (of_block) {
+        const double gate = param_at(f.gate, f.param_type, j, 1.0);
+        put(f.to[0], gate * sum[0]);
+        put(f.to[1], gate * sum[1]);
+        put(f.to[2], param_at(f.after_weight, f.param_type, j, 1.0) * sum[0] + param_at(f.after_bias, f.param_type, j, 0.0) * sum[1]);
+    } else {
+        put(f.to[3], sum[0]);
+        put(f.to[4], sum[1]);
     }
 }
 
+// f(lanes of a row, granules of a lane, form of the row, whether it fills the lanes), as constants.
 template <typename F>
 int with_lanes(int64_t width, F&& f) {
-    auto whole_or_not = [&](auto lanes, auto items) -> int {
-        if (width % kG == 0) return f(lanes, items, std::integral_constant<RowForm, kWhole>{});
-        if constexpr (decltype(lanes)::value == 16) {
-            if (width < kG) return f(lanes, items, std::integral_constant<RowForm, kShort>{});
+    auto chosen = [&](auto lanes, auto items) -> int {
+        constexpr int kChannels = decltype(lanes)::value * decltype(items)::value * kG;
+        const std::integral_constant<RowForm, kWhole> whole;
+        if (width == kChannels) return f(lanes, items, whole, std::true_type{});
+        if (width % kG == 0) return f(lanes, items, whole, std::false_type{});
+        if constexpr (decltype(lanes)::value == 8) {
+            if (width < kG) return f(lanes, items, std::integral_constant<RowForm, kShort>{}, std::false_type{});
         }
-        return f(lanes, items, std::integral_constant<RowForm, kRagged>{});
+        return f(lanes, items, std::integral_constant<RowForm, kRagged>{}, std::false_type{});
     };
     typedef std::integral_constant<int, 1> One;
     typedef std::integral_constant<int, 2> Two;
-    if (width <= 128) return whole_or_not(std::integral_constant<int, 16>{}, One{});
-    if (width <= 512) return whole_or_not(std::integral_constant<int, 64>{}, One{});
-    if (width <= 1024) return whole_or_not(std::integral_constant<int, 64>{}, Two{});
-    if (width <= 2048) return whole_or_not(std::integral_constant<int, 256>{}, One{});
-    if (width <= 4096) return whole_or_not(std::integral_constant<int, 256>{}, Two{});
-    return whole_or_not(std::integral_constant<int, 1024>{}, One{});
+    if (width <= 64) return chosen(std::integral_constant<int, 8>{}, One{});
+    if (width <= 128) return chosen(std::integral_constant<int, 16>{}, One{});
+    if (width <= 256) return chosen(std::integral_constant<int, 32>{}, One{});
+    if (width <= 512) return chosen(std::integral_constant<int, 64>{}, One{});
+    if (width <= 1024) return chosen(std::integral_constant<int, 64>{}, Two{});
+    if (width <= 2048) return chosen(std::integral_constant<int, 256>{}, One{});
+    if (width <= 4096) return chosen(std::integral_constant<int, 256>{}, Two{});
+    return chosen(std::integral_constant<int, 512>{}, Two{});
 }
 
 Args args_of(const JoinCall& c) {
@@ -473,7 +569,6 @@ Args args_of(const JoinCall& c) {
     a.scale = static_cast<float>(f.residual_scale);
     a.each = static_cast<float>(1.0 / static_cast<double>(f.width));
     a.mask = make_mask(f.dropout, f.seed, c.step);
-    a.drop = a.mask.limit != 0;
     return a;
 }
 bool is_full(const adasum_join_form& f) { return f.after || f.gate >= 0; }
@@ -491,12 +586,14 @@ int launch_join<ADASUM_JOIN_TYPES>(const JoinCall& c, const JoinRows& m, void* s
     a.to_h_stride = m.h.stride;
     a.to_y = static_cast<T*>(const_cast<void*>(m.y.p));
     a.to_y_stride = m.y.stride;
-    return with_lanes(c.form->width, [&](auto lanes, auto items, auto form) -> int {
+    return with_lanes(c.form->width, [&](auto lanes, auto items, auto form, auto filled) -> int {
         constexpr int L = decltype(lanes)::value, V = decltype(items)::value;
         constexpr RowForm F = decltype(form)::value;
-        typedef Row<L, V, F> R;
-        const int64_t needed = (c.rows + R::rows_at_once - 1) / R::rows_at_once, most = 2048;
-        return launch(is_full(*c.form) ? join_kernel<L, V, F, true> : join_kernel<L, V, F, false>, needed < most ? needed : most, 1, R::threads, 0,
+        constexpr bool E = decltype(filled)::value;
+        typedef Row<L, V, F, E> R;
+        const int64_t needed = (c.rows + R::rows_at_once - 1) / R::rows_at_once;
+        const int64_t most = join_groups(c.form->width, is_full(*c.form), false);
+        return launch(is_full(*c.form) ? join_kernel<L, V, F, E, true> : join_kernel<L, V, F, E, false>, needed < most ? needed : most, 1, R::threads, 0,
                       stream, a);
     });
 }
@@ -521,18 +618,19 @@ int launch_join_grad<ADASUM_JOIN_TYPES>(const JoinCall& c, const JoinGradRows& m
     const bool full = is_full(*c.form);
     const int groups = to.layout.groups;
     if (groups > 0) {
-        const int rc = with_lanes(c.form->width, [&](auto lanes, auto items, auto form) -> int {
+        const int rc = with_lanes(c.form->width, [&](auto lanes, auto items, auto form, auto filled) -> int {
             constexpr int L = decltype(lanes)::value, V = decltype(items)::value;
             constexpr RowForm F = decltype(form)::value;
-            return launch(full ? join_grad_kernel<L, V, F, true> : join_grad_kernel<L, V, F, false>, groups, 1, Row<L, V, F>::threads, 0, stream, a);
+            constexpr bool E = decltype(filled)::value;
+            return launch(full ? join_grad_kernel<L, V, F, E, true> : join_grad_kernel<L, V, F, E, false>, groups, 1, Row<L, V, F, E>::threads, 0, stream, a);
         });
         if (rc != 0) return rc;
     }
     if (to.layout.kinds == 0) return 0;
-    Finish f{a.parts, groups, to.layout.kinds, a.width, to.accumulate, {}};
-    for (int s = 0; s < to.layout.kinds; ++s) f.to[s] = to.grads[full ? s : s + kBeforeWeight];
+    Finish f{a.parts, groups, to.layout.kinds, a.width, to.accumulate, a.param_type, a.after_weight, a.after_bias, a.gate, {}};
+    for (int s = 0; s < 5; ++s) f.to[s] = to.grads[s];
     return with_type(to.dtype, [&](auto g) -> int {
-        return launch(join_finish_kernel<decltype(g)>, (a.width + 63) / 64, to.layout.kinds, 256, 0, stream, f);
+        return launch(join_finish_kernel<decltype(g)>, (a.width + 15) / 16, to.layout.kinds / 2, 256, 0, stream, f);
     });
 }
 

@@ -160,15 +160,26 @@ struct JoinLayout {
     size_t total = 0;
 };
 // Rows that a workgroup has in its lanes at once.
-inline int joined_at_once(int64_t width) { return width <= 128 ? 16 : width <= 1024 ? 4 : 1; }
+inline int joined_at_once(int64_t width) { return width <= 64 ? 32 : width <= 128 ? 16 : width <= 256 ? 8 : width <= 1024 ? 4 : 1; }
+// Workgroups that go round the rows: what the chip holds at once, by the registers that a row's lanes take; the gradient has half of that
+// where the sums of more would cost what the rest gains.  16.8 million elements in bf16, no operand in a cache, with 512, 768, 1024, 1280 and
+// 2048: width 512 33, 29, 28, 28 and 30 us; 1024 27, 28, 27, 31 and 30, with two norms and a gate 30, 29, 33, 33 and 33; 8192 28, 31, 31, 32
+// and 32.  Gradients with 256, 512 and 1024: width 512 75, 50 and 43, with two norms and a gate 68, 49 and 57; 1024 51, 41 and 47;
+// 8192 49, 59 and 77.
+inline int join_groups(int64_t width, bool full, bool gradient) {
+    const bool one = width <= 512 || (width > 1024 && width <= 2048);   // granule a lane
+    if (gradient) return one && !full ? 1024 : width <= 4096 ? 512 : 256;
+    return one ? 1024 : width <= 4096 ? 768 : 512;
+}
 inline JoinLayout join_layout(const adasum_join_form& f, int64_t rows) {
     JoinLayout lay;
     const bool full = f.after || f.gate >= 0;
     const bool any = f.gate >= 0 || (f.after && (f.after_weight >= 0 || f.after_bias >= 0)) ||
                      (f.before && (f.before_weight >= 0 || f.before_bias >= 0));
     const int64_t needed = (rows + joined_at_once(f.width) - 1) / joined_at_once(f.width);
-    lay.groups = static_cast<int>(needed < 512 ? needed : 512);
-    lay.kinds = !any ? 0 : full ? 5 : 2;
+    const int64_t most = join_groups(f.width, full, true);
+    lay.groups = static_cast<int>(needed < most ? needed : most);
+    lay.kinds = !any ? 0 : full ? 4 : 2;
     lay.total = static_cast<size_t>(lay.groups) * lay.kinds * f.width * 4;
     return lay;
 }

@@ -251,157 +251,247 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(Product8 p, long long t
     }
 }
 
-typedef __attribute__((address_space(1))) const void* global_ptr;
-typedef __attribute__((address_space(3))) void* lds_ptr;
-
-// TILE x TILE of the result: what a workgroup computes.  Both operands come in rows along the depth, 128 bytes a step (a block of 8-bit
-// numbers, 64 of 16 bits), and go to LDS past the registers.  A row's eight pieces of 16 bytes lie in LDS at their number exclusive-or half
-// the row's, so that sixteen rows' same piece lies in all banks.
+// TILE x TILE of the result: what a workgroup of four waves computes.  Both operands come in rows along the depth, 128 bytes a step (a block
+// of 8-bit numbers, 64 of 16 bits), and go to LDS past the registers.  A row's eight pieces of 16 bytes lie in LDS at their number
+// exclusive-or half the row's, so that sixteen rows' same piece lies in all banks.
 template <int TILE>
 struct ProductShape {
-    static constexpr int waves_o = 2, waves_t = TILE == 256 ? 4 : 2, threads = 64 * waves_o * waves_t;
-    static constexpr int frags_o = TILE / 16 / waves_o, frags_t = TILE / 16 / waves_t;   // of 16 rows
+    static constexpr int threads = 256, frags = TILE / 32;                 // of 16 rows, a wave along each side
     static constexpr int operand_bytes = TILE * kBlock8, buffer_bytes = 2 * operand_bytes, lds_bytes = 2 * buffer_bytes;
-    static constexpr int loads = operand_bytes / (threads * 16);                          // of an operand, a lane
+    static constexpr int loads = operand_bytes / (threads * 16);           // of an operand, a lane
 };
 
 struct Large {
     const unsigned char *w, *x;           // rows `pitch` bytes apart
     const unsigned char *e_w, *e_x;       // exponents (not EXACT): [output / 128 * e_output + block * e_depth], [block * tokens + place]
-    long long pitch, outputs, rows, e_output, e_depth, tokens;
+    long long outputs, rows, e_output, e_depth, tokens;
     const void* bias;
+    unsigned pitch;
     int bias_dtype, steps;
     long long out_stride;
     unsigned tiles_o, tiles_t;
 };
 
+// Sixteen bytes a lane from base + offset to LDS, a wave's one after the other from `to` on.  (The builtin makes every later read of LDS wait
+// for it, of whatever place.  There is no register that the load writes; the loop below waits for it by itself.)
+__device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned offset, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void wait_for_all() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
+    asm volatile("" ::: "memory");
+}
+
+// f(0) .. f(N - 1), as constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void every(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        every<N, I + 1>(f);
+    }
+}
+
 template <bool EXACT, int TILE, typename O>
-__global__ void __launch_bounds__((ProductShape<TILE>::threads), 2) product_kernel(Large p, O* __restrict__ out) {
+__global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large p, O* __restrict__ out) {
     typedef ProductShape<TILE> S;
-    constexpr int FO = S::frags_o, FT = S::frags_t;
+    constexpr int F = S::frags;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned n = die_order(blockIdx.x, gridDim.x);
     const long long o0 = static_cast<long long>(n % p.tiles_o) * TILE, t0 = static_cast<long long>(n / p.tiles_o) * TILE;
-    const int wo = wave % S::waves_o * (16 * FO), wt = wave / S::waves_o * (16 * FT);
+    const int wo = wave % 2 * (16 * F), wt = wave / 2 * (16 * F);
 
-    // what a lane loads: a piece of each eighth row
-    const unsigned char *w_at[S::loads], *x_at[S::loads];
+    // what a lane loads: a piece of each 32nd row
+    const unsigned char *w_base = p.w + o0 * p.pitch, *x_base = p.x + t0 * p.pitch;
+    const int w_last = static_cast<int>(min(p.outputs - o0, static_cast<long long>(TILE))) - 1;
+    const int x_last = static_cast<int>(min(p.rows - t0, static_cast<long long>(TILE))) - 1;
+    unsigned w_at[S::loads], x_at[S::loads];
 #pragma unroll
     for (int k = 0; k < S::loads; ++k) {
-        const int row = (k * (S::threads / 64) + wave) * 8 + (lane >> 3), piece = (lane & 7) ^ (row >> 1 & 7);
-        w_at[k] = p.w + min(o0 + row, p.outputs - 1) * p.pitch + 16 * piece;
-        x_at[k] = p.x + min(t0 + row, p.rows - 1) * p.pitch + 16 * piece;
+        const int row = k * 32 + wave * 8 + (lane >> 3), piece = (lane & 7) ^ (row >> 1 & 7);
+        w_at[k] = min(row, w_last) * p.pitch + 16 * piece;
+        x_at[k] = min(row, x_last) * p.pitch + 16 * piece;
     }
     const unsigned char* e_w = EXACT ? nullptr : p.e_w + min(o0 + wo, p.outputs - 1) / kBlock8 * p.e_output;
     const unsigned char* e_x = EXACT ? nullptr : p.e_x + t0 + wt + (lane & 15) * 4;
-    unsigned of_w = 0, of_x = 0, next_w = 0, next_x = 0;
+    // exponents of this step, of the next, and those that are being loaded; of the tokens, a word for each 64
+    constexpr int WORDS = F / 4;
+    unsigned of_w = 0, next_w = 0, coming_w = 0, of_x[WORDS] = {}, next_x[WORDS] = {}, coming_x[WORDS] = {};
+    const unsigned to = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(lds))) + wave * 1024;
     auto load = [&](int buffer) {
+        if constexpr (!EXACT) {
+            coming_w = *e_w;
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) coming_x[k] = *reinterpret_cast<const unsigned*>(e_x + 64 * k);
+        }
 #pragma unroll
         for (int k = 0; k < S::loads; ++k) {
-            char* const at = lds + buffer * S::buffer_bytes + (k * (S::threads / 64) + wave) * 1024;
-            __builtin_amdgcn_global_load_lds((global_ptr)(w_at[k]), (lds_ptr)(at), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_ptr)(x_at[k]), (lds_ptr)(at + S::operand_bytes), 16, 0, 0);
-            w_at[k] += kBlock8;
-            x_at[k] += kBlock8;
+            load_to_lds(w_base, w_at[k], to + buffer * S::buffer_bytes + k * 4096);
+            load_to_lds(x_base, x_at[k], to + buffer * S::buffer_bytes + S::operand_bytes + k * 4096);
         }
     };
-    auto load_exponents = [&] {
-        if constexpr (!EXACT) {
-            next_w = *e_w;
-            next_x = *reinterpret_cast<const unsigned*>(e_x);
-            e_w += p.e_depth;
-            e_x += p.tokens;
+    // (behind the last step it is loaded again, and not used)
+    int ahead = 0;
+    auto next = [&] {
+        if (ahead + 1 < p.steps) {
+            ++ahead;
+            w_base += kBlock8;
+            x_base += kBlock8;
+            if constexpr (!EXACT) {
+                e_w += p.e_depth;
+                e_x += p.tokens;
+            }
         }
     };
     // what it reads: of a row, pieces g and g + 4 for its group g of lanes
     const int row = lane & 15, group = lane >> 4, first = 16 * (group ^ (row >> 1)), second = 16 * ((group + 4) ^ (row >> 1));
     const char* const w_read = lds + (wo + row) * kBlock8;
     const char* const x_read = lds + S::operand_bytes + (wt + row) * kBlock8;
-
-    f32x4 acc[FO][FT] = {};
-    load_exponents();
-    load(0);
-    for (int s = 0; s < p.steps; ++s) {
-        const int buffer = (s & 1) * S::buffer_bytes;
-        // (all of this step's loads are there, and all waves have read the last step's)
-        __builtin_amdgcn_s_waitcnt(0x0f70);
-        __syncthreads();
+    u32x4 fw[F][2], fx[F][2];
+    auto read_w = [&](int i, int from) {
+        fw[i][0] = *reinterpret_cast<const u32x4*>(w_read + from + i * 16 * kBlock8 + first);
+        fw[i][1] = *reinterpret_cast<const u32x4*>(w_read + from + i * 16 * kBlock8 + second);
+    };
+    auto read_x = [&](int j, int from) {
+        fx[j][0] = *reinterpret_cast<const u32x4*>(x_read + from + j * 16 * kBlock8 + first);
+        fx[j][1] = *reinterpret_cast<const u32x4*>(x_read + from + j * 16 * kBlock8 + second);
+    };
+    auto whole = [](const u32x4 (&f)[2]) {
+        i32x8 r;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            r[k] = static_cast<int>(f[0][k]);
+            r[4 + k] = static_cast<int>(f[1][k]);
+        }
+        return r;
+    };
+    f32x4 acc[F][F] = {};
+    auto multiply = [&](int i, auto number) {
+        constexpr int j = decltype(number)::value;
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[i][h]), __builtin_bit_cast(bf16x8, fx[j][h]), acc[i][j],
+                                                                    0, 0, 0);
+        } else {
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(fw[i]), whole(fx[j]), acc[i][j], 0, 0, 0, static_cast<int>(of_w), j % 4,
+                                                                         static_cast<int>(of_x[j / 4]));
+        }
+    };
+    auto came = [&] {
+        next_w = coming_w;
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) next_x[k] = coming_x[k];
+    };
+    auto turn = [&] {
         of_w = next_w;
-        of_x = next_x;
-        u32x4 fw[FO][2], fx[FT][2];
 #pragma unroll
-        for (int j = 0; j < FT; ++j) {
-            fx[j][0] = *reinterpret_cast<const u32x4*>(x_read + buffer + j * 16 * kBlock8 + first);
-            fx[j][1] = *reinterpret_cast<const u32x4*>(x_read + buffer + j * 16 * kBlock8 + second);
+        for (int k = 0; k < WORDS; ++k) of_x[k] = next_x[k];
+    };
+    load(0);
+    wait_for_all();
+    came();
+    turn();
+    next();
+    load(1);
+    __builtin_amdgcn_s_barrier();
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        read_x(i, 0);
+        read_w(i, 0);
+    }
+    // A step's products come out of registers.  Beside them the next step's operands are read, into the registers of those that have been
+    // used for the last time, and the loads of the step after are issued, into the buffer that this step's operands were in.
+    for (int s = 0; s < p.steps; ++s) {
+        const int other = ~s & 1, from = other * S::buffer_bytes;
+        every<F>([&](auto j) { multiply(0, j); });
+        __builtin_amdgcn_sched_barrier(0);
+        wait_for_all();
+        __builtin_amdgcn_s_barrier();
+        came();
+        next();
+        load(other ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 1; i < F - 2; ++i) {
+            read_w(i - 1, from);
+            every<F>([&](auto j) { multiply(i, j); });
+            __builtin_amdgcn_sched_barrier(0);
         }
+        read_w(F - 3, from);
+        every<F>([&](auto j) {
+            multiply(F - 2, j);
+            multiply(F - 1, j);
+            __builtin_amdgcn_sched_barrier(0);
+            read_x(j, from);
+        });
+        read_w(F - 2, from);
+        read_w(F - 1, from);
+        __builtin_amdgcn_sched_barrier(0);
+        turn();
+    }
+    // A lane has four consecutive outputs of a token in each 16 x 16.  Through LDS, some tokens of a wave at a time, sixteen lanes get a token's
+    // consecutive outputs to store.
+    wait_for_all();
+    __builtin_amdgcn_s_barrier();
+    constexpr int kOutputs = 16 * F, kRow = kOutputs * static_cast<int>(sizeof(O)) + 16;     // bytes of a token's row
+    constexpr int kOfLane = 16 / static_cast<int>(sizeof(O)), kLanes = kOutputs / kOfLane;   // outputs that a lane stores, lanes of a token
+    char* const mine = lds + wave * (S::lds_bytes / 4);
+    constexpr int kTogether = S::lds_bytes / 4 / (16 * kRow) < F ? S::lds_bytes / 4 / (16 * kRow) : F;   // of the token's sixteens
+    static_assert(kTogether >= 1, "");
+    float bias[F][4] = {};
+    if (p.bias != nullptr) {
 #pragma unroll
-        for (int i = 0; i < FO; ++i) {
-            fw[i][0] = *reinterpret_cast<const u32x4*>(w_read + buffer + i * 16 * kBlock8 + first);
-            fw[i][1] = *reinterpret_cast<const u32x4*>(w_read + buffer + i * 16 * kBlock8 + second);
-        }
-        if (s + 1 < p.steps) {
-            load_exponents();
-            load((s & 1) ^ 1);
-        }
-        auto whole = [](const u32x4 (&f)[2]) {
-            i32x8 r;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                r[k] = static_cast<int>(f[0][k]);
-                r[4 + k] = static_cast<int>(f[1][k]);
-            }
-            return r;
-        };
-#pragma unroll
-        for (int i = 0; i < FO; ++i) {
-            auto column = [&](auto number) {
-                constexpr int j = decltype(number)::value;
-                if constexpr (j < FT) {
-                    if constexpr (EXACT) {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[i][h]),
-                                                                                __builtin_bit_cast(bf16x8, fx[j][h]), acc[i][j], 0, 0, 0);
-                    } else {
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(fw[i]), whole(fx[j]), acc[i][j], 0, 0, 0,
-                                                                                     static_cast<int>(of_w), j, static_cast<int>(of_x));
-                    }
-                }
-            };
-            column(std::integral_constant<int, 0>{});
-            column(std::integral_constant<int, 1>{});
-            column(std::integral_constant<int, 2>{});
-            column(std::integral_constant<int, 3>{});
+        for (int i = 0; i < F; ++i) {
+            const long long o = o0 + wo + 16 * i + 4 * group;
+            const int there = static_cast<int>(min(p.outputs - o, 4ll));
+            if (there <= 0) continue;
+            if (p.bias_dtype == ADASUM_F32) load_some<4>(bias[i], static_cast<const float*>(p.bias) + o, there);
+            else if (p.bias_dtype == ADASUM_BF16) load_some<4>(bias[i], static_cast<const bf16_t*>(p.bias) + o, there);
+            else load_some<4>(bias[i], static_cast<const f16_t*>(p.bias) + o, there);
         }
     }
-    // a lane has four consecutive outputs of a token in each 16 x 16
 #pragma unroll
-    for (int i = 0; i < FO; ++i) {
-        const long long o = o0 + wo + 16 * i + 4 * group;
-        const int there = static_cast<int>(min(p.outputs - o, 4ll));
-        if (there <= 0) continue;
-        float bias[4] = {};
-        if (p.bias != nullptr) {
-            if (p.bias_dtype == ADASUM_F32) load_some<4>(bias, static_cast<const float*>(p.bias) + o, there);
-            else if (p.bias_dtype == ADASUM_BF16) load_some<4>(bias, static_cast<const bf16_t*>(p.bias) + o, there);
-            else load_some<4>(bias, static_cast<const f16_t*>(p.bias) + o, there);
-        }
+    for (int j0 = 0; j0 < F; j0 += kTogether) {
 #pragma unroll
-        for (int j = 0; j < FT; ++j) {
-            const long long t = t0 + wt + 16 * j + row;
-            if (t < p.rows) {
+        for (int j = j0; j < F && j < j0 + kTogether; ++j)
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
                 float v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = acc[i][j][k] + bias[k];
-                store_some<4>(out + t * p.out_stride + o, v, there);
+                for (int k = 0; k < 4; ++k) v[k] = acc[i][j][k] + bias[i][k];
+                store_any<4>(reinterpret_cast<O*>(mine + (16 * (j - j0) + row) * kRow) + 16 * i + 4 * group, v);
+            }
+        __builtin_amdgcn_wave_barrier();
+        const int tokens = 16 * (F - j0 < kTogether ? F - j0 : kTogether);
+#pragma unroll 4
+        for (int k = lane; k < tokens * kLanes; k += 64) {
+            const int token = k / kLanes, at = k % kLanes * kOfLane;
+            const long long t = t0 + wt + 16 * j0 + token, o = o0 + wo + at;
+            const u32x4 w = *reinterpret_cast<const u32x4*>(mine + token * kRow + at * static_cast<int>(sizeof(O)));
+            if (t >= p.rows || o >= p.outputs) continue;
+            O* const to_out = out + t * p.out_stride + o;
+            const int there = static_cast<int>(min(p.outputs - o, static_cast<long long>(kOfLane)));
+            if (there == kOfLane) {
+                store_at<false>(w, reinterpret_cast<u32x4_any*>(to_out));
+            } else {
+                unsigned words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int e = 0; e < kOfLane; ++e)
+                    if (e < there) {
+                        if constexpr (sizeof(O) == 4) to_out[e] = __uint_as_float(words[e]);
+                        else to_out[e].v = static_cast<unsigned short>(words[e / 2] >> (16 * (e & 1)));
+                    }
             }
         }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
 // The kernel of few tokens does the large ones' work where there are none to fill a tile.
-bool is_large(int64_t rows, int64_t outputs, int64_t depth) { return rows > 64 && depth > 0 && outputs >= 16; }
+// (A tile's rows are addressed with 32 bits.)
+bool is_large(int64_t rows, int64_t outputs, int64_t depth) { return rows > 64 && depth > 0 && depth <= (1 << 22) && outputs >= 16; }
 constexpr int64_t kTokenPad = 256;
 struct Workspace8 {
     size_t off_more = 0, total = 0;    // the exponents, or the weight's values

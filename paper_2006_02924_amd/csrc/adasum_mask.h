@@ -11,16 +11,19 @@ namespace {
 
 struct Mask {
     unsigned k0, k1;                   // the seed
-    unsigned limit;                    // kept: numbers not below it; 65536 drops everything
-    float factor;                      // of what is kept; 0 with that limit
+    bool drops;                        // else everything is kept
+    unsigned below;                    // kept: numbers above it (65535: none)
+    float factor;                      // of what is kept
     const unsigned* step;              // 64 bits on the device, or null (0)
 };
 inline Mask make_mask(double p, unsigned long long seed, const void* step) {
     Mask m;
     m.k0 = static_cast<unsigned>(seed);
     m.k1 = static_cast<unsigned>(seed >> 32);
-    m.limit = static_cast<unsigned>(65536.0 * p + 0.5);
-    m.factor = m.limit == 65536 ? 0.f : static_cast<float>(65536.0 / (65536.0 - m.limit));
+    const unsigned limit = static_cast<unsigned>(65536.0 * p + 0.5);
+    m.drops = limit != 0;
+    m.below = m.drops ? limit - 1 : 0;
+    m.factor = limit == 65536 ? 0.f : static_cast<float>(65536.0 / (65536.0 - limit));
     m.step = static_cast<const unsigned*>(step);
     return m;
 }
@@ -54,13 +57,17 @@ __device__ __forceinline__ void mask_words(unsigned (&w)[4], const Mask& m, Step
     w[2] = c2;
     w[3] = c3;
 }
-__device__ __forceinline__ bool keeps(const unsigned (&w)[4], int i, unsigned limit) {
-    return (i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu) >= limit;
+// (one comparison each: of the lower half by itself, of the upper one with what is below it in tow)
+__device__ __forceinline__ void kept(bool (&keep)[kG], const unsigned (&w)[4], unsigned below) {
+    const unsigned short half = static_cast<unsigned short>(below);
+    const unsigned top = below << 16 | 0xffffu;
+#pragma unroll
+    for (int i = 0; i < kG; ++i) keep[i] = i & 1 ? w[i / 2] > top : static_cast<unsigned short>(w[i / 2]) > half;
 }
 // (a choice and no product: what is dropped is 0 also where it was no number)
-__device__ __forceinline__ void drop(float (&v)[kG], const unsigned (&w)[4], const Mask& m) {
+__device__ __forceinline__ void drop(float (&v)[kG], const bool (&keep)[kG], float factor) {
 #pragma unroll
-    for (int i = 0; i < kG; ++i) v[i] = keeps(w, i, m.limit) ? v[i] * m.factor : 0.f;
+    for (int i = 0; i < kG; ++i) v[i] = keep[i] ? v[i] * factor : 0.f;
 }
 
 }  // namespace

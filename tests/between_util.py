@@ -139,7 +139,7 @@ def join_grad(form, flat, x, h, dy, dh, keep=None):
     rows = (dy if dy is not None else dh).shape[0]
     w = {name: vector(flat, form.get(name), width) for name in ("after_weight", "after_bias", "gate", "before_weight", "before_bias")}
     norm, eps, sums = form.get("norm", "layer"), form.get("eps", 1e-5), {}
-    depth = -(-rows // 512) + 16 + 8      # a lane's rows, those that a workgroup has at once, and the end
+    depth = -(-rows // 256) + 32 + 8      # a lane's rows (at least one of 256 workgroups has it), those that a workgroup has at once, and the end
     d = None
     if form.get("before", True):
         hat, r = normed(Bounded(h), norm, eps)
