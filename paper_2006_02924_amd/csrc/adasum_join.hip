@@ -283,8 +283,10 @@ join_kernel(Args a) {
         Part v, res;
         r.values(v, raw_x);
         if (a.residual != nullptr) r.values(res, raw_r);
-        now.at(first + each);
-        load(now.row);
+        if (first + each < a.rows) {
+            now.at(first + each);
+            load(now.row);
+        }
         if constexpr (FULL) {
             if (a.after) r.normed(v, sums, a.centred, a.eps, a.each);
 #pragma unroll
@@ -371,8 +373,10 @@ join_grad_kernel(Args a) {
         }
         if (a.dh != nullptr) r.values(dh, raw_dh);
         if constexpr (FULL) r.values(v, raw_x);
-        now.at(first + each);
-        load(now.row);
+        if (first + each < a.rows) {
+            now.at(first + each);
+            load(now.row);
+        }
         // (a row that is not there adds zeros)
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -592,8 +596,9 @@ int launch_join<ADASUM_JOIN_TYPES>(const JoinCall& c, const JoinRows& m, void* s
         constexpr bool E = decltype(filled)::value;
         typedef Row<L, V, F, E> R;
         const int64_t needed = (c.rows + R::rows_at_once - 1) / R::rows_at_once;
+        // (fewer than two rounds: each workgroup takes its rows and goes, so that the chip stays full to the end)
         const int64_t most = join_groups(c.form->width, is_full(*c.form), false);
-        return launch(is_full(*c.form) ? join_kernel<L, V, F, E, true> : join_kernel<L, V, F, E, false>, needed < most ? needed : most, 1, R::threads, 0,
+        return launch(is_full(*c.form) ? join_kernel<L, V, F, E, true> : join_kernel<L, V, F, E, false>, needed < 2 * most ? needed : most, 1, R::threads, 0,
                       stream, a);
     });
 }
