@@ -510,9 +510,9 @@ ADASUM_API int adasum_join_grad(const adasum_join_form* form, const void* params
  * what lies 2^-13 below the largest (its power of two) of the products of eight consecutive channels, and add the rest in fp32.
  *
  * adasum_linear_store puts the weight of a layer (outputs x width, row-major, at `offset` of the flat buffer `params`) into 8 bits, once
- * as it is and once transposed, with the same blocks: adasum_linear_bytes, 16-byte aligned.  Layout: outputs rows of
- * width rounded up to a whole block, width rows of outputs rounded up, zeros behind the last channel; then a byte e + 127 for each
- * block, [blocks of outputs][blocks of width].  outputs and width at most 2^24.
+ * as it is and once transposed, with the same blocks: adasum_linear_bytes, 16-byte aligned.  Layout: panels of 64
+ * inputs, [panels][outputs][64], with whole blocks of panels and zeros behind the last input; panels of 64 outputs in the same way,
+ * [panels][width][64]; then a byte e + 127 for each block, [blocks of outputs][blocks of width].  outputs and width at most 2^24.
  */
 #define ADASUM_LINEAR_BLOCK 128
 ADASUM_API int adasum_linear_bytes(int64_t outputs, int64_t width, size_t* bytes);

@@ -207,8 +207,8 @@ template <> int launch_join_grad<4>(const JoinCall&, const JoinGradRows&, const 
 
 constexpr int kBlock8 = ADASUM_LINEAR_BLOCK;
 inline int64_t blocks8(int64_t n) { return (n + kBlock8 - 1) / kBlock8; }
-// A weight: its rows, [outputs][blocks of width * 128] bytes, those of its transpose, [width][blocks of outputs * 128], and a byte for
-// each block, [blocks of outputs][blocks of width], e + 127.
+// A weight: its rows in panels of 64 channels, [blocks of width * 2][outputs][64] bytes, those of its transpose, [blocks of outputs * 2]
+// [width][64], and a byte for each block, [blocks of outputs][blocks of width], e + 127.
 struct Weight8 {
     unsigned char *q, *turned, *e;
     int64_t outputs, width;
@@ -230,7 +230,7 @@ int launch_weight8_store(const void* w, int dtype, const Weight8& to, void* stre
 
 // out [rows][outputs] = x [rows][depth] times the transpose of w [outputs][depth] in 8 bits, and a bias.
 struct Product8 {
-    const unsigned char *w, *e;          // rows of whole blocks; the exponent of block (output, depth) is e[output * e_output + depth * e_depth]
+    const unsigned char *w, *e;          // panels of 64 channels; the exponent of block (output, depth) is e[output * e_output + depth * e_depth]
     int64_t outputs, depth, e_output, e_depth;
     const void* x;
     int dtype;

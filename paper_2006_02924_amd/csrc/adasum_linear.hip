@@ -10,7 +10,15 @@ namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Where operands lie: in panels of 64 bytes of the depth, all rows of a panel one after the other, so that sixteen rows' pieces of a panel are
+// a kilobyte of memory in one.
+constexpr int kPanel = 64;
+__device__ __forceinline__ long long panel_place(long long rows, long long row, int byte) {
+    return (byte / kPanel * rows + row) * kPanel + byte % kPanel;
+}
 
 // ---- into 8 bits ----------------------------------------------------------------
 
@@ -53,15 +61,15 @@ __device__ __forceinline__ unsigned most_of_16(unsigned v) {
     v = max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x122, 0xf, 0xf, true)));
     return max(v, static_cast<unsigned>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x121, 0xf, 0xf, true)));
 }
-// Where a token's exponent lies among those of one block of channels: of each 64 tokens, those 16 apart are together, so that a lane of the
+// Where a token's exponent lies among those of one block of channels: of each 128 tokens, those 32 apart are together, so that a lane of the
 // matrix cores' operand has its four tokens' in a word.
-__device__ __forceinline__ long long exponent_place(long long t) { return (t & ~63ll) + (t & 15) * 4 + (t >> 4 & 3); }
+__device__ __forceinline__ long long exponent_place(long long t) { return (t & ~127ll) + (t & 31) * 4 + (t >> 5 & 3); }
 
 // Rows of activations into 8 bits (EXACT: into the values those stand for, in bf16), sixteen lanes a block of channels.
 template <typename X, RowForm FORM, bool EXACT, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
-rows8_kernel(const X* __restrict__ x, long long stride, int width, unsigned char* __restrict__ to, unsigned char* __restrict__ e, long long pitch,
-             long long tokens, RowWork work) {
+rows8_kernel(const X* __restrict__ x, long long stride, int width, unsigned char* __restrict__ to, unsigned char* __restrict__ e, long long tokens,
+             RowWork work) {
     constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
@@ -90,9 +98,9 @@ rows8_kernel(const X* __restrict__ x, long long stride, int width, unsigned char
                     q.x = in_8_bits(v, exponent);
                     q.y = in_8_bits(v + 4, exponent);
                     if constexpr (EXACT) {
-                        *reinterpret_cast<u32x4*>(to + (p.row * pitch + p.at) * 2) = in_bf16(q, exponent);
+                        *reinterpret_cast<u32x4*>(to + panel_place(work.rows, p.row, 2 * p.at)) = in_bf16(q, exponent);
                     } else {
-                        *reinterpret_cast<u32x2*>(to + p.row * pitch + p.at) = q;
+                        *reinterpret_cast<u32x2*>(to + panel_place(work.rows, p.row, p.at)) = q;
                         if ((g & 15) == 0) e[p.at / kBlock8 * tokens + exponent_place(p.row)] = static_cast<unsigned char>(exponent);
                     }
                 }
@@ -102,13 +110,14 @@ rows8_kernel(const X* __restrict__ x, long long stride, int width, unsigned char
 }
 // A weight's rows in 8 bits into the values they stand for.
 __global__ void __launch_bounds__(kThreadsRow)
-weight_values_kernel(const unsigned char* __restrict__ q, const unsigned char* __restrict__ e, long long e_output, long long e_depth, long long pitch,
+weight_values_kernel(const unsigned char* __restrict__ q, const unsigned char* __restrict__ e, long long e_output, long long e_depth,
                      unsigned char* __restrict__ to, RowWork work) {
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned g = threadIdx.x; g < n; g += kThreadsRow) {
             const Place p = place_of(work, first, g);
-            *reinterpret_cast<u32x4*>(to + (p.row * pitch + p.at) * 2) =
-                in_bf16(*reinterpret_cast<const u32x2*>(q + p.row * pitch + p.at), e[p.row / kBlock8 * e_output + p.at / kBlock8 * e_depth]);
+            *reinterpret_cast<u32x4*>(to + panel_place(work.rows, p.row, 2 * p.at)) =
+                in_bf16(*reinterpret_cast<const u32x2*>(q + panel_place(work.rows, p.row, p.at)),
+                        e[p.row / kBlock8 * e_output + p.at / kBlock8 * e_depth]);
         }
     });
 }
@@ -118,7 +127,6 @@ template <typename T>
 __global__ void __launch_bounds__(256) weight8_store_kernel(const T* __restrict__ from, Weight8 w, int blocks_i, long long blocks) {
     __shared__ unsigned most_of[4];
     __shared__ __align__(16) unsigned char turned[kBlock8][kBlock8 + 4];   // [input][output]
-    const long long pitch = static_cast<long long>(blocks_i) * kBlock8, pitch_turned = (w.outputs + kBlock8 - 1) / kBlock8 * kBlock8;
     const int r = threadIdx.x / 16, c = threadIdx.x % 16 * 8;
     for (long long block = blockIdx.x; block < blocks; block += gridDim.x) {
         const long long o0 = block / blocks_i * kBlock8, i0 = block % blocks_i * kBlock8;
@@ -147,7 +155,7 @@ __global__ void __launch_bounds__(256) weight8_store_kernel(const T* __restrict_
             q.x = in_8_bits(v[k], exponent);
             q.y = in_8_bits(v[k] + 4, exponent);
             const long long o = o0 + 16 * k + r;
-            if (o < w.outputs) *reinterpret_cast<u32x2*>(w.q + o * pitch + i0 + c) = q;
+            if (o < w.outputs) *reinterpret_cast<u32x2*>(w.q + panel_place(w.outputs, o, static_cast<int>(i0) + c)) = q;
 #pragma unroll
             for (int i = 0; i < 8; ++i) turned[c + i][16 * k + r] = static_cast<unsigned char>((i < 4 ? q.x : q.y) >> (8 * (i % 4)));
         }
@@ -159,7 +167,7 @@ __global__ void __launch_bounds__(256) weight8_store_kernel(const T* __restrict_
                 u32x2 q;
                 q.x = *reinterpret_cast<const unsigned*>(&turned[in][c]);
                 q.y = *reinterpret_cast<const unsigned*>(&turned[in][c + 4]);
-                *reinterpret_cast<u32x2*>(w.turned + (i0 + in) * pitch_turned + o0 + c) = q;
+                *reinterpret_cast<u32x2*>(w.turned + panel_place(w.width, i0 + in, static_cast<int>(o0) + c)) = q;
             }
         }
     }
@@ -179,17 +187,17 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(Product8 p, long long t
     __shared__ float meet[4][16][17];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, group = lane >> 4;
     const int blocks = static_cast<int>((p.depth + kBlock8 - 1) / kBlock8), depth = static_cast<int>(p.depth);
-    const long long pitch = static_cast<long long>(blocks) * kBlock8;
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const long long o0 = tile % tiles_o * 16, t0 = tile / tiles_o * 16;
-        const unsigned char* const w = p.w + min(o0 + row, static_cast<long long>(p.outputs) - 1) * pitch + 32 * group;
+        const unsigned char* const w =
+            p.w + ((group >> 1) * static_cast<long long>(p.outputs) + min(o0 + row, static_cast<long long>(p.outputs) - 1)) * kPanel + 32 * (group & 1);
         const X* const x = static_cast<const X*>(p.x) + min(t0 + row, static_cast<long long>(p.rows) - 1) * p.x_stride;
         const unsigned char* const e = p.e + o0 / kBlock8 * p.e_output;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int b = wave; b < blocks; b += 4) {
             i32x8 a, q;
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(w + static_cast<long long>(b) * kBlock8);
-            const u32x4 hi = *reinterpret_cast<const u32x4*>(w + static_cast<long long>(b) * kBlock8 + 16);
+            const unsigned char* const here = w + b * static_cast<long long>(p.outputs) * kBlock8;
+            const u32x4 lo = *reinterpret_cast<const u32x4*>(here), hi = *reinterpret_cast<const u32x4*>(here + 16);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 a[i] = static_cast<int>(lo[i]);
@@ -251,35 +259,53 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(Product8 p, long long t
     }
 }
 
-// TILE x TILE of the result: what a workgroup of four waves computes.  Both operands come in rows along the depth, 128 bytes a step (a block
-// of 8-bit numbers, 64 of 16 bits), and go to LDS past the registers.  A row's eight pieces of 16 bytes lie in LDS at their number
-// exclusive-or half the row's, so that sixteen rows' same piece lies in all banks.
-template <int TILE>
+// TILE x TILE of the result: what a workgroup of four waves computes at a time.  A step is a panel of both operands, 64 bytes of the depth (64
+// numbers of 8 bits, 32 of 16).  Panels go to LDS past the registers, into one of four places in turn.  A row's four pieces of 16 bytes lie
+// there at their number exclusive-or a quarter of the row's, so that sixteen rows' same piece lies in all banks.
+template <bool EXACT, int TILE>
 struct ProductShape {
-    static constexpr int threads = 256, frags = TILE / 32;                 // of 16 rows, a wave along each side
-    static constexpr int operand_bytes = TILE * kBlock8, buffer_bytes = 2 * operand_bytes, lds_bytes = 2 * buffer_bytes;
-    static constexpr int loads = operand_bytes / (threads * 16);           // of an operand, a lane
+    static constexpr int threads = 256, frags = TILE / 64;                 // of 32 rows, a wave along each side
+    static constexpr int panel_bytes = TILE * kPanel, step_bytes = 2 * panel_bytes, places = 4;
+    static constexpr int loads = panel_bytes / (threads * 16);             // of an operand, a wave
+    static constexpr int exponents = EXACT ? 0 : 256;                      // bytes of a block's exponents, a wave
+    // results pass through LDS, 32 tokens of a wave at a time
+    static constexpr int row_bytes = TILE == 256 || EXACT ? 128 : 64, result_bytes = 32 * row_bytes;
+    static constexpr int off_exponents = places * step_bytes, off_results = off_exponents + 4 * places * exponents;
+    static constexpr int lds_bytes = off_results + 4 * result_bytes;
 };
 
 struct Large {
-    const unsigned char *w, *x;           // rows `pitch` bytes apart
+    const unsigned char *w, *x;           // panels
     const unsigned char *e_w, *e_x;       // exponents (not EXACT): [output / 128 * e_output + block * e_depth], [block * tokens + place]
     long long outputs, rows, e_output, e_depth, tokens;
     const void* bias;
-    unsigned pitch;
-    int bias_dtype, steps;
+    int bias_dtype, steps;                // steps of a tile: an even number
     long long out_stride;
-    unsigned tiles_o, tiles_t;
+    unsigned tiles_o, tiles;
 };
 
-// Sixteen bytes a lane from base + offset to LDS, a wave's one after the other from `to` on.  (The builtin makes every later read of LDS wait
-// for it, of whatever place.  There is no register that the load writes; the loop below waits for it by itself.)
+// (Scalars that the vector unit writes may be read as addresses five instructions later, m0 one later: nobody but this file sees to that in
+// the assembly below.)
+// Sixteen (or four) bytes a lane from base + offset to LDS, a wave's one after the other from `to` on.  (The builtin makes every later read of
+// LDS wait for it, of whatever place.  There is no register that the load writes; the loop below waits for it by itself.)
 __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned offset, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
 }
-__device__ __forceinline__ void wait_for_all() {
+__device__ __forceinline__ void load_word_to_lds(const unsigned char* at, unsigned to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(at) : "memory");
+}
+// An address that all lanes have, in scalar registers.
+__device__ __forceinline__ const unsigned char* in_scalars(const unsigned char* p) {
+    const unsigned long long a = reinterpret_cast<unsigned long long>(p);
+    const unsigned lo = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(a)), hi = __builtin_amdgcn_readfirstlane(static_cast<unsigned>(a >> 32));
+    return reinterpret_cast<const unsigned char*>(static_cast<unsigned long long>(hi) << 32 | lo);
+}
+// Until at most LOADS of the wave's accesses to memory are under way, and none to LDS.
+template <int LOADS>
+__device__ __forceinline__ void wait_for_loads() {
+    static_assert(LOADS <= 63, "");
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt 0, lgkmcnt 0
+    __builtin_amdgcn_s_waitcnt(0x0070 | (LOADS & 15) | (LOADS >> 4) << 14);
     asm volatile("" ::: "memory");
 }
 
@@ -292,72 +318,73 @@ __device__ __forceinline__ void every(F&& f) {
     }
 }
 
+#define ADASUM_INLINE __attribute__((always_inline))
+// Loads run three steps ahead of the products.  A step's operands are in registers when it begins; beside its products the next step's are
+// read, into the registers of those that have been used for the last time.
 template <bool EXACT, int TILE, typename O>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large p, O* __restrict__ out) {
-    typedef ProductShape<TILE> S;
-    constexpr int F = S::frags;
+    typedef ProductShape<EXACT, TILE> S;
+    constexpr int F = S::frags, L = S::loads;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wo = wave % 2 * (32 * F), wt = wave / 2 * (32 * F);
+    const unsigned lds_base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(lds)));
+
     const unsigned n = die_order(blockIdx.x, gridDim.x);
     const long long o0 = static_cast<long long>(n % p.tiles_o) * TILE, t0 = static_cast<long long>(n / p.tiles_o) * TILE;
-    const int wo = wave % 2 * (16 * F), wt = wave / 2 * (16 * F);
 
-    // what a lane loads: a piece of each 32nd row
-    const unsigned char *w_base = p.w + o0 * p.pitch, *x_base = p.x + t0 * p.pitch;
+    // ---- loads: a lane's piece of each 64th row
+    int load_place = 0;
+    const unsigned char *w_base = in_scalars(p.w + o0 * kPanel), *x_base = in_scalars(p.x + t0 * kPanel);
     const int w_last = static_cast<int>(min(p.outputs - o0, static_cast<long long>(TILE))) - 1;
     const int x_last = static_cast<int>(min(p.rows - t0, static_cast<long long>(TILE))) - 1;
-    unsigned w_at[S::loads], x_at[S::loads];
+    unsigned w_at[L], x_at[L];
 #pragma unroll
-    for (int k = 0; k < S::loads; ++k) {
-        const int row = k * 32 + wave * 8 + (lane >> 3), piece = (lane & 7) ^ (row >> 1 & 7);
-        w_at[k] = min(row, w_last) * p.pitch + 16 * piece;
-        x_at[k] = min(row, x_last) * p.pitch + 16 * piece;
+    for (int k = 0; k < L; ++k) {
+        const int row = (k * 4 + wave) * 16 + (lane >> 2), piece = (lane & 3) ^ (lane >> 4);
+        w_at[k] = min(row, w_last) * kPanel + 16 * piece;
+        x_at[k] = min(row, x_last) * kPanel + 16 * piece;
     }
-    const unsigned char* e_w = EXACT ? nullptr : p.e_w + min(o0 + wo, p.outputs - 1) / kBlock8 * p.e_output;
-    const unsigned char* e_x = EXACT ? nullptr : p.e_x + t0 + wt + (lane & 15) * 4;
-    // exponents of this step, of the next, and those that are being loaded; of the tokens, a word for each 64
-    constexpr int WORDS = F / 4;
-    unsigned of_w = 0, next_w = 0, coming_w = 0, of_x[WORDS] = {}, next_x[WORDS] = {}, coming_x[WORDS] = {};
-    const unsigned to = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(lds))) + wave * 1024;
-    auto load = [&](int buffer) {
-        if constexpr (!EXACT) {
-            coming_w = *e_w;
+    // (of the exponents, the first half of the lanes load the tokens', the others the word that has the weight's)
+    const unsigned char* const of_x0 = EXACT ? nullptr : p.e_x + t0 + (wt & ~127) + 4 * (lane & 31);
+    const unsigned char* const of_w0 = EXACT ? nullptr : p.e_w + min(o0 + wo, p.outputs - 1) / kBlock8 * p.e_output;
+    const unsigned char* e_at = lane < 32 ? of_x0 : of_w0;
+    const long long of_tokens = p.tokens, of_weight = p.e_depth, e_next = lane < 32 ? of_tokens : of_weight;
+    // a panel, the first of a block of the depth or its second
+    auto load = [&](auto odd) ADASUM_INLINE {
+        if constexpr (!EXACT && !decltype(odd)::value) {
+            load_word_to_lds(reinterpret_cast<const unsigned char*>(reinterpret_cast<uintptr_t>(e_at) & ~static_cast<uintptr_t>(3)),
+                             lds_base + S::off_exponents + (wave * S::places + (load_place >> 1 & 3)) * S::exponents);
+            e_at += e_next;
+        }
+        const unsigned to = lds_base + (load_place & 3) * S::step_bytes + wave * 1024;
 #pragma unroll
-            for (int k = 0; k < WORDS; ++k) coming_x[k] = *reinterpret_cast<const unsigned*>(e_x + 64 * k);
+        for (int k = 0; k < L; ++k) {
+            load_to_lds(w_base, w_at[k], to + k * 4096);
+            load_to_lds(x_base, x_at[k], to + S::panel_bytes + k * 4096);
         }
-#pragma unroll
-        for (int k = 0; k < S::loads; ++k) {
-            load_to_lds(w_base, w_at[k], to + buffer * S::buffer_bytes + k * 4096);
-            load_to_lds(x_base, x_at[k], to + buffer * S::buffer_bytes + S::operand_bytes + k * 4096);
-        }
+        ++load_place;
+        w_base += p.outputs * kPanel;
+        x_base += p.rows * kPanel;
     };
-    // (behind the last step it is loaded again, and not used)
-    int ahead = 0;
-    auto next = [&] {
-        if (ahead + 1 < p.steps) {
-            ++ahead;
-            w_base += kBlock8;
-            x_base += kBlock8;
-            if constexpr (!EXACT) {
-                e_w += p.e_depth;
-                e_x += p.tokens;
-            }
-        }
-    };
-    // what it reads: of a row, pieces g and g + 4 for its group g of lanes
-    const int row = lane & 15, group = lane >> 4, first = 16 * (group ^ (row >> 1)), second = 16 * ((group + 4) ^ (row >> 1));
-    const char* const w_read = lds + (wo + row) * kBlock8;
-    const char* const x_read = lds + S::operand_bytes + (wt + row) * kBlock8;
+
+    // ---- products
+    const int row = lane & 31, group = lane >> 5, turn = row >> 2 & 3;
+    const char* const w_read = lds + (wo + row) * kPanel;
+    const char* const x_read = lds + S::panel_bytes + (wt + row) * kPanel;
+    const int piece[2] = {16 * (group ^ turn), 16 * ((group + 2) ^ turn)};
     u32x4 fw[F][2], fx[F][2];
-    auto read_w = [&](int i, int from) {
-        fw[i][0] = *reinterpret_cast<const u32x4*>(w_read + from + i * 16 * kBlock8 + first);
-        fw[i][1] = *reinterpret_cast<const u32x4*>(w_read + from + i * 16 * kBlock8 + second);
+    auto read_w = [&](int i, int from) ADASUM_INLINE {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fw[i][h] = *reinterpret_cast<const u32x4*>(w_read + from + i * 32 * kPanel + piece[h]);
     };
-    auto read_x = [&](int j, int from) {
-        fx[j][0] = *reinterpret_cast<const u32x4*>(x_read + from + j * 16 * kBlock8 + first);
-        fx[j][1] = *reinterpret_cast<const u32x4*>(x_read + from + j * 16 * kBlock8 + second);
+    auto read_x = [&](int j, int from) ADASUM_INLINE {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) fx[j][h] = *reinterpret_cast<const u32x4*>(x_read + from + j * 32 * kPanel + piece[h]);
     };
-    auto whole = [](const u32x4 (&f)[2]) {
+    // the exponents of this block of the depth, and of the next
+    unsigned of_w = 0, of_x = 0, next_w = 0, next_x = 0;
+    auto whole = [](const u32x4 (&f)[2]) ADASUM_INLINE {
         i32x8 r;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -366,132 +393,170 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
         }
         return r;
     };
-    f32x4 acc[F][F] = {};
-    auto multiply = [&](int i, auto number) {
+    f32x16 acc[F][F] = {};
+    auto multiply = [&](int i, auto number) ADASUM_INLINE {
         constexpr int j = decltype(number)::value;
+        f32x16 sum = acc[i][j];
         if constexpr (EXACT) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[i][h]), __builtin_bit_cast(bf16x8, fx[j][h]), acc[i][j],
-                                                                    0, 0, 0);
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[i][h]), __builtin_bit_cast(bf16x8, fx[j][h]), sum, 0, 0, 0);
         } else {
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(whole(fw[i]), whole(fx[j]), acc[i][j], 0, 0, 0, static_cast<int>(of_w), j % 4,
-                                                                         static_cast<int>(of_x[j / 4]));
+            sum = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(whole(fw[i]), whole(fx[j]), sum, 0, 0, 0, static_cast<int>(of_w), j,
+                                                                  static_cast<int>(of_x));
+        }
+        acc[i][j] = sum;
+    };
+    int place = 0;                        // of the panels that are multiplied; a tile begins with an even one
+    // where the weight's exponent lies in its word
+    unsigned e_shift = static_cast<unsigned>(reinterpret_cast<uintptr_t>(of_w0) & 3) * 8;
+    const unsigned e_shift_next = static_cast<unsigned>(p.e_depth & 3) * 8;
+    auto read_exponents = [&](int block) ADASUM_INLINE {
+        if constexpr (!EXACT) {
+            const char* const at = lds + S::off_exponents + (wave * S::places + (block & 3)) * S::exponents;
+            // (of a wave with 64 of the 128 tokens, the upper or lower two bytes)
+            next_x = *reinterpret_cast<const unsigned*>(at + 4 * row) >> (8 * ((wt & 127) / 32));
+            next_w = *reinterpret_cast<const unsigned*>(at + 128) >> e_shift;
+            e_shift = (e_shift + e_shift_next) & 31;
         }
     };
-    auto came = [&] {
-        next_w = coming_w;
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) next_x[k] = coming_x[k];
-    };
-    auto turn = [&] {
-        of_w = next_w;
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) of_x[k] = next_x[k];
-    };
-    load(0);
-    wait_for_all();
-    came();
-    turn();
-    next();
-    load(1);
-    __builtin_amdgcn_s_barrier();
-#pragma unroll
-    for (int i = 0; i < F; ++i) {
-        read_x(i, 0);
-        read_w(i, 0);
-    }
-    // A step's products come out of registers.  Beside them the next step's operands are read, into the registers of those that have been
-    // used for the last time, and the loads of the step after are issued, into the buffer that this step's operands were in.
-    for (int s = 0; s < p.steps; ++s) {
-        const int other = ~s & 1, from = other * S::buffer_bytes;
+    constexpr int kAhead = 2 * L + (EXACT ? 0 : 1);                                     // loads of two steps
+    // One step.  What is waited for is the next step's panel; those of two more steps came after it and may be under way.
+    auto step = [&](auto odd, auto more) ADASUM_INLINE {
         every<F>([&](auto j) { multiply(0, j); });
         __builtin_amdgcn_sched_barrier(0);
-        wait_for_all();
+        wait_for_loads<decltype(more)::value ? kAhead : 0>();
         __builtin_amdgcn_s_barrier();
-        came();
-        next();
-        load(other ^ 1);
+        if constexpr (decltype(more)::value) load(odd);
+        ++place;
+        const int from = (place & 3) * S::step_bytes;
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (decltype(odd)::value) read_exponents(place >> 1);
 #pragma unroll
         for (int i = 1; i < F - 2; ++i) {
             read_w(i - 1, from);
             every<F>([&](auto j) { multiply(i, j); });
             __builtin_amdgcn_sched_barrier(0);
         }
-        read_w(F - 3, from);
+        constexpr int kLeft = F > 2 ? F - 2 : 1;   // the rows that are left, column by column
+        read_w(kLeft - 1, from);
         every<F>([&](auto j) {
-            multiply(F - 2, j);
-            multiply(F - 1, j);
+#pragma unroll
+            for (int i = kLeft; i < F; ++i) multiply(i, j);
             __builtin_amdgcn_sched_barrier(0);
             read_x(j, from);
         });
-        read_w(F - 2, from);
-        read_w(F - 1, from);
+#pragma unroll
+        for (int i = kLeft; i < F; ++i) read_w(i, from);
         __builtin_amdgcn_sched_barrier(0);
-        turn();
-    }
-    // A lane has four consecutive outputs of a token in each 16 x 16.  Through LDS, some tokens of a wave at a time, sixteen lanes get a token's
-    // consecutive outputs to store.
-    wait_for_all();
-    __builtin_amdgcn_s_barrier();
-    constexpr int kOutputs = 16 * F, kRow = kOutputs * static_cast<int>(sizeof(O)) + 16;     // bytes of a token's row
-    constexpr int kOfLane = 16 / static_cast<int>(sizeof(O)), kLanes = kOutputs / kOfLane;   // outputs that a lane stores, lanes of a token
-    char* const mine = lds + wave * (S::lds_bytes / 4);
-    constexpr int kTogether = S::lds_bytes / 4 / (16 * kRow) < F ? S::lds_bytes / 4 / (16 * kRow) : F;   // of the token's sixteens
-    static_assert(kTogether >= 1, "");
-    float bias[F][4] = {};
-    if (p.bias != nullptr) {
-#pragma unroll
-        for (int i = 0; i < F; ++i) {
-            const long long o = o0 + wo + 16 * i + 4 * group;
-            const int there = static_cast<int>(min(p.outputs - o, 4ll));
-            if (there <= 0) continue;
-            if (p.bias_dtype == ADASUM_F32) load_some<4>(bias[i], static_cast<const float*>(p.bias) + o, there);
-            else if (p.bias_dtype == ADASUM_BF16) load_some<4>(bias[i], static_cast<const bf16_t*>(p.bias) + o, there);
-            else load_some<4>(bias[i], static_cast<const f16_t*>(p.bias) + o, there);
+        if constexpr (decltype(odd)::value) {
+            of_w = next_w;
+            of_x = next_x;
         }
-    }
+    };
+
+    // ---- results: a lane has four times four consecutive outputs of a token in each 32 x 32; through LDS consecutive lanes get a token's
+    // consecutive outputs to store
+    char* const mine = lds + S::off_results + wave * S::result_bytes;
+    constexpr int kPieces = S::row_bytes / 16, kFrags = S::row_bytes / (32 * static_cast<int>(sizeof(O)));   // of 32 outputs, at a time
+    static_assert(kFrags >= 1, "");
+    auto piece_at = [&](int token, int n) {
+        return mine + token * S::row_bytes + 16 * (n ^ (kPieces == 8 ? token >> 1 & 7 : token >> 2 & 3));
+    };
+    auto store = [&](bool all) ADASUM_INLINE {
 #pragma unroll
-    for (int j0 = 0; j0 < F; j0 += kTogether) {
+        for (int i0 = 0; i0 < F; i0 += kFrags) {
+            float bias[kFrags][4][4] = {};
+            if (p.bias != nullptr) {
 #pragma unroll
-        for (int j = j0; j < F && j < j0 + kTogether; ++j)
+                for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-            for (int i = 0; i < F; ++i) {
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = acc[i][j][k] + bias[i][k];
-                store_any<4>(reinterpret_cast<O*>(mine + (16 * (j - j0) + row) * kRow) + 16 * i + 4 * group, v);
-            }
-        __builtin_amdgcn_wave_barrier();
-        const int tokens = 16 * (F - j0 < kTogether ? F - j0 : kTogether);
-#pragma unroll 4
-        for (int k = lane; k < tokens * kLanes; k += 64) {
-            const int token = k / kLanes, at = k % kLanes * kOfLane;
-            const long long t = t0 + wt + 16 * j0 + token, o = o0 + wo + at;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(mine + token * kRow + at * static_cast<int>(sizeof(O)));
-            if (t >= p.rows || o >= p.outputs) continue;
-            O* const to_out = out + t * p.out_stride + o;
-            const int there = static_cast<int>(min(p.outputs - o, static_cast<long long>(kOfLane)));
-            if (there == kOfLane) {
-                store_at<false>(w, reinterpret_cast<u32x4_any*>(to_out));
-            } else {
-                unsigned words[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int e = 0; e < kOfLane; ++e)
-                    if (e < there) {
-                        if constexpr (sizeof(O) == 4) to_out[e] = __uint_as_float(words[e]);
-                        else to_out[e].v = static_cast<unsigned short>(words[e / 2] >> (16 * (e & 1)));
+                    for (int q = 0; q < 4; ++q) {
+                        const long long o = o0 + wo + 32 * (i0 + i) + 8 * q + 4 * group;
+                        const int there = static_cast<int>(min(p.outputs - o, 4ll));
+                        if (there <= 0) continue;
+                        if (p.bias_dtype == ADASUM_F32) load_some<4>(bias[i][q], static_cast<const float*>(p.bias) + o, there);
+                        else if (p.bias_dtype == ADASUM_BF16) load_some<4>(bias[i][q], static_cast<const bf16_t*>(p.bias) + o, there);
+                        else load_some<4>(bias[i][q], static_cast<const f16_t*>(p.bias) + o, there);
                     }
             }
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+#pragma unroll
+                for (int i = 0; i < kFrags; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float v[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[k] = acc[i0 + i][j][4 * q + k] + bias[i][q][k];
+                        if constexpr (sizeof(O) == 4) store_any<4>(reinterpret_cast<O*>(piece_at(row, 2 * q + group)), v);
+                        else store_any<4>(reinterpret_cast<O*>(piece_at(row, 4 * i + q) + 8 * group), v);
+                    }
+                asm volatile("" ::: "memory");   // (a wave's own accesses to LDS keep their order)
+                constexpr int kOfLane = 16 / static_cast<int>(sizeof(O));
+#pragma unroll
+                for (int k = 0; k < kPieces / 2; ++k) {
+                    const int token = k * (64 / kPieces) + lane / kPieces, n = lane % kPieces;
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(piece_at(token, n));
+                    const long long t = t0 + wt + 32 * j + token, o = o0 + wo + 32 * i0 + n * kOfLane;
+                    O* const to = out + t * p.out_stride + o;
+                    if (all) {
+                        store_at<false>(v, reinterpret_cast<u32x4_any*>(to));
+                    } else if (t < p.rows && o < p.outputs) {
+                        if (p.outputs - o >= kOfLane) {
+                            store_at<false>(v, reinterpret_cast<u32x4_any*>(to));
+                        } else {
+                            const unsigned words[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int e = 0; e < kOfLane; ++e)
+                                if (o + e < p.outputs) {
+                                    if constexpr (sizeof(O) == 4) to[e] = __uint_as_float(words[e]);
+                                    else to[e].v = static_cast<unsigned short>(words[e / 2] >> (16 * (e & 1)));
+                                }
+                        }
+                    }
+                }
+                asm volatile("" ::: "memory");
+            }
         }
-        __builtin_amdgcn_wave_barrier();
+    };
+
+    const std::true_type yes;
+    const std::false_type no;
+    // (there are at least four steps)
+    asm volatile("s_nop 4");
+    load(no);
+    load(yes);
+    load(no);
+    load(yes);
+    wait_for_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    read_exponents(0);
+    of_w = next_w;
+    of_x = next_x;
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        read_x(i, 0);
+        read_w(i, 0);
     }
+    for (int s = 4; s < p.steps; s += 2) {
+        step(no, yes);
+        step(yes, yes);
+    }
+    // (the last four find all their panels loaded)
+    for (int s = 0; s < 4; s += 2) {
+        step(no, no);
+        step(yes, no);
+    }
+    if (o0 + TILE <= p.outputs && t0 + TILE <= p.rows) store(true);
+    else store(false);
 }
 
 // The kernel of few tokens does the large ones' work where there are none to fill a tile.
-// (A tile's rows are addressed with 32 bits.)
-bool is_large(int64_t rows, int64_t outputs, int64_t depth) { return rows > 64 && depth > 0 && depth <= (1 << 22) && outputs >= 16; }
+bool is_large(int64_t rows, int64_t outputs, int64_t depth) { return rows > 64 && depth > 0 && outputs >= 16; }
+// Whether operands are multiplied as the bf16 numbers that they stand for: for fp32 results, and where a tile would have two steps only (the
+// kernel's loads are three ahead).
+bool is_exact(int64_t depth, int out_dtype) { return out_dtype == ADASUM_F32 || depth <= kBlock8; }
 constexpr int64_t kTokenPad = 256;
 struct Workspace8 {
     size_t off_more = 0, total = 0;    // the exponents, or the weight's values
@@ -500,7 +565,7 @@ Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtyp
     Workspace8 w;
     if (!is_large(rows, outputs, depth)) return w;
     const size_t pitch = static_cast<size_t>(blocks8(depth)) * kBlock8;
-    const bool exact = out_dtype == ADASUM_F32;
+    const bool exact = is_exact(depth, out_dtype);
     w.off_more = static_cast<size_t>(rows) * pitch * (exact ? 2 : 1);
     w.total = w.off_more + (exact ? static_cast<size_t>(outputs) * pitch * 2
                                   : static_cast<size_t>(blocks8(depth)) * align_up(static_cast<size_t>(rows), kTokenPad));
@@ -509,11 +574,11 @@ Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtyp
 
 template <bool EXACT, int TILE, typename O>
 int launch_large(const Product8& p, const Large& l, void* stream) {
-    typedef ProductShape<TILE> S;
+    typedef ProductShape<EXACT, TILE> S;
     const auto kernel = product_kernel<EXACT, TILE, O>;
     const int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds_bytes));
     if (rc != 0) return rc;
-    return launch(kernel, static_cast<int64_t>(l.tiles_o) * l.tiles_t, 1, S::threads, S::lds_bytes, stream, l, static_cast<O*>(p.out));
+    return launch(kernel, l.tiles, 1, S::threads, S::lds_bytes, stream, l, static_cast<O*>(p.out));
 }
 
 constexpr int64_t kMany8 = 1 << 19;
@@ -532,14 +597,14 @@ int large_product(const Product8& p, void* stream) {
             constexpr RowForm F = decltype(form)::value;
             return with_items<X>(g, [&](auto items) -> int {
                 return launch(rows8_kernel<X, F, EXACT, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const X*>(p.x),
-                              p.x_stride, p.depth, x, EXACT ? nullptr : more, pitch, tokens, g.work);
+                              p.x_stride, p.depth, x, EXACT ? nullptr : more, tokens, g.work);
             });
         });
     });
     if (rc != 0) return rc;
     if (EXACT) {
         const RowGrid g = row_grid(p.outputs, pitch, ADASUM_F32, 0);
-        rc = launch(weight_values_kernel, g.groups, 1, kThreadsRow, 0, stream, p.w, p.e, p.e_output, p.e_depth, pitch, more, g.work);
+        rc = launch(weight_values_kernel, g.groups, 1, kThreadsRow, 0, stream, p.w, p.e, p.e_output, p.e_depth, more, g.work);
         if (rc != 0) return rc;
     }
     Large l{};
@@ -547,7 +612,6 @@ int large_product(const Product8& p, void* stream) {
     l.x = x;
     l.e_w = p.e;
     l.e_x = EXACT ? nullptr : more;
-    l.pitch = pitch * (EXACT ? 2 : 1);
     l.outputs = p.outputs;
     l.rows = p.rows;
     l.e_output = p.e_output;
@@ -555,12 +619,12 @@ int large_product(const Product8& p, void* stream) {
     l.tokens = tokens;
     l.bias = p.bias;
     l.bias_dtype = p.bias_dtype;
-    l.steps = static_cast<int>(l.pitch / kBlock8);
+    l.steps = static_cast<int>(pitch * (EXACT ? 2 : 1) / kPanel);
     l.out_stride = p.out_stride;
-    auto tiles = [&](int64_t n, int tile) { return static_cast<unsigned>((n + tile - 1) / tile); };
-    const bool wide = static_cast<int64_t>(tiles(p.outputs, 256)) * tiles(p.rows, 256) >= 192;
-    l.tiles_o = tiles(p.outputs, wide ? 256 : 128);
-    l.tiles_t = tiles(p.rows, wide ? 256 : 128);
+    auto tiles = [&](int64_t n, int tile) { return (n + tile - 1) / tile; };
+    const bool wide = tiles(p.outputs, 256) * tiles(p.rows, 256) >= 192;
+    l.tiles_o = static_cast<unsigned>(tiles(p.outputs, wide ? 256 : 128));
+    l.tiles = static_cast<unsigned>(l.tiles_o * tiles(p.rows, wide ? 256 : 128));
     return wide ? launch_large<EXACT, 256, O>(p, l, stream) : launch_large<EXACT, 128, O>(p, l, stream);
 }
 
@@ -578,10 +642,11 @@ size_t product8_workspace(int64_t rows, int64_t outputs, int64_t depth, int out_
 
 int launch_product8(const Product8& p, void* stream) {
     if (is_large(p.rows, p.outputs, p.depth)) {
+        const bool exact = is_exact(p.depth, p.out_dtype);
         switch (p.out_dtype) {
             case ADASUM_F32: return large_product<true, float>(p, stream);
-            case ADASUM_BF16: return large_product<false, bf16_t>(p, stream);
-            default: return large_product<false, f16_t>(p, stream);
+            case ADASUM_BF16: return exact ? large_product<true, bf16_t>(p, stream) : large_product<false, bf16_t>(p, stream);
+            default: return exact ? large_product<true, f16_t>(p, stream) : large_product<false, f16_t>(p, stream);
         }
     }
     return with_type(p.dtype, [&](auto x) -> int {

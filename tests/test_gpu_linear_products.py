@@ -22,7 +22,8 @@ def parts(weight):
     data = weight.data.cpu()
     a, b = o * wb * 128, w * ob * 128
     number = lambda t: t.view(torch.float8_e4m3fn).double().numpy()
-    return (number(data[:a]).reshape(o, wb * 128), number(data[a:a + b]).reshape(w, ob * 128),
+    panels = lambda t, rows: t.reshape(-1, rows, 64).transpose(1, 0, 2).reshape(rows, -1)
+    return (panels(number(data[:a]), o), panels(number(data[a:a + b]), w),
             data[a + b:a + b + ob * wb].numpy().astype(np.int64).reshape(ob, wb) - 127)
 
 
@@ -120,6 +121,29 @@ def test_numbers_that_8_bits_hold_are_multiplied_exactly():
         weight = B.adasum_linear_store(w.reshape(-1).cuda(), 0, outputs, width)
         assert torch.equal(B.adasum_linear(weight, x.cuda()).cpu().double(), x.double() @ w.double().t())
         assert torch.equal(B.adasum_linear_grad(weight, dy.cuda()).cpu().double(), dy.double() @ w.double())
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n, width, outputs", [(12345, 100, 1100), (16640, 128, 1024), (9000, 384, 2050), (33000, 250, 520), (2300, 130, 515), (4100, 1000, 640),
+                                              (70000, 64, 256), (257, 64, 60000)])
+def test_many_tiles(n, width, outputs, out):
+    """More tiles than workgroups, whole ones and others, few and many steps: whole numbers whose sums all types hold."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    small = lambda *shape: torch.randint(-1, 2, shape, generator=g, device="cuda").float() * (torch.rand(*shape, generator=g, device="cuda") < 0.4)
+    w, bias = small(outputs, width), small(outputs)
+    flat = torch.cat([w.reshape(-1), bias])
+    weight = B.adasum_linear_store(flat, 0, outputs, width)
+    for rep in range(2):
+        x = small(n, width).bfloat16()
+        want = x.float() @ w.t() + bias
+        assert want.abs().max() <= 256
+        assert torch.equal(B.adasum_linear(weight, x, params=flat, bias_offset=outputs * width, out_dtype=out).float(), want)
+        dy = small(n, outputs).bfloat16()
+        want = dy.float() @ w
+        if out == torch.float32 or want.abs().max() <= 256:
+            assert torch.equal(B.adasum_linear_grad(weight, dy, out_dtype=out).float(), want)
+        else:
+            assert torch.equal(B.adasum_linear_grad(weight, dy, out_dtype=out), want.to(out))
 
 
 @pytest.mark.parametrize("n", [20, 600])
