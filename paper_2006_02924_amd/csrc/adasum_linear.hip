@@ -180,43 +180,71 @@ __global__ void __launch_bounds__(256) weight8_store_kernel(const T* __restrict_
 // operands come out off by 1.5e-5 of the result's size.  16-bit results are rounded by far more (2^-9 and 2^-12).  fp32 results are
 // therefore computed from the same operands as bf16 numbers, which hold what they stand for: exact products, sums in fp32, half the rate.
 
-// 16 outputs x 16 tokens of a workgroup.  Its four waves share the depth, block by block: a wave reads 128 channels of 16 rows of the weight as
+// 16 OUTPUTS outputs x 16 tokens of a workgroup.  Its waves share the depth, block by block: a wave reads 128 channels of the weight's rows as
 // they are, puts those of the tokens into 8 bits where the matrix cores want them, and multiplies.
-template <typename X, typename O, RowForm FORM>
-__global__ void __launch_bounds__(256) few_tokens_kernel(Product8 p, long long tiles_o, long long tiles) {
-    __shared__ float meet[4][16][17];
+template <typename X, typename O, RowForm FORM, int WAVES, int OUTPUTS>
+__global__ void __launch_bounds__(64 * WAVES) few_tokens_kernel(Product8 p, long long tiles_o, long long tiles) {
+    constexpr int kOutputs = 16 * OUTPUTS;
+    __shared__ float meet[WAVES][16][kOutputs + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, group = lane >> 4;
     const int blocks = static_cast<int>((p.depth + kBlock8 - 1) / kBlock8), depth = static_cast<int>(p.depth);
     for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const long long o0 = tile % tiles_o * 16, t0 = tile / tiles_o * 16;
-        const unsigned char* const w =
-            p.w + ((group >> 1) * static_cast<long long>(p.outputs) + min(o0 + row, static_cast<long long>(p.outputs) - 1)) * kPanel + 32 * (group & 1);
+        const long long o0 = tile % tiles_o * kOutputs, t0 = tile / tiles_o * 16;
+        const unsigned char* w[OUTPUTS];
+#pragma unroll
+        for (int i = 0; i < OUTPUTS; ++i)
+            w[i] = p.w + ((group >> 1) * static_cast<long long>(p.outputs) + min(o0 + 16 * i + row, static_cast<long long>(p.outputs) - 1)) * kPanel +
+                   32 * (group & 1);
         const X* const x = static_cast<const X*>(p.x) + min(t0 + row, static_cast<long long>(p.rows) - 1) * p.x_stride;
         const unsigned char* const e = p.e + o0 / kBlock8 * p.e_output;
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int b = wave; b < blocks; b += 4) {
-            i32x8 a, q;
-            const unsigned char* const here = w + b * static_cast<long long>(p.outputs) * kBlock8;
-            const u32x4 lo = *reinterpret_cast<const u32x4*>(here), hi = *reinterpret_cast<const u32x4*>(here + 16);
+        f32x4 acc[OUTPUTS] = {};
+        // (a block's loads are issued before the products of the one before it)
+        u32x4 lo[OUTPUTS], hi[OUTPUTS];
+        Granule<X, 8> raw[4];
+        unsigned weight_exponent = 0;
+        auto load = [&](int b) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = static_cast<int>(lo[i]);
-                a[4 + i] = static_cast<int>(hi[i]);
+            for (int i = 0; i < OUTPUTS; ++i) {
+                const unsigned char* const here = w[i] + b * static_cast<long long>(p.outputs) * kBlock8;
+                lo[i] = *reinterpret_cast<const u32x4*>(here);
+                hi[i] = *reinterpret_cast<const u32x4*>(here + 16);
             }
-            Granule<X, 8> raw[4];
+            weight_exponent = e[b * p.e_depth];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = b * kBlock8 + 32 * group + 8 * k;
+                if constexpr (FORM == kRagged) load_any(raw[k], x + min(at, depth - 8));
+                else load_row<FORM>(raw[k], x, at, depth);
+            }
+        };
+        if (wave < blocks) load(wave);
+        for (int b = wave; b < blocks; b += WAVES) {
+            i32x8 a[OUTPUTS], q;
+#pragma unroll
+            for (int n = 0; n < OUTPUTS; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    a[n][i] = static_cast<int>(lo[n][i]);
+                    a[n][4 + i] = static_cast<int>(hi[n][i]);
+                }
+            const unsigned of_weight = weight_exponent;
             float v[4][8];
             unsigned most = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) load_row<FORM>(raw[k], x, b * kBlock8 + 32 * group + 8 * k, depth);
-#pragma unroll
             for (int k = 0; k < 4; ++k) {
+                const int at = b * kBlock8 + 32 * group + 8 * k;
+                if constexpr (FORM == kRagged) {
+                    // (the row's last eight channels, moved down)
+                    if (b == blocks - 1) move_down(raw[k], at - min(at, depth - 8));
+                }
                 unpack(raw[k], v[k]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (b * kBlock8 + 32 * group + 8 * k + (FORM == kWhole ? 0 : i) >= depth) v[k][i] = 0.f;
+                    if (at + (FORM == kWhole ? 0 : i) >= depth) v[k][i] = 0.f;
                     most = max(most, finite_size(v[k][i]));
                 }
             }
+            if (b + WAVES < blocks) load(b + WAVES);
             most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 16, 64)));
             most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), 32, 64)));
             const unsigned exponent = exponent_of(most);
@@ -225,30 +253,37 @@ __global__ void __launch_bounds__(256) few_tokens_kernel(Product8 p, long long t
                 q[2 * k] = static_cast<int>(in_8_bits(v[k], exponent));
                 q[2 * k + 1] = static_cast<int>(in_8_bits(v[k] + 4, exponent));
             }
-            const unsigned of_weight = e[b * p.e_depth];
             if constexpr (sizeof(O) == 4) {
                 // (the same eight channels of both, whichever they are)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    u32x2 l, m;
-                    l.x = static_cast<unsigned>(a[2 * k]);
-                    l.y = static_cast<unsigned>(a[2 * k + 1]);
-                    m.x = static_cast<unsigned>(q[2 * k]);
-                    m.y = static_cast<unsigned>(q[2 * k + 1]);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, in_bf16(l, of_weight)),
-                                                                  __builtin_bit_cast(bf16x8, in_bf16(m, exponent)), acc, 0, 0, 0);
+                    const u32x2 m = {static_cast<unsigned>(q[2 * k]), static_cast<unsigned>(q[2 * k + 1])};
+                    const bf16x8 token = __builtin_bit_cast(bf16x8, in_bf16(m, exponent));
+#pragma unroll
+                    for (int n = 0; n < OUTPUTS; ++n) {
+                        const u32x2 l = {static_cast<unsigned>(a[n][2 * k]), static_cast<unsigned>(a[n][2 * k + 1])};
+                        acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, in_bf16(l, of_weight)), token, acc[n], 0, 0, 0);
+                    }
                 }
             } else {
-                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, acc, 0, 0, 0, static_cast<int>(of_weight), 0, static_cast<int>(exponent));
+#pragma unroll
+                for (int n = 0; n < OUTPUTS; ++n)
+                    acc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a[n], q, acc[n], 0, 0, 0, static_cast<int>(of_weight), 0,
+                                                                              static_cast<int>(exponent));
             }
         }
         __syncthreads();   // (the last tile's sums have been read)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) meet[wave][row][4 * group + i] = acc[i];
+        for (int n = 0; n < OUTPUTS; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) meet[wave][row][16 * n + 4 * group + i] = acc[n][i];
         __syncthreads();
-        const int t = threadIdx.x / 16, o = threadIdx.x % 16;
-        if (t0 + t < p.rows && o0 + o < p.outputs) {
-            float sum = (meet[0][t][o] + meet[1][t][o]) + (meet[2][t][o] + meet[3][t][o]);
+        for (int at = threadIdx.x; at < 16 * kOutputs; at += 64 * WAVES) {
+            const int t = at / kOutputs, o = at % kOutputs;
+            if (t0 + t >= p.rows || o0 + o >= p.outputs) continue;
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < WAVES; k += 4) sum += (meet[k][t][o] + meet[k + 1][t][o]) + (meet[k + 2][t][o] + meet[k + 3][t][o]);
             if (p.bias != nullptr) {
                 if (p.bias_dtype == ADASUM_F32) sum += load_elem(static_cast<const float*>(p.bias) + o0 + o);
                 else if (p.bias_dtype == ADASUM_BF16) sum += load_elem(static_cast<const bf16_t*>(p.bias) + o0 + o);
@@ -267,6 +302,8 @@ struct ProductShape {
     static constexpr int threads = 256, frags = TILE / 64;                 // of 32 rows, a wave along each side
     static constexpr int panel_bytes = TILE * kPanel, step_bytes = 2 * panel_bytes, places = 4;
     static constexpr int loads = panel_bytes / (threads * 16);             // of an operand, a wave
+    // what a wave loads of PANELS panels in a row behind one that begins a block: both operands', and the exponents with every second
+    static constexpr int loads_of(int panels) { return 2 * loads * panels + (EXACT ? 0 : panels / 2); }
     static constexpr int exponents = EXACT ? 0 : 256;                      // bytes of a block's exponents, a wave
     // results pass through LDS, 32 tokens of a wave at a time
     static constexpr int row_bytes = TILE == 256 || EXACT ? 128 : 64, result_bytes = 32 * row_bytes;
@@ -274,6 +311,7 @@ struct ProductShape {
     static constexpr int lds_bytes = off_results + 4 * result_bytes;
 };
 
+constexpr unsigned kStrip = 4;
 struct Large {
     const unsigned char *w, *x;           // panels
     const unsigned char *e_w, *e_x;       // exponents (not EXACT): [output / 128 * e_output + block * e_depth], [block * tokens + place]
@@ -322,7 +360,7 @@ __device__ __forceinline__ void every(F&& f) {
 // Loads run three steps ahead of the products.  A step's operands are in registers when it begins; beside its products the next step's are
 // read, into the registers of those that have been used for the last time.
 template <bool EXACT, int TILE, typename O>
-__global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large p, O* __restrict__ out) {
+__global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large p, O* __restrict__ out) {
     typedef ProductShape<EXACT, TILE> S;
     constexpr int F = S::frags, L = S::loads;
     extern __shared__ __align__(16) char lds[];
@@ -330,8 +368,10 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
     const int wo = wave % 2 * (32 * F), wt = wave / 2 * (32 * F);
     const unsigned lds_base = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(lds)));
 
-    const unsigned n = die_order(blockIdx.x, gridDim.x);
-    const long long o0 = static_cast<long long>(n % p.tiles_o) * TILE, t0 = static_cast<long long>(n / p.tiles_o) * TILE;
+    // Tiles go by four along the outputs, then along the tokens: what one die has at a time is near a square, and shares operands both ways.
+    const unsigned n = die_order(blockIdx.x, gridDim.x), tiles_t = gridDim.x / p.tiles_o;
+    const unsigned strip = n / (kStrip * tiles_t), across = min(p.tiles_o - strip * kStrip, kStrip), at = n - strip * kStrip * tiles_t;
+    const long long o0 = static_cast<long long>(strip * kStrip + at % across) * TILE, t0 = static_cast<long long>(at / across) * TILE;
 
     // ---- loads: a lane's piece of each 64th row
     int load_place = 0;
@@ -354,10 +394,10 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
     auto load = [&](auto odd) ADASUM_INLINE {
         if constexpr (!EXACT && !decltype(odd)::value) {
             load_word_to_lds(reinterpret_cast<const unsigned char*>(reinterpret_cast<uintptr_t>(e_at) & ~static_cast<uintptr_t>(3)),
-                             lds_base + S::off_exponents + (wave * S::places + (load_place >> 1 & 3)) * S::exponents);
+                             lds_base + S::off_exponents + (wave * S::places + (load_place >> 1 & (S::places - 1))) * S::exponents);
             e_at += e_next;
         }
-        const unsigned to = lds_base + (load_place & 3) * S::step_bytes + wave * 1024;
+        const unsigned to = lds_base + (load_place & (S::places - 1)) * S::step_bytes + wave * 1024;
 #pragma unroll
         for (int k = 0; k < L; ++k) {
             load_to_lds(w_base, w_at[k], to + k * 4096);
@@ -413,23 +453,22 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
     const unsigned e_shift_next = static_cast<unsigned>(p.e_depth & 3) * 8;
     auto read_exponents = [&](int block) ADASUM_INLINE {
         if constexpr (!EXACT) {
-            const char* const at = lds + S::off_exponents + (wave * S::places + (block & 3)) * S::exponents;
+            const char* const at = lds + S::off_exponents + (wave * S::places + (block & (S::places - 1))) * S::exponents;
             // (of a wave with 64 of the 128 tokens, the upper or lower two bytes)
             next_x = *reinterpret_cast<const unsigned*>(at + 4 * row) >> (8 * ((wt & 127) / 32));
             next_w = *reinterpret_cast<const unsigned*>(at + 128) >> e_shift;
             e_shift = (e_shift + e_shift_next) & 31;
         }
     };
-    constexpr int kAhead = 2 * L + (EXACT ? 0 : 1);                                     // loads of two steps
-    // One step.  What is waited for is the next step's panel; those of two more steps came after it and may be under way.
+    // One step.  What is waited for is the next step's panel; all others that there are places for came after it and may be under way.
     auto step = [&](auto odd, auto more) ADASUM_INLINE {
         every<F>([&](auto j) { multiply(0, j); });
         __builtin_amdgcn_sched_barrier(0);
-        wait_for_loads<decltype(more)::value ? kAhead : 0>();
+        wait_for_loads<decltype(more)::value ? S::loads_of(S::places - 2) : 0>();
         __builtin_amdgcn_s_barrier();
         if constexpr (decltype(more)::value) load(odd);
         ++place;
-        const int from = (place & 3) * S::step_bytes;
+        const int from = (place & (S::places - 1)) * S::step_bytes;
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (decltype(odd)::value) read_exponents(place >> 1);
 #pragma unroll
@@ -523,13 +562,14 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
 
     const std::true_type yes;
     const std::false_type no;
-    // (there are at least four steps)
     asm volatile("s_nop 4");
-    load(no);
-    load(yes);
-    load(no);
-    load(yes);
-    wait_for_loads<0>();
+    // (there are at least as many steps as places)
+#pragma unroll
+    for (int k = 0; k < S::places; k += 2) {
+        load(no);
+        load(yes);
+    }
+    wait_for_loads<S::loads_of(S::places - 1)>();
     __builtin_amdgcn_s_barrier();
     read_exponents(0);
     of_w = next_w;
@@ -539,12 +579,12 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
         read_x(i, 0);
         read_w(i, 0);
     }
-    for (int s = 4; s < p.steps; s += 2) {
+    for (int s = S::places; s < p.steps; s += 2) {
         step(no, yes);
         step(yes, yes);
     }
-    // (the last four find all their panels loaded)
-    for (int s = 0; s < 4; s += 2) {
+    // (the last find all their panels loaded)
+    for (int s = 0; s < S::places; s += 2) {
         step(no, no);
         step(yes, no);
     }
@@ -552,8 +592,17 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
     else store(false);
 }
 
-// The kernel of few tokens does the large ones' work where there are none to fill a tile.
-bool is_large(int64_t rows, int64_t outputs, int64_t depth) { return rows > 64 && depth > 0 && outputs >= 16; }
+// From how many tiles of 16 x 16 on a workgroup takes two, and four, along the outputs: the tokens' operands are made once for them.  (4096 -> 1024 in
+// bf16, 64 rows with one 9.5 us, with two 7.2; 256 rows 28, 19 and with four 14; 1000 -> 2048, 128 rows 9.6 and 9.6.)
+constexpr int64_t kSomeTiles = 512, kManyTiles = 1024;
+// Whether the products go by tiles of 128 or 256, by what a call takes (microseconds) beside 3.5 either way: the kernel of few tokens 0.3 for each
+// thousand blocks of 16 x 16 x 128, the other, with the launch before it, 3 and 0.48 for each block of the depth; for fp32 results 0.5, and 7
+// and 1.  1024 -> 4096 in bf16, 128 rows 8.7 and 10.1, 256 rows 14.4 and 10.1; 2048 -> 1000, 256 rows 10.7 and 13.5, 512 rows 13.1 and 14;
+// 8192 -> 8192, 16 rows 21 and 35, 64 rows 38 and 37; 256 -> 256, 512 rows 4.1 and 6.4; fp32 1024 -> 4096, 128 rows 12.8 and 19, 256 rows 21 and 20.
+bool is_large(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) {
+    const double blocks = static_cast<double>(blocks8(depth)), tiles = static_cast<double>((rows + 15) / 16) * static_cast<double>((outputs + 15) / 16);
+    return depth > 0 && (out_dtype == ADASUM_F32 ? 0.0005 * tiles * blocks > 7 + blocks : 0.0003 * tiles * blocks > 3 + 0.48 * blocks);
+}
 // Whether operands are multiplied as the bf16 numbers that they stand for: for fp32 results, and where a tile would have two steps only (the
 // kernel's loads are three ahead).
 bool is_exact(int64_t depth, int out_dtype) { return out_dtype == ADASUM_F32 || depth <= kBlock8; }
@@ -563,7 +612,7 @@ struct Workspace8 {
 };
 Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) {
     Workspace8 w;
-    if (!is_large(rows, outputs, depth)) return w;
+    if (!is_large(rows, outputs, depth, out_dtype)) return w;
     const size_t pitch = static_cast<size_t>(blocks8(depth)) * kBlock8;
     const bool exact = is_exact(depth, out_dtype);
     w.off_more = static_cast<size_t>(rows) * pitch * (exact ? 2 : 1);
@@ -575,6 +624,7 @@ Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtyp
 template <bool EXACT, int TILE, typename O>
 int launch_large(const Product8& p, const Large& l, void* stream) {
     typedef ProductShape<EXACT, TILE> S;
+    static_assert(S::lds_bytes * (TILE == 128 ? 2 : 1) <= 160 << 10, "what a compute unit has");
     const auto kernel = product_kernel<EXACT, TILE, O>;
     const int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds_bytes));
     if (rc != 0) return rc;
@@ -622,9 +672,12 @@ int large_product(const Product8& p, void* stream) {
     l.steps = static_cast<int>(pitch * (EXACT ? 2 : 1) / kPanel);
     l.out_stride = p.out_stride;
     auto tiles = [&](int64_t n, int tile) { return (n + tile - 1) / tile; };
-    const bool wide = tiles(p.outputs, 256) * tiles(p.rows, 256) >= 192;
+    // A round of 256 tiles of edge 256 takes as long as 1.75 rounds of 512 of edge 128, of which it has two's work.  (8192 -> 8192 in bf16, 1024 rows:
+    // 80 us with 128 and 100 with 256, 2048: 148 and 137; 4096 -> 1024, 8192 rows 61 and 77, 16384: 116 and 108.)
+    const int64_t wide_tiles = tiles(p.outputs, 256) * tiles(p.rows, 256), small_tiles = tiles(p.outputs, 128) * tiles(p.rows, 128);
+    const bool wide = 7 * tiles(wide_tiles, 256) < 4 * tiles(small_tiles, 512);
     l.tiles_o = static_cast<unsigned>(tiles(p.outputs, wide ? 256 : 128));
-    l.tiles = static_cast<unsigned>(l.tiles_o * tiles(p.rows, wide ? 256 : 128));
+    l.tiles = static_cast<unsigned>(wide ? wide_tiles : small_tiles);
     return wide ? launch_large<EXACT, 256, O>(p, l, stream) : launch_large<EXACT, 128, O>(p, l, stream);
 }
 
@@ -641,7 +694,7 @@ int launch_weight8_store(const void* w, int dtype, const Weight8& to, void* stre
 size_t product8_workspace(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) { return workspace8(rows, outputs, depth, out_dtype).total; }
 
 int launch_product8(const Product8& p, void* stream) {
-    if (is_large(p.rows, p.outputs, p.depth)) {
+    if (is_large(p.rows, p.outputs, p.depth, p.out_dtype)) {
         const bool exact = is_exact(p.depth, p.out_dtype);
         switch (p.out_dtype) {
             case ADASUM_F32: return large_product<true, float>(p, stream);
@@ -655,8 +708,21 @@ int launch_product8(const Product8& p, void* stream) {
             typedef decltype(out) O;
             return with_form(row_form(p.depth, 8), [&](auto form) -> int {
                 constexpr RowForm F = decltype(form)::value;
-                const int64_t tiles_o = (p.outputs + 15) / 16, tiles = tiles_o * ((p.rows + 15) / 16);
-                return launch(few_tokens_kernel<X, O, F>, at_most_groups(tiles), 1, 256, 0, stream, p, tiles_o, tiles);
+                const int64_t tiles_t = (p.rows + 15) / 16, tiles = (p.outputs + 15) / 16 * tiles_t, blocks = blocks8(p.depth);
+                auto go = [&](auto waves, auto outputs) -> int {
+                    constexpr int W = decltype(waves)::value, N = decltype(outputs)::value;
+                    const int64_t tiles_o = (p.outputs + 16 * N - 1) / (16 * N);
+                    return launch(few_tokens_kernel<X, O, F, W, N>, at_most_groups(tiles_o * tiles_t), 1, 64 * W, 0, stream, p, tiles_o,
+                                  tiles_o * tiles_t);
+                };
+                const std::integral_constant<int, 1> one;
+                const std::integral_constant<int, 2> two;
+                const std::integral_constant<int, 4> four;
+                const std::integral_constant<int, 16> sixteen;
+                // (sixteen waves share a depth that four would go through in turn: 4096 -> 1024 in bf16, one row 10.0 and 7.9 us; fp32, whose
+                // operands take longer to make, 12.1 and 10.5, but 2048 -> 1000, 16 rows 8.4 and 9.6)
+                if (p.out_dtype == ADASUM_F32 ? tiles <= 64 && blocks > 16 : tiles <= 256 && blocks > 8) return go(sixteen, one);
+                return tiles >= kManyTiles ? go(four, four) : tiles >= kSomeTiles ? go(four, two) : go(four, one);
             });
         });
     });
