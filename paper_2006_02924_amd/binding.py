@@ -699,6 +699,11 @@ def _step_of(step, dev):
 
 def _same_rows(t, n, width, dtype, what):
     """The distance of two rows of a tensor that must have n rows of `width` elements of `dtype`."""
+    shape = t.shape
+    if len(shape) == 2 and shape[0] == n and shape[1] == width and (dtype is None or t.dtype == dtype):
+        stride = t.stride()
+        if stride[1] == 1:
+            return stride[0]
     have, _, stride = _rows_of(t, width, what)
     if (have != n and width) or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{what} must have {n} rows of {dtype}")
@@ -764,7 +769,6 @@ def adasum_join(join: Join, params, x, residual=None, *, step=None, h=None, y=No
     """The new residual stream ``h`` and the next block's input ``y`` (None without the norm ``before``) of a block's output ``x`` and the
     stream ``residual`` (None: none).  Returns (h, y), made here when None; without ``keep_h`` no h is made where none is given.
     ``h`` may be ``residual``.  The gradient wants h where the form has ``before``."""
-    lib = _lib or load()
     n, width, stride = _rows_of(x, join.width, "x")
     if x.dtype != join.dtype:
         raise ValueError("x must have the form's dtype")
@@ -776,15 +780,21 @@ def adasum_join(join: Join, params, x, residual=None, *, step=None, h=None, y=No
             y = _empty(tuple(x.shape), join.dtype, dev, stream)
     elif not join.before:
         raise ValueError("a form without the norm before the next block has no y")
-    there = [t for t in (params, residual, h, y) if t is not None]
-    _device_of(x, *there)
+    at_h = at_y = at_residual = None
+    h_stride = y_stride = residual_stride = 0
+    one_device = dev >= 0
+    if h is not None:
+        h_stride, at_h, one_device = _same_rows(h, n, width, join.stream_dtype, "h"), h.data_ptr(), one_device and h.get_device() == dev
+    if y is not None:
+        y_stride, at_y, one_device = _same_rows(y, n, width, join.dtype, "y"), y.data_ptr(), one_device and y.get_device() == dev
+    if residual is not None:
+        residual_stride = _same_rows(residual, n, width, join.stream_dtype, "residual")
+        at_residual, one_device = residual.data_ptr(), one_device and residual.get_device() == dev
+    if not one_device or (params is not None and params.get_device() != dev):
+        _device_of(x, *[t for t in (params, residual, h, y) if t is not None])
     flat, flat_type = join._flat(params, "params")
-    h_stride = 0 if h is None else _same_rows(h, n, width, join.stream_dtype, "h")
-    y_stride = 0 if y is None else _same_rows(y, n, width, join.dtype, "y")
-    residual_stride = 0 if residual is None else _same_rows(residual, n, width, join.stream_dtype, "residual")
-    _call(lib.adasum_join, dev, stream, join._ref, flat, flat_type, _step_of(step, dev), x.data_ptr(), stride,
-          None if residual is None else residual.data_ptr(), residual_stride, n, None if h is None else h.data_ptr(), h_stride,
-          None if y is None else y.data_ptr(), y_stride)
+    _call((_lib or load()).adasum_join, dev, stream, join._ref, flat, flat_type, None if step is None else _step_of(step, dev), x.data_ptr(), stride,
+          at_residual, residual_stride, n, at_h, h_stride, at_y, y_stride)
     return h, y
 
 

@@ -123,46 +123,52 @@ weight_values_kernel(const unsigned char* __restrict__ q, const unsigned char* _
 }
 
 // A workgroup puts a block of 128 outputs x 128 inputs into 8 bits, as it is and transposed (through LDS).
-template <typename T>
-__global__ void __launch_bounds__(256) weight8_store_kernel(const T* __restrict__ from, Weight8 w, int blocks_i, long long blocks) {
-    __shared__ unsigned most_of[4];
+template <typename T, RowForm FORM>
+__global__ void __launch_bounds__(1024) weight8_store_kernel(const T* __restrict__ from, Weight8 w, int blocks_i, long long blocks) {
+    __shared__ unsigned most_of[16];
     __shared__ __align__(16) unsigned char turned[kBlock8][kBlock8 + 4];   // [input][output]
     const int r = threadIdx.x / 16, c = threadIdx.x % 16 * 8;
     for (long long block = blockIdx.x; block < blocks; block += gridDim.x) {
         const long long o0 = block / blocks_i * kBlock8, i0 = block % blocks_i * kBlock8;
-        float v[8][8];
+        // (without branches: both are loaded before either is waited for)
+        Granule<T, 8> raw[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            load_row<FORM>(raw[k], from + min(o0 + 64 * k + r, static_cast<long long>(w.outputs) - 1) * w.width, static_cast<int>(i0) + c, static_cast<int>(w.width));
+        float v[2][8];
         unsigned most = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const long long o = o0 + 16 * k + r, left = w.width - (i0 + c);
+        for (int k = 0; k < 2; ++k) {
+            unpack(raw[k], v[k]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
-            if (o < w.outputs && left > 0) load_some(v[k], from + o * w.width + i0 + c, static_cast<int>(min(left, 8ll)));
-#pragma unroll
-            for (int i = 0; i < 8; ++i) most = max(most, finite_size(v[k][i]));
+            for (int i = 0; i < 8; ++i) {
+                if (o0 + 64 * k + r >= w.outputs || i0 + c + (FORM == kWhole ? 0 : i) >= w.width) v[k][i] = 0.f;
+                most = max(most, finite_size(v[k][i]));
+            }
         }
 #pragma unroll
         for (int m = 32; m >= 1; m >>= 1) most = max(most, static_cast<unsigned>(__shfl_xor(static_cast<int>(most), m, 64)));
         __syncthreads();   // (the last block's have been read)
         if ((threadIdx.x & 63) == 0) most_of[threadIdx.x / 64] = most;
         __syncthreads();
-        most = max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3]));
+#pragma unroll
+        for (int k = 0; k < 16; ++k) most = max(most, most_of[k]);
         const unsigned exponent = exponent_of(most);
         if (threadIdx.x == 0) w.e[block] = static_cast<unsigned char>(exponent);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 2; ++k) {
             u32x2 q;
             q.x = in_8_bits(v[k], exponent);
             q.y = in_8_bits(v[k] + 4, exponent);
-            const long long o = o0 + 16 * k + r;
+            const long long o = o0 + 64 * k + r;
             if (o < w.outputs) *reinterpret_cast<u32x2*>(w.q + panel_place(w.outputs, o, static_cast<int>(i0) + c)) = q;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) turned[c + i][16 * k + r] = static_cast<unsigned char>((i < 4 ? q.x : q.y) >> (8 * (i % 4)));
+            for (int i = 0; i < 8; ++i) turned[c + i][64 * k + r] = static_cast<unsigned char>((i < 4 ? q.x : q.y) >> (8 * (i % 4)));
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int in = 16 * k + r;
+        for (int k = 0; k < 2; ++k) {
+            const int in = 64 * k + r;
             if (i0 + in < w.width) {
                 u32x2 q;
                 q.x = *reinterpret_cast<const unsigned*>(&turned[in][c]);
@@ -687,7 +693,10 @@ int launch_weight8_store(const void* w, int dtype, const Weight8& to, void* stre
     const int64_t blocks_i = blocks8(to.width), blocks = blocks8(to.outputs) * blocks_i;
     return with_type(dtype, [&](auto t) -> int {
         typedef decltype(t) T;
-        return launch(weight8_store_kernel<T>, at_most_groups(blocks), 1, 256, 0, stream, static_cast<const T*>(w), to, blocks_i, blocks);
+        return with_form(row_form(to.width, 8), [&](auto form) -> int {
+            return launch(weight8_store_kernel<T, decltype(form)::value>, at_most_groups(blocks), 1, 1024, 0, stream, static_cast<const T*>(w), to,
+                          blocks_i, blocks);
+        });
     });
 }
 
