@@ -545,8 +545,9 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
                     const u32x4 v = *reinterpret_cast<const u32x4*>(piece_at(token, n));
                     const long long t = t0 + wt + 32 * j + token, o = o0 + wo + 32 * i0 + n * kOfLane;
                     O* const to = out + t * p.out_stride + o;
+                    // (past the caches: 32768 x 1024 -> 4096 in bf16 206 -> 202 us, in fp32 346 -> 318)
                     if (all) {
-                        store_at<false>(v, reinterpret_cast<u32x4_any*>(to));
+                        store_at<true>(v, reinterpret_cast<u32x4_any*>(to));
                     } else if (t < p.rows && o < p.outputs) {
                         if (p.outputs - o >= kOfLane) {
                             store_at<false>(v, reinterpret_cast<u32x4_any*>(to));
