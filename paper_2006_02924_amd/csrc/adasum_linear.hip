@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
 
     const std::true_type yes;
     const std::false_type no;
-    asm volatile("s_nop 4");
+    asm volatile("s_nop 4" : "+s"(w_base), "+s"(x_base));
     // (there are at least as many steps as places)
 #pragma unroll
     for (int k = 0; k < S::places; k += 2) {

@@ -187,6 +187,14 @@ def backward(types, k, n, width, gap):
         assert got[1] is dev[3] and torch.equal(got[1], dr) and torch.equal(got[0], dx)
 
 
+@pytest.mark.parametrize("k", [1, 3, 4])
+@pytest.mark.parametrize("n, width", [(20000, 130), (7000, 600), (1700, 2050), (70000, 24), (2600, 1024), (700, 5000)])
+def test_workgroups_that_go_round(k, n, width):
+    """More rows than the workgroups have at once."""
+    forward(("bf16", "f32"), k, n, width, 0)
+    backward(("bf16", "bf16"), k, n, width, 0)
+
+
 @pytest.mark.parametrize("k", range(len(FORMS)))
 def test_gradient_against_differences(k):
     """The gradient of sum(y wy + h wh) along random directions, by the pass that fp64 makes of the definition."""
