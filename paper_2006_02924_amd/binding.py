@@ -503,12 +503,24 @@ def _device_of(first, *others) -> int:
     return dev
 
 
+_current_stream = _current_device = None    # torch's own, without the objects around them; looked up by the first call
+
+
+def _learn_streams() -> None:
+    global _current_stream, _current_device
+    from torch import _C
+    _current_device = getattr(_C, "_cuda_getDevice", None)
+    _current_stream = getattr(_C, "_cuda_getCurrentRawStream", None) if _current_device is not None else None
+    if _current_stream is None:
+        _current_device = lambda: -1
+
+
 def _call(fn, dev, stream, *args):
     """The library launches on the current device: make that the tensors'."""
-    from torch import _C
-    raw = getattr(_C, "_cuda_getCurrentRawStream", None)
-    if raw is not None and stream is None and _C._cuda_getDevice() == dev:
-        code = fn(*args, raw(dev))
+    if _current_device is None:
+        _learn_streams()
+    if stream is None and _current_device() == dev:
+        code = fn(*args, _current_stream(dev))
     else:
         import torch
         with torch.cuda.device(dev):
