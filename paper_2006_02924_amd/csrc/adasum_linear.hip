@@ -410,6 +410,7 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
             e_at += e_next;
         }
         const unsigned to = lds_base + (load_place & (S::places - 1)) * S::step_bytes + wave * 1024;
+        asm volatile("s_nop 4" : "+s"(w_base), "+s"(x_base));   // (whoever wrote them last)
 #pragma unroll
         for (int k = 0; k < L; ++k) {
             load_to_lds(w_base, w_at[k], to + k * 4096);
@@ -575,7 +576,6 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
 
     const std::true_type yes;
     const std::false_type no;
-    asm volatile("s_nop 4" : "+s"(w_base), "+s"(x_base));
     // (there are at least as many steps as places)
 #pragma unroll
     for (int k = 0; k < S::places; k += 2) {

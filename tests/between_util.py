@@ -183,7 +183,7 @@ def e4m3(v):
 def exponent(block):
     """The least e >= -120 with max |x| <= 448 * 2^e over the finite values."""
     most = np.abs(np.where(np.isfinite(block), block, 0.0)).max(initial=0.0)
-    e = -120
+    e = max(-120, int(np.frexp(most)[1]) - 12) if most else -120      # 448 * 2^e is below it
     while most > np.ldexp(448.0, e):
         e += 1
     return e

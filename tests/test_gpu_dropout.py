@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from between_util import kept
+from between_util import kept, philox
 from layer_grads_util import DTYPES
 from paper_2006_02924_amd import binding as B
 
@@ -66,12 +66,14 @@ def test_more_dimensions_and_shared_rows():
 def test_rows_beyond_32_bits():
     n, width = (1 << 20) + 3, 2080
     x = torch.ones(n, width, dtype=torch.bfloat16, device="cuda")
-    got = B.adasum_dropout(x, 0.5, 1)
-    for row in (0, n // 2, n - 1):
-        lone, factor = kept(1, width, 0.5, 1) if row == 0 else (None, 2.0)
-        if lone is not None:
-            assert np.array_equal(got[0].float().cpu().numpy() == factor, lone[0])
-    assert abs(float((got != 0).double().mean()) - 0.5) < 1e-3
+    got = B.adasum_dropout(x, 0.5, SEED)
+    granules = np.arange(width // 8)
+    for row in (0, 1, n // 2, n - 2, n - 1):
+        words = philox([granules, np.full_like(granules, row), 0 * granules, 0 * granules], [SEED % 2 ** 32, SEED >> 32])
+        halves = np.stack([h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=1).reshape(-1)
+        assert np.array_equal(got[row].float().cpu().numpy(), np.where(halves >= 32768, 2.0, 0.0))
+    # five deviations of as many draws
+    assert abs(float((got != 0).double().mean()) - 0.5) < 5 * 0.5 / (n * width) ** 0.5
 
 
 def test_captured_with_a_step_that_moves():

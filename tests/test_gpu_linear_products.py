@@ -123,6 +123,15 @@ def test_numbers_that_8_bits_hold_are_multiplied_exactly():
         assert torch.equal(B.adasum_linear_grad(weight, dy.cuda()).cpu().double(), dy.double() @ w.double())
 
 
+@pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f32", "bf16")], ids="-".join)
+@pytest.mark.parametrize("n, width, outputs", [(3000, 300, 700), (2600, 1000, 520), (9000, 130, 260), (4100, 384, 1024)])
+def test_both_products_by_tiles(types, n, width, outputs):
+    """As above, of sizes that do not go the way of few tokens."""
+    dtype, out = DTYPES[types[0]], DTYPES[types[1]]
+    assert B.adasum_linear_workspace_bytes(n, width, outputs, out) > 0
+    products(dtype, out, n, width, outputs, 3)
+
+
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("n, width, outputs", [(12345, 100, 1100), (16640, 128, 1024), (9000, 384, 2050), (33000, 250, 520), (2300, 130, 515), (4100, 1000, 640),
                                               (70000, 64, 256), (257, 64, 60000)])
@@ -146,28 +155,30 @@ def test_many_tiles(n, width, outputs, out):
             assert torch.equal(B.adasum_linear_grad(weight, dy, out_dtype=out), want.to(out))
 
 
-@pytest.mark.parametrize("n", [20, 600])
-def test_rows_that_are_no_numbers_stay_alone(n):
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [20, 20000])
+def test_rows_that_are_no_numbers_stay_alone(n, out):
     width, outputs = 300, 140
     weight = B.adasum_linear_store((rand(1, outputs * width)).cuda(), 0, outputs, width)
     x = rand(2, n, width)
-    clean = B.adasum_linear(weight, x.cuda())
+    clean = B.adasum_linear(weight, x.cuda(), out_dtype=out)
     x[3, 5], x[7, 299], x[n - 1, 130] = float("nan"), float("inf"), float("-inf")
-    got = B.adasum_linear(weight, x.cuda())
+    got = B.adasum_linear(weight, x.cuda(), out_dtype=out)
     bad = [3, 7, n - 1]
     rest = [i for i in range(n) if i not in bad]
     assert got[bad].isnan().all() and torch.equal(got[rest], clean[rest])
 
 
-def test_magnitudes_at_the_ends():
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_magnitudes_at_the_ends(out):
     """Exponents of both ends of the range, apart and against each other."""
-    width, outputs = 256, 64
+    width, outputs = 256, 1024
     for wide, small in ((1e30, 1e-30), (1e-36, 1.0), (1.0, 1e-38), (2.0 ** 127, 2.0 ** -100)):
-        for n in (4, 300):
+        for n in (4, 4000):
             w, x = rand(1, outputs, width) * small, rand(2, n, width).clamp(-1.9, 1.9) * wide
             weight = B.adasum_linear_store(w.reshape(-1).cuda(), 0, outputs, width)
             w8, x8 = in_8_bits(f64(w), 128)[0], in_8_bits(f64(x), 1)[0]
-            near(B.adasum_linear(weight, x.cuda()), x8 @ w8.T, bound(x8, w8, width, torch.float32))
+            near(B.adasum_linear(weight, x.cuda(), out_dtype=out), x8 @ w8.T, bound(x8, w8, width, out))
 
 
 def test_more_dimensions_no_rows_and_no_depth():
@@ -200,7 +211,7 @@ def test_rows_beyond_32_bits():
     assert int(torch.count_nonzero(back[1:n - 1])) == 0
 
 
-@pytest.mark.parametrize("n", [3, 900])
+@pytest.mark.parametrize("n", [3, 5000])
 def test_captured_on_another_stream_and_with_a_workspace(n):
     width, outputs = 768, 520
     flat = rand(1, outputs * width + outputs).cuda()
