@@ -837,19 +837,28 @@ def adasum_join_grad(join: Join, params, grad, *, x=None, h=None, dy=None, dh=No
         dresidual = _empty(tuple(first.shape), join.stream_dtype, dev, stream)
     elif dresidual is False:
         dresidual = None
-    rows = []
-    for t, dtype, what in ((x if join.reads_x else None, join.dtype, "x"), (h, join.stream_dtype, "h"), (dy, join.dtype, "dy"),
-                           (dh, join.stream_dtype, "dh")):
-        rows += (None, 0) if t is None else (t.data_ptr(), _same_rows(t, n, width, dtype, what))
-    to = []
-    for t, dtype, what in ((dx, join.dtype, "dx"), (dresidual, join.stream_dtype, "dresidual")):
-        to += (None, 0) if t is None else (t.data_ptr(), _same_rows(t, n, width, dtype, what))
-    _device_of(first, *[t for t in (params, grad, x, h, dy, dh, dx, dresidual) if t is not None])
+    one_device = dev >= 0
+    at_x = at_h = at_dy = at_dh = at_dresidual = None
+    x_stride = h_stride = dy_stride = dh_stride = dresidual_stride = 0
+    if join.reads_x:
+        x_stride, at_x, one_device = _same_rows(x, n, width, join.dtype, "x"), x.data_ptr(), one_device and x.get_device() == dev
+    if h is not None:
+        h_stride, at_h, one_device = _same_rows(h, n, width, join.stream_dtype, "h"), h.data_ptr(), one_device and h.get_device() == dev
+        dy_stride, at_dy, one_device = _same_rows(dy, n, width, join.dtype, "dy"), dy.data_ptr(), one_device and dy.get_device() == dev
+    if dh is not None:
+        dh_stride, at_dh, one_device = _same_rows(dh, n, width, join.stream_dtype, "dh"), dh.data_ptr(), one_device and dh.get_device() == dev
+    if dresidual is not None:
+        dresidual_stride = _same_rows(dresidual, n, width, join.stream_dtype, "dresidual")
+        at_dresidual, one_device = dresidual.data_ptr(), one_device and dresidual.get_device() == dev
+    dx_stride = _same_rows(dx, n, width, join.dtype, "dx")
+    if not one_device or dx.get_device() != dev or (params is not None and params.get_device() != dev) or (grad is not None and grad.get_device() != dev):
+        _device_of(first, *[t for t in (params, grad, x if join.reads_x else None, h, dy, dh, dx, dresidual) if t is not None])
     flat, flat_type = join._flat(params, "params")
     grads, grad_type = join._flat(grad, "grad")
     ws, ws_bytes, _keep = _scratch(workspace, lambda: adasum_join_grad_workspace_bytes(join, n), dev, stream)
-    _call(lib.adasum_join_grad, dev, stream, join._ref, flat, flat_type, _step_of(step, dev), *rows, n, *to, grads, grad_type,
-          1 if accumulate else 0, ws, ws_bytes)
+    _call(lib.adasum_join_grad, dev, stream, join._ref, flat, flat_type, None if step is None else _step_of(step, dev), at_x, x_stride, at_h, h_stride,
+          at_dy, dy_stride, at_dh, dh_stride, n, dx.data_ptr(), dx_stride, at_dresidual, dresidual_stride, grads, grad_type, 1 if accumulate else 0, ws,
+          ws_bytes)
     return dx, dresidual
 
 

@@ -372,7 +372,7 @@ __device__ __forceinline__ void every(F&& f) {
 // again on its start and its results.  Loads run three steps ahead of the products.  A step's operands are in registers when it begins; beside its products the next step's are
 // read, into the registers of those that have been used for the last time.
 template <bool EXACT, int TILE, typename O>
-__global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large p, O* __restrict__ out) {
+__global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large p, O* __restrict__ out) {
     typedef ProductShape<EXACT, TILE> S;
     constexpr int F = S::frags, L = S::loads;
     extern __shared__ __align__(16) char lds[];
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
         x_at[k] = min(row, x_last) * kPanel + 16 * piece;
     }
     // (of the exponents, the first half of the lanes load the tokens', the others the word that has the weight's)
-    const unsigned char* const of_x0 = EXACT ? nullptr : p.e_x + t0 + (wt & ~127) + 4 * (lane & 31);
+    const unsigned char* const of_x0 = EXACT ? nullptr : p.e_x + ((t0 + wt) & ~127ll) + 4 * (lane & 31);
     const unsigned char* const of_w0 = EXACT ? nullptr : p.e_w + min(o0 + wo, p.outputs - 1) / kBlock8 * p.e_output;
     const unsigned char* e_at = lane < 32 ? of_x0 : of_w0;
     const long long of_tokens = p.tokens, of_weight = p.e_depth, e_next = lane < 32 ? of_tokens : of_weight;
@@ -467,8 +467,8 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
     auto read_exponents = [&](int block) ADASUM_INLINE {
         if constexpr (!EXACT) {
             const char* const at = lds + S::off_exponents + (wave * S::places + (block & (S::places - 1))) * S::exponents;
-            // (of a wave with 64 of the 128 tokens, the upper or lower two bytes)
-            next_x = *reinterpret_cast<const unsigned*>(at + 4 * row) >> (8 * ((wt & 127) / 32));
+            // (of a wave with fewer than the 128 tokens, its bytes)
+            next_x = *reinterpret_cast<const unsigned*>(at + 4 * row) >> (8 * (static_cast<int>(t0 + wt) & 127) / 32);
             next_w = *reinterpret_cast<const unsigned*>(at + 128) >> e_shift;
             e_shift = (e_shift + e_shift_next) & 31;
         }
@@ -608,13 +608,14 @@ __global__ void __launch_bounds__(256, TILE == 128 ? 2 : 1) product_kernel(Large
 // From how many tiles of 16 x 16 on a workgroup takes two, and four, along the outputs: the tokens' operands are made once for them.  (4096 -> 1024 in
 // bf16, 64 rows with one 9.5 us, with two 7.2; 256 rows 28, 19 and with four 14; 1000 -> 2048, 128 rows 9.6 and 9.6.)
 constexpr int64_t kSomeTiles = 512, kManyTiles = 1024;
-// Whether the products go by tiles of 128 or 256, by what a call takes (microseconds) beside 3.5 either way: the kernel of few tokens 0.3 for each
-// thousand blocks of 16 x 16 x 128, the other, with the launch before it, 3 and 0.48 for each block of the depth; for fp32 results 0.5, and 7
-// and 1.  1024 -> 4096 in bf16, 128 rows 8.7 and 10.1, 256 rows 14.4 and 10.1; 2048 -> 1000, 256 rows 10.7 and 13.5, 512 rows 13.1 and 14;
-// 8192 -> 8192, 16 rows 21 and 35, 64 rows 38 and 37; 256 -> 256, 512 rows 4.1 and 6.4; fp32 1024 -> 4096, 128 rows 12.8 and 19, 256 rows 21 and 20.
+// Whether the products go by tiles of 64 to 256, by what a call takes (microseconds) beside 3.5 either way: the kernel of few tokens 0.3 for each
+// thousand blocks of 16 x 16 x 128, the other, with the launch before it, 1.5 and 0.33 for each block of the depth; for fp32 results 0.48, and
+// 3 and 0.75.  1024 -> 4096 in bf16, 64 rows 6.3 and 7.4, 128 rows 8.6 and 7.5; 2048 -> 1000, 256 rows 11.0 and 10.5, 512 rows 13.4 and 11.2;
+// 8192 -> 8192, 32 rows 22 and 27, 64 rows 38 and 28; 256 -> 256, 2048 rows 5.2 and 5.6, 4096 rows 8.7 and 6.2; fp32 1024 -> 4096, 128 rows 12.5 and
+// 15.4, 256 rows 20.6 and 16.5.
 bool is_large(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) {
     const double blocks = static_cast<double>(blocks8(depth)), tiles = static_cast<double>((rows + 15) / 16) * static_cast<double>((outputs + 15) / 16);
-    return depth > 0 && (out_dtype == ADASUM_F32 ? 0.0005 * tiles * blocks > 7 + blocks : 0.0003 * tiles * blocks > 3 + 0.48 * blocks);
+    return depth > 0 && (out_dtype == ADASUM_F32 ? 0.00048 * tiles * blocks > 3 + 0.75 * blocks : 0.0003 * tiles * blocks > 1.5 + 0.33 * blocks);
 }
 // Whether operands are multiplied as the bf16 numbers that they stand for: for fp32 results, and where a tile would have two steps only (the
 // kernel's loads are three ahead).
@@ -637,7 +638,7 @@ Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtyp
 template <bool EXACT, int TILE, typename O>
 int launch_large(const Product8& p, const Large& l, void* stream) {
     typedef ProductShape<EXACT, TILE> S;
-    static_assert(S::lds_bytes * (TILE == 128 ? 2 : 1) <= 160 << 10, "what a compute unit has");
+    static_assert(S::lds_bytes * (TILE == 256 ? 1 : 2) <= 160 << 10, "what a compute unit has");
     const auto kernel = product_kernel<EXACT, TILE, O>;
     const int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds_bytes));
     if (rc != 0) return rc;
@@ -648,6 +649,10 @@ int launch_large(const Product8& p, const Large& l, void* stream) {
 // four, 16777 127 and 116)
 constexpr int64_t kMany8 = 1 << 23;
 
+// Tiles of edge 128 up to which those of 64 are faster: a compute unit's own loads bound these calls (some 60 GB/s), and more of them share a
+// product.  8192 -> 8192 in bf16, 256 rows (128 tiles) 39 us with 128 and 35 with 64, 512 rows (256 tiles) 44 and 64; 4096 -> 1024, 128 rows 19.7 and
+// 14.8, 2048 rows (128 tiles) 27.6 and 26.1.
+constexpr int64_t kFewSmall = 128;
 // Rows into 8 bits (fp32 results: both operands into the values those stand for), then the product.
 template <bool EXACT, typename O>
 int large_product(const Product8& p, void* stream) {
@@ -691,9 +696,11 @@ int large_product(const Product8& p, void* stream) {
     // 80 us with 128 and 100 with 256, 2048: 148 and 137; 4096 -> 1024, 8192 rows 61 and 77, 16384: 116 and 108.)
     const int64_t wide_tiles = tiles(p.outputs, 256) * tiles(p.rows, 256), small_tiles = tiles(p.outputs, 128) * tiles(p.rows, 128);
     const bool wide = 7 * tiles(wide_tiles, 256) < 4 * tiles(small_tiles, 512);
-    l.tiles_o = static_cast<unsigned>(tiles(p.outputs, wide ? 256 : 128));
-    l.tiles = static_cast<unsigned>(wide ? wide_tiles : small_tiles);
-    return wide ? launch_large<EXACT, 256, O>(p, l, stream) : launch_large<EXACT, 128, O>(p, l, stream);
+    const int tile = wide ? 256 : small_tiles > kFewSmall ? 128 : 64;
+    l.tiles_o = static_cast<unsigned>(tiles(p.outputs, tile));
+    l.tiles = static_cast<unsigned>(l.tiles_o * tiles(p.rows, tile));
+    return tile == 256 ? launch_large<EXACT, 256, O>(p, l, stream)
+                       : tile == 128 ? launch_large<EXACT, 128, O>(p, l, stream) : launch_large<EXACT, 64, O>(p, l, stream);
 }
 
 }  // namespace

@@ -124,7 +124,7 @@ def test_numbers_that_8_bits_hold_are_multiplied_exactly():
 
 
 @pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f32", "bf16")], ids="-".join)
-@pytest.mark.parametrize("n, width, outputs", [(3000, 300, 700), (2600, 1000, 520), (9000, 130, 260), (4100, 384, 1024)])
+@pytest.mark.parametrize("n, width, outputs", [(3000, 300, 700), (2600, 1000, 520), (9000, 130, 260), (4100, 384, 1024), (8300, 300, 1030)])
 def test_both_products_by_tiles(types, n, width, outputs):
     """As above, of sizes that do not go the way of few tokens."""
     dtype, out = DTYPES[types[0]], DTYPES[types[1]]
@@ -134,7 +134,7 @@ def test_both_products_by_tiles(types, n, width, outputs):
 
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("n, width, outputs", [(12345, 100, 1100), (16640, 128, 1024), (9000, 384, 2050), (33000, 250, 520), (2300, 130, 515), (4100, 1000, 640),
-                                              (70000, 64, 256), (257, 64, 60000)])
+                                              (70000, 64, 256), (257, 64, 60000), (8300, 300, 1030), (8300, 1030, 300)])
 def test_many_tiles(n, width, outputs, out):
     """More tiles than workgroups, whole ones and others, few and many steps: whole numbers whose sums all types hold."""
     g = torch.Generator(device="cuda").manual_seed(1)
