@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(64 * WAVES) few_tokens_kernel(Product8 p, long
 // TILE x TILE of the result: what a workgroup of four waves computes at a time.  A step is a panel of both operands, 64 bytes of the depth (64
 // numbers of 8 bits, 32 of 16).  Panels go to LDS past the registers, into one of four places in turn.  A row's four pieces of 16 bytes lie
 // there at their number exclusive-or a quarter of the row's, so that sixteen rows' same piece lies in all banks.
-template <bool EXACT, int TILE>
+template <bool EXACT, int TILE, typename O>
 struct ProductShape {
     static constexpr int threads = 256, frags = TILE / 64;                 // of 32 rows, a wave along each side
     static constexpr int panel_bytes = TILE * kPanel, step_bytes = 2 * panel_bytes, places = 4;
@@ -315,8 +315,11 @@ struct ProductShape {
     // what a wave loads of PANELS panels in a row behind one that begins a block: both operands', and the exponents with every second
     static constexpr int loads_of(int panels) { return 2 * loads * panels + (EXACT ? 0 : panels / 2); }
     static constexpr int exponents = EXACT ? 0 : 256;                      // bytes of a block's exponents, a wave
-    // results pass through LDS, 32 tokens of a wave at a time
-    static constexpr int row_bytes = TILE == 256 || EXACT ? 128 : 64, result_bytes = 32 * row_bytes;
+    // results pass through LDS, 32 tokens of a wave at a time, as many of its outputs as there is room for, in whole fragments
+    static constexpr int frag_bytes = 32 * static_cast<int>(sizeof(O));
+    static constexpr int row_bytes = (TILE == 256 || EXACT) && frags * frag_bytes >= 128 ? 128 : 64, result_bytes = 32 * row_bytes;
+    static constexpr int frags_at_once = row_bytes / frag_bytes;
+    static_assert(frags_at_once >= 1 && frags % frags_at_once == 0, "a wave has no other fragments than its own");
     static constexpr int off_exponents = places * step_bytes, off_results = off_exponents + 4 * places * exponents;
     static constexpr int lds_bytes = off_results + 4 * result_bytes;
 };
@@ -373,7 +376,7 @@ __device__ __forceinline__ void every(F&& f) {
 // read, into the registers of those that have been used for the last time.
 template <bool EXACT, int TILE, typename O>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large p, O* __restrict__ out) {
-    typedef ProductShape<EXACT, TILE> S;
+    typedef ProductShape<EXACT, TILE, O> S;
     constexpr int F = S::frags, L = S::loads;
     extern __shared__ __align__(16) char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -510,8 +513,7 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
     // ---- results: a lane has four times four consecutive outputs of a token in each 32 x 32; through LDS consecutive lanes get a token's
     // consecutive outputs to store
     char* const mine = lds + S::off_results + wave * S::result_bytes;
-    constexpr int kPieces = S::row_bytes / 16, kFrags = S::row_bytes / (32 * static_cast<int>(sizeof(O)));   // of 32 outputs, at a time
-    static_assert(kFrags >= 1, "");
+    constexpr int kPieces = S::row_bytes / 16, kFrags = S::frags_at_once;   // of 32 outputs, at a time
     auto piece_at = [&](int token, int n) {
         return mine + token * S::row_bytes + 16 * (n ^ (kPieces == 8 ? token >> 1 & 7 : token >> 2 & 3));
     };
@@ -637,7 +639,7 @@ Workspace8 workspace8(int64_t rows, int64_t outputs, int64_t depth, int out_dtyp
 
 template <bool EXACT, int TILE, typename O>
 int launch_large(const Product8& p, const Large& l, void* stream) {
-    typedef ProductShape<EXACT, TILE> S;
+    typedef ProductShape<EXACT, TILE, O> S;
     static_assert(S::lds_bytes * (TILE == 256 ? 1 : 2) <= 160 << 10, "what a compute unit has");
     const auto kernel = product_kernel<EXACT, TILE, O>;
     const int rc = static_cast<int>(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::lds_bytes));
