@@ -509,10 +509,9 @@ _current_stream = _current_device = None    # torch's own, without the objects a
 def _learn_streams() -> None:
     global _current_stream, _current_device
     from torch import _C
-    _current_device = getattr(_C, "_cuda_getDevice", None)
-    _current_stream = getattr(_C, "_cuda_getCurrentRawStream", None) if _current_device is not None else None
-    if _current_stream is None:
-        _current_device = lambda: -1
+    device, _current_stream = getattr(_C, "_cuda_getDevice", None), getattr(_C, "_cuda_getCurrentRawStream", None)
+    # (last: a thread that finds a device calls the stream)
+    _current_device = device if device is not None and _current_stream is not None else lambda: -1
 
 
 def _call(fn, dev, stream, *args):
