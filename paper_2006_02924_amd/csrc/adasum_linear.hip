@@ -340,10 +340,10 @@ struct Large {
 // Sixteen (or four) bytes a lane from base + offset to LDS, a wave's one after the other from `to` on.  (The builtin makes every later read of
 // LDS wait for it, of whatever place.  There is no register that the load writes; the loop below waits for it by itself.)
 __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned offset, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
 __device__ __forceinline__ void load_word_to_lds(const unsigned char* at, unsigned to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(at) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(at) : "m0", "memory");
 }
 // An address that all lanes have, in scalar registers.
 __device__ __forceinline__ const unsigned char* in_scalars(const unsigned char* p) {
