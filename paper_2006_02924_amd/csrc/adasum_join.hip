@@ -173,7 +173,9 @@ struct Row {
         for (int k = 0; k < V; ++k)
 #pragma unroll
             for (int i = 0; i < kG; ++i) q = __builtin_fmaf(v[k][i], v[k][i], q);
-        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(sums(q), each, eps));
+        const float square = __builtin_fmaf(sums(q), each, eps);
+        // (one over an infinity would be 0, and the row its bias)
+        const float r = square < __builtin_inff() ? 1.f / __builtin_sqrtf(square) : __builtin_nanf("");
 #pragma unroll
         for (int k = 0; k < V; ++k)
 #pragma unroll
