@@ -3,7 +3,7 @@
 // with N the norm of a row (its mean and spread, or its spread alone) and D dropout.  (Compiled once for each pair of storage types.)
 //
 // A row lies in the registers of a run of lanes, eight channels a granule, from its loads to its stores: the statistics are sums over the
-// lanes, first the mean, then the squares of what is left, so that nothing cancels.  A workgroup goes from row to row with the
+// lanes, first the mean, then that of what is left, then the squares, so that nothing cancels.  A workgroup goes from row to row with the
 // parameters' vectors in registers; the gradient adds those of the parameters up there too, each lane its own channels' in fp32 over the
 // workgroup's rows, and a second launch adds the workgroups' in fp64.  The gradient works the statistics out again from the rows that it
 // reads anyhow: nothing is kept for it but the rows themselves.
@@ -156,17 +156,22 @@ struct Row {
     }
     // v normed (hat); returns one over its spread
     __device__ __forceinline__ float normed(Part& v, RowSums<LANES>& sums, bool centred, float eps, float each) const {
+        // (the mean a second time: what the first one's rounding leaves is the whole of a row of equal values, and counts where eps is small.  16384 x
+        // 1024 in bf16 28.8 and 29.3 us, gradient 34.3 and 34.5; 32749 x 1024 with all parts, two gradients, 246 and 249.)
         if (centred) {
-            float s = 0.f;
 #pragma unroll
-            for (int k = 0; k < V; ++k)
+            for (int pass = 0; pass < 2; ++pass) {
+                float s = 0.f;
 #pragma unroll
-                for (int i = 0; i < kG; ++i) s += v[k][i];
-            const float mean = sums(s) * each;
+                for (int k = 0; k < V; ++k)
 #pragma unroll
-            for (int k = 0; k < V; ++k)
+                    for (int i = 0; i < kG; ++i) s += v[k][i];
+                const float mean = sums(s) * each;
 #pragma unroll
-                for (int i = 0; i < kG; ++i) v[k][i] = there(k, i) ? v[k][i] - mean : 0.f;
+                for (int k = 0; k < V; ++k)
+#pragma unroll
+                    for (int i = 0; i < kG; ++i) v[k][i] = there(k, i) ? v[k][i] - mean : 0.f;
+            }
         }
         float q = 0.f;
 #pragma unroll
