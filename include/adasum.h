@@ -493,7 +493,8 @@ ADASUM_API int adasum_join(const adasum_join_form* form, const void* params, int
  *   grad       may be NULL where the form names no vector.  Every result's layer (offset, width) has its place: two that overlap
  *              are ADASUM_ERR_ALIAS, as is any other overlap of a result.
  * rows = 0 sets the parameters' gradients to 0 (or leaves them, with `accumulate`).  A lane sums up to rows / 256 of its rows (rounded up) in
- * fp32, what is above that is summed in fp64: bit-identical from run to run.
+ * fp32.  The lanes of a workgroup that have the same channel meet in fp64, what a workgroup has is rounded to fp32 once, and the
+ * workgroups are summed in fp64: bit-identical from run to run.
  */
 ADASUM_API int adasum_join_grad_workspace_bytes(const adasum_join_form* form, int64_t rows, size_t* bytes);
 ADASUM_API int adasum_join_grad(const adasum_join_form* form, const void* params, int param_dtype, const uint64_t* step,

@@ -5,8 +5,8 @@
 // A row lies in the registers of a run of lanes, eight channels a granule, from its loads to its stores: the statistics are sums over the
 // lanes, first the mean, then that of what is left, then the squares, so that nothing cancels.  A workgroup goes from row to row with the
 // parameters' vectors in registers; the gradient adds those of the parameters up there too, each lane its own channels' in fp32 over the
-// workgroup's rows, and a second launch adds the workgroups' in fp64.  The gradient works the statistics out again from the rows that it
-// reads anyhow: nothing is kept for it but the rows themselves.
+// workgroup's rows, which meet in fp64 (rounded once into the workspace), and a second launch adds the workgroups' in fp64.  The gradient
+// works the statistics out again from the rows that it reads anyhow: nothing is kept for it but the rows themselves.
 //
 // Memory bounds it: 16384 x 1024 in bf16 with dropout (134 MB) 28 us, its gradient 30 and 4 for the second launch; 32749 x 1024 with an fp32 stream and
 // all parts (604 MB), gradient 114 - 118 us, 5.1 TB/s.  The vector units take half to two thirds of that, so that what they do counts: rows that fill their
@@ -465,10 +465,10 @@ join_grad_kernel(Args a) {
                 for (int i = 0; i < kG; ++i) meet[threadIdx.x / LANES][r.at(k) + i] = total[s][k][i];
             __syncthreads();
             for (int j = threadIdx.x; j < a.width; j += R::threads) {
-                float sum = 0.f;
+                double sum = 0.0;
 #pragma unroll
                 for (int w = 0; w < R::rows_at_once; ++w) sum += meet[w][j];
-                to[s * a.width + j] = sum;
+                to[s * a.width + j] = static_cast<float>(sum);
             }
         }
     } else {
