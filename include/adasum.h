@@ -485,7 +485,8 @@ ADASUM_API int adasum_join(const adasum_join_form* form, const void* params, int
  *   dx = gradient of gate * dropout(v) at x, of D
  *   grad[before_weight + j] (+)= sum_t dy N(h),  [before_bias + j] (+)= sum_t dy,  [gate + j] (+)= sum_t D dropout(v),
  *   grad[after_weight + j] (+)= sum_t dv N(x),   [after_bias + j] (+)= sum_t dv,   with dv = the gradient that reaches v
- * The statistics are those of the rows that are given here.
+ * The statistics are those of the rows that are given here.  The gate's gradient is made of the sums of the two below it, as after_weight *
+ * (sum_t D' N(x)) + after_bias * (sum_t D') with D' the gradient that leaves dropout: its error is that of the two, also where they nearly cancel.
  *   x          read with `after` or a gate, else not looked at
  *   h, dy      read with `before`, else not looked at
  *   dh         NULL: none (only with `before`)

@@ -268,7 +268,8 @@ join_kernel(Args a) {
     r.lane = threadIdx.x % LANES;
     if (a.rows == 0) return;
     const Step step = step_of(a.mask);
-    // (gate * dropout(hat * weight + bias) is taken as dropout(hat * (gate * weight) + gate * bias))
+    // (gate * dropout(hat * weight + bias) is taken as dropout(hat * (gate * weight) + gate * bias), two vectors in registers instead of three: either
+    // way three roundings to fp32, of products of the gate instead of what it multiplies)
     Part aw, ab, bw, bb;
     if constexpr (FULL) {
         r.param(aw, a.after_weight, a.param_type, 1.f);
@@ -337,7 +338,8 @@ join_kernel(Args a) {
 
 // What is summed over the rows, with D the gradient that comes to dropout, as it leaves of it, and v what the gate and the norm of x get to
 // see: x, normed where there is a norm.  The gradients of the weight and bias of that norm are gate * (sum of D v) and gate * (sum of D),
-// the gate's is weight * (sum of D v) + bias * (sum of D).
+// the gate's is weight * (sum of D v) + bias * (sum of D), both in fp64 by then: where those nearly cancel its error is that of the two sums, of
+// the same kind as the rounding of each row's hat * weight + bias would leave.
 enum { kAfterProduct, kAfter, kBeforeWeight, kBeforeBias };
 
 template <int LANES, int V, RowForm FORM, bool FILLED, bool FULL>
