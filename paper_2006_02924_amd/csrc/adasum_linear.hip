@@ -337,6 +337,8 @@ struct Large {
 
 // (Scalars that the vector unit writes may be read as addresses five instructions later, m0 one later: nobody but this file sees to that in
 // the assembly below.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // (that nobody keeps m0 for later across these: nobody is to)
 // Sixteen (or four) bytes a lane from base + offset to LDS, a wave's one after the other from `to` on.  (The builtin makes every later read of
 // LDS wait for it, of whatever place.  There is no register that the load writes; the loop below waits for it by itself.)
 __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned offset, unsigned to) {
@@ -345,6 +347,7 @@ __device__ __forceinline__ void load_to_lds(const unsigned char* base, unsigned 
 __device__ __forceinline__ void load_word_to_lds(const unsigned char* at, unsigned to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(at) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 // An address that all lanes have, in scalar registers.
 __device__ __forceinline__ const unsigned char* in_scalars(const unsigned char* p) {
     const unsigned long long a = reinterpret_cast<unsigned long long>(p);
