@@ -74,6 +74,7 @@ template <typename X, RowForm FORM, bool EXACT, int ITEMS>
 __global__ void __launch_bounds__(kThreadsRow)
 rows8_kernel(const X* __restrict__ x, long long stride, int width, unsigned char* __restrict__ to, unsigned char* __restrict__ e, long long tokens,
              RowWork work) {
+    static_assert(EXACT || FORM != kShort, "a depth below 8 is EXACT");
     constexpr bool NT = ITEMS > 1;
     every_rows(work, [&](long long first, unsigned n) {
         for (unsigned base = threadIdx.x; base < n; base += kThreadsRow * ITEMS) {
@@ -194,6 +195,7 @@ __global__ void __launch_bounds__(1024) weight8_store_kernel(const T* __restrict
 // they are, puts those of the tokens into 8 bits where the matrix cores want them, and multiplies.
 template <typename X, typename O, RowForm FORM, int WAVES, int OUTPUTS>
 __global__ void __launch_bounds__(64 * WAVES) few_tokens_kernel(Product8 p, long long tiles_o, long long tiles) {
+    static_assert(WAVES == 4 || FORM != kShort, "a depth below 8 is one block, which needs no sixteen waves");
     constexpr int kOutputs = 16 * OUTPUTS;
     __shared__ float meet[WAVES][16][kOutputs + 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, group = lane >> 4;
@@ -669,7 +671,8 @@ int large_product(const Product8& p, void* stream) {
         typedef decltype(t) X;
         const RowGrid g = row_grid(p.rows, pitch, p.dtype, kMany8);
         return with_form(row_form(p.depth, kG), [&](auto form) -> int {
-            constexpr RowForm F = decltype(form)::value;
+            // (a depth below 8 is EXACT)
+            constexpr RowForm F = !EXACT && decltype(form)::value == kShort ? kRagged : decltype(form)::value;
             return with_items<X>(g, [&](auto items) -> int {
                 return launch(rows8_kernel<X, F, EXACT, decltype(items)::value>, g.groups, 1, kThreadsRow, 0, stream, static_cast<const X*>(p.x),
                               p.x_stride, p.depth, x, EXACT ? nullptr : more, tokens, g.work);
@@ -751,7 +754,9 @@ int launch_product8(const Product8& p, void* stream) {
                 const std::integral_constant<int, 16> sixteen;
                 // (sixteen waves share a depth that four would go through in turn: 4096 -> 1024 in bf16, one row 10.0 and 7.9 us; fp32, whose
                 // operands take longer to make, 12.1 and 10.5, but 2048 -> 1000, 16 rows 8.4 and 9.6)
-                if (p.out_dtype == ADASUM_F32 ? tiles <= 64 && blocks > 16 : tiles <= 256 && blocks > 8) return go(sixteen, one);
+                if constexpr (F != kShort) {
+                    if (p.out_dtype == ADASUM_F32 ? tiles <= 64 && blocks > 16 : tiles <= 256 && blocks > 8) return go(sixteen, one);
+                }
                 return tiles >= kManyTiles ? go(four, four) : tiles >= kSomeTiles ? go(four, two) : go(four, one);
             });
         });
