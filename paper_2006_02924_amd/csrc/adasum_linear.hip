@@ -615,6 +615,10 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) product_kernel(Large
 // From how many tiles of 16 x 16 on a workgroup takes two, and four, along the outputs: the tokens' operands are made once for them.  (4096 -> 1024 in
 // bf16, 64 rows with one 9.5 us, with two 7.2; 256 rows 28, 19 and with four 14; 1000 -> 2048, 128 rows 9.6 and 9.6.)
 constexpr int64_t kSomeTiles = 512, kManyTiles = 1024;
+// 16-bit results of one block of depth: the other kernel's workgroups are on the chip at once up to 4096 tiles of 16 x 16 (16 x 64 for each of four a
+// compute unit).  128 -> 1024 in bf16, 1024 rows (4096 tiles) 7.3 and 7.4 with tiles, 1088 rows 9.4 and 7.6, 2048 rows 12.9 and 8.2; 128 -> 128, 8192
+// rows 7.2 and 8.0, 9216 rows 9.5 and 8.6; but 128 -> 32, 36864 rows (4608 tiles) 15.0 and 15.6.  (Three launches, of operands as bf16 numbers.)
+constexpr double kShallowTiles = 4096;
 // Whether the products go by tiles of 64 to 256, by what a call takes (microseconds) beside 3.5 either way: the kernel of few tokens 0.3 for each
 // thousand blocks of 16 x 16 x 128, the other, with the launch before it, 1.5 and 0.33 for each block of the depth; for fp32 results 0.48, and
 // 3 and 0.75.  1024 -> 4096 in bf16, 64 rows 6.3 and 7.4, 128 rows 8.6 and 7.5; 2048 -> 1000, 256 rows 11.0 and 10.5, 512 rows 13.4 and 11.2;
@@ -622,6 +626,7 @@ constexpr int64_t kSomeTiles = 512, kManyTiles = 1024;
 // 15.4, 256 rows 20.6 and 16.5.
 bool is_large(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) {
     const double blocks = static_cast<double>(blocks8(depth)), tiles = static_cast<double>((rows + 15) / 16) * static_cast<double>((outputs + 15) / 16);
+    if (out_dtype != ADASUM_F32 && blocks == 1) return tiles > kShallowTiles;
     return depth > 0 && (out_dtype == ADASUM_F32 ? 0.00048 * tiles * blocks > 3 + 0.75 * blocks : 0.0003 * tiles * blocks > 1.5 + 0.33 * blocks);
 }
 // Whether operands are multiplied as the bf16 numbers that they stand for: for fp32 results, and where a tile would have two steps only (the

@@ -1,4 +1,4 @@
-"""Products of at most 128 in depth with 16-bit results, by tiles of 64: from some 6100 tiles of 16 x 16 on, in at most 128 tiles of edge 128."""
+"""Products of at most 128 in depth with 16-bit results, by tiles of 64: of more than 4096 tiles of 16 x 16, in at most 128 tiles of edge 128."""
 import numpy as np
 import pytest
 import torch
@@ -11,7 +11,7 @@ from test_gpu_linear_products import bound, near, spread
 pytestmark = pytest.mark.gpu
 TYPES = [torch.bfloat16, torch.float16]
 SIZES = [(2048, 128, 1024), (2000, 100, 1000), (4093, 64, 500), (16384, 128, 128), (16300, 60, 120), (500, 64, 4090), (1568, 128, 1000), (2048, 7, 1024),
-         (1985, 1, 1021)]                         # rows, depth, results of a row
+         (1985, 1, 1021), (1100, 100, 1000), (1088, 128, 1024), (8800, 33, 120)]                         # rows, depth, results of a row
 GUARD = 77.0
 
 
