@@ -529,7 +529,9 @@ __global__ void __launch_bounds__(256) join_finish_kernel(Finish f) {
         const double gate = param_at(f.gate, f.param_type, j, 1.0);
         put(f.to[0], gate * sum[0]);
         put(f.to[1], gate * sum[1]);
-        put(f.to[2], param_at(f.after_weight, f.param_type, j, 1.0) * sum[0] + param_at(f.after_bias, f.param_type, j, 0.0) * sum[1]);
+        // (without a bias the second sum is not asked for, whatever it is)
+        const double weighed = param_at(f.after_weight, f.param_type, j, 1.0) * sum[0];
+        put(f.to[2], f.after_bias == nullptr ? weighed : weighed + param_at(f.after_bias, f.param_type, j, 0.0) * sum[1]);
     } else {
         put(f.to[3], sum[0]);
         put(f.to[4], sum[1]);
