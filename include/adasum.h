@@ -505,12 +505,14 @@ ADASUM_API int adasum_join_grad(const adasum_join_form* form, const void* params
                                 void* grad, int grad_dtype, int accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * (Linear layers: no relation to ADASUM_ORDER_LINEAR, the reduction's order from left to right.)
  * Linear layers whose products are taken in 8-bit floating point (e4m3: 1 sign, 4 exponent and 3 fraction bits, at most 448).
  * Blocks of ADASUM_LINEAR_BLOCK channels of a row of activations (or gradients), and of 128 outputs x 128 inputs of a weight, share
  * an exponent e: the least with max |x| <= 448 * 2^e, but at least -120, where the largest finite value counts.  x / 2^e is
  * rounded to nearest even; infinities and NaN become NaN.  Products of the rounded operands are exact.  For fp32 results they are summed in
  * fp32 (operands as bf16 numbers: from 1.9375 * 2^127 on they are infinities); for 16-bit results by the 8-bit matrix cores, which cut off
- * what lies 2^-13 below the largest (its power of two) of the products of eight consecutive channels, and add the rest in fp32.
+ * what lies 2^-13 below the largest (its power of two) of the products of eight consecutive channels, and add the rest in fp32 (large
+ * products of at most 128 in depth are taken as fp32 results are).  Ask for fp32 results where that cut counts.
  *
  * adasum_linear_store puts the weight of a layer (outputs x width, row-major, at `offset` of the flat buffer `params`) into 8 bits, once
  * as it is and once transposed, with the same blocks: adasum_linear_bytes, 16-byte aligned.  Layout: panels of 64

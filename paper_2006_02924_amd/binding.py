@@ -4,6 +4,12 @@ Argument marshalling only: every step of the path runs in the library's HIP
 kernels.  PyTorch supplies device memory (``tensor.data_ptr()``) and the current
 HIP stream.  There is no fallback: if the library has not been built,
 ``load()`` raises.
+
+The calls stand outside of autograd: tensors that require gradients are read
+and written as they are, results carry no graph, and a ``backward()`` through
+them finds nothing.  The gradients are calls of their own
+(``adasum_..._grad``; of ``adasum_dropout``, the same call), which a program
+makes itself or from the ``backward`` of a ``torch.autograd.Function``.
 """
 from __future__ import annotations
 
