@@ -65,3 +65,21 @@ def test_a_small_spread_beside_a_large_mean():
     # spread (whose mean size is at most that); the spread by as many of itself
     off = 1.1 * DEPTH * U32
     assert (np.abs(f64(y) - t / spread) <= off * off * 4096 / spread + (DEPTH + 10) * U32 * (1 + np.abs(t / spread))).all()
+
+
+@pytest.mark.parametrize("width", WIDTHS[1:])
+def test_other_rows_do_not_notice(width):
+    """The same bits for ordinary rows, whatever the rows beside them in a wave or a workgroup are."""
+    g = torch.Generator().manual_seed(width)
+    x, dy = torch.randn(70, width, generator=g), torch.randn(70, width, generator=g)
+    mixed = x.clone()
+    mixed[::3] = 100.3
+    mixed[1::6] += 4000.0
+    rest = [i for i in range(70) if i % 3 and i % 6 != 1]
+    form = B.Join(width, torch.float32, eps=EPS)
+    out = []
+    for t in (x, mixed):
+        y = B.adasum_join(form, None, t.cuda(), keep_h=False)[1]
+        out.append((y, B.adasum_join_grad(form, None, None, h=t.cuda(), dy=dy.cuda(), dresidual=False)[0]))
+    for a, b in zip(*out):
+        assert torch.equal(a[rest], b[rest])
