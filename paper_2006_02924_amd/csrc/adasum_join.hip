@@ -8,9 +8,11 @@
 // workgroup's rows, which meet in fp64 (rounded once into the workspace), and a second launch adds the workgroups' in fp64.  The gradient
 // works the statistics out again from the rows that it reads anyhow: nothing is kept for it but the rows themselves.
 //
-// Memory bounds it: 16384 x 1024 in bf16 with dropout (134 MB) 28 us, its gradient 30 and 4 for the second launch; 32749 x 1024 with an fp32 stream and
-// all parts (604 MB), gradient 114 - 118 us, 5.1 TB/s.  The vector units take half to two thirds of that, so that what they do counts: rows that fill their
-// lanes have no masks, two sums serve three parameters, weight and gate are one vector (gradient 134 us with five sums and three vectors).
+// Memory bounds it: 16384 x 1024 in bf16 with dropout (134 MB) 29 us, its gradient 31 and 4 for the second launch; 32749 x 1024 with an fp32 stream and
+// all parts (604 MB), gradient 116 - 119 us, 5.1 TB/s.  The vector units take half to two thirds of that, so that what they do counts: rows that fill their
+// lanes have no masks, two sums serve three parameters, weight and gate are one vector (gradient 134 us with five sums and three vectors).  Above 4096 channels with
+// all parts the gradient's registers do not suffice: 512 lanes have 256 each, in fp32 24 (filled lanes), 69 (whole granules) and some 480 (ragged rows)
+// are kept in memory, in bf16 none, 1 and 27.
 #include <hip/hip_runtime.h>
 
 #include "adasum_layers.h"
