@@ -450,8 +450,8 @@ ADASUM_API int adasum_dropout(const void* x, int dtype, int64_t x_stride, int64_
  * N of a row t: (t - mean t) / sqrt(mean (t - mean t)^2 + eps) (ADASUM_NORM_LAYER) or t / sqrt(mean t^2 + eps) (ADASUM_NORM_RMS).
  * Weights, biases and the gate are vectors of `width` elements at offsets of the flat buffer `params`; a negative offset means that
  * there is none (1 for a weight and the gate, 0 for a bias), and those of a norm that is not there are not looked at.
- * y is that of h before h's rounding.  A row whose squares leave the range of fp32 (from some 1e19 on) is NaN behind its norm, and
- * behind the gradient of that; it makes NaN of the vectors' gradients that sum over it.
+ * y is that of h before h's rounding.  A row whose squares leave the range of fp32 in their sum (one value from 1.8e19 on, 8192 from 2e17
+ * on) is NaN behind its norm, and behind the gradient of that; it makes NaN of the vectors' gradients that sum over it.
  */
 #define ADASUM_NORM_LAYER 0
 #define ADASUM_NORM_RMS   1
