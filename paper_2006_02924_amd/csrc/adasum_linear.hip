@@ -621,9 +621,10 @@ constexpr int64_t kSomeTiles = 512, kManyTiles = 1024;
 constexpr double kShallowTiles = 4096;
 // Whether the products go by tiles of 64 to 256, by what a call takes (microseconds) beside 3.5 either way: the kernel of few tokens 0.3 for each
 // thousand blocks of 16 x 16 x 128, the other, with the launch before it, 1.5 and 0.33 for each block of the depth; for fp32 results 0.48, and
-// 3 and 0.75.  1024 -> 4096 in bf16, 64 rows 6.3 and 7.4, 128 rows 8.6 and 7.5; 2048 -> 1000, 256 rows 11.0 and 10.5, 512 rows 13.4 and 11.2;
-// 8192 -> 8192, 32 rows 22 and 27, 64 rows 38 and 28; 256 -> 256, 2048 rows 5.2 and 5.6, 4096 rows 8.7 and 6.2; fp32 1024 -> 4096, 128 rows 12.5 and
-// 15.4, 256 rows 20.6 and 16.5.
+// 3 and 0.75.  (Fitted; both ways:)  1024 -> 4096 in bf16, 64 rows 6.0 and 7.0, 128 rows 8.1 and 7.2; 2048 -> 1000, 256 rows 10 and 10, 512 rows
+// 12.2 and 10.8; 8192 -> 8192, 32 rows 21 and 26, 64 rows 35 and 26; 256 -> 256, 2048 rows 5.1 and 5.3, 4096 rows 8.4 and 5.8; fp32 1024 -> 4096, 128
+// rows 12 and 15, 256 rows 20 and 16; 2048 -> 1000, 512 rows 20 and 20.  It does not count the values of a large weight, which fp32 results
+// take a launch more for: 8192 -> 8192 in fp32, 64 rows 54 and 83, by tiles all the same.
 bool is_large(int64_t rows, int64_t outputs, int64_t depth, int out_dtype) {
     const double blocks = static_cast<double>(blocks8(depth)), tiles = static_cast<double>((rows + 15) / 16) * static_cast<double>((outputs + 15) / 16);
     if (out_dtype != ADASUM_F32 && blocks == 1) return tiles > kShallowTiles;
